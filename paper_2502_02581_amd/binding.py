@@ -22,7 +22,10 @@ EXPORTS = ["moe_abi_version", "moe_last_error", "moe_route_bwd", "moe_router_fwd
            "moe_plan_overlap_degree", "moe_plan_predict_load", "moe_plan_materialize", "moe_plan_dispatch",
            "moe_dispatch_static", "moe_mfma_probe", "moe_expert_fwd_gather", "moe_expert_bwd_gather",
            "moe_route_dispatch_workspace_bytes", "moe_route_dispatch", "moe_route_aux_bwd", "moe_experts_fwd",
-           "moe_experts_bwd", "moe_expert_plan_bytes", "moe_route_dispatch_plan"]
+           "moe_experts_bwd", "moe_expert_plan_bytes", "moe_route_dispatch_plan",
+           "moe_quant_row_bytes", "moe_quant_scale_bytes", "moe_quant_rows", "moe_quant_weights", "moe_quant_gemm_workspace_bytes",
+           "moe_quant_gemm", "moe_quant_expert_fwd_workspace_bytes", "moe_quant_expert_bwd_workspace_bytes", "moe_quant_expert_fwd",
+           "moe_quant_expert_bwd", "moe_grad_norm_workspace_bytes", "moe_grad_norm", "moe_grad_clip"]
 
 
 class MoEError(RuntimeError):
@@ -38,6 +41,16 @@ class _CExpertSet(ctypes.Structure):   # moe_expert_set_t
                 [(n, ctypes.c_void_p) for n in ("offsets", "src_of", "Xin", "Wg", "Wu", "Wd", "G", "U", "H", "Yout", "dYin", "dY",
                                                 "row_w", "dXin", "active_ids", "n_active", "dWg_c", "dWu_c", "dWd_c", "ws")] +
                 [("ws_bytes", ctypes.c_size_t), ("plan", ctypes.c_void_p)])
+
+
+class _CQuantWeights(ctypes.Structure):   # moe_quant_weights_t
+    _fields_ = [(n, ctypes.c_void_p) for n in ("WgT", "WgT_s", "WuT", "WuT_s", "WdT", "WdT_s", "Wgu", "Wgu_s", "Wd", "Wd_s")] + \
+               [("gated", ctypes.c_int32)]
+
+
+class _CGrad(ctypes.Structure):   # moe_grad_t
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("n_active", ctypes.c_void_p),
+                ("slot", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 @dataclasses.dataclass(frozen=True)
@@ -138,6 +151,31 @@ def load_library():
     for f in (lib.moe_experts_fwd, lib.moe_experts_bwd):
         f.restype = ctypes.c_int
         f.argtypes = [shp, ctypes.POINTER(_CExpertSet), ctypes.POINTER(_CExpertSet), vp]
+    i64, qw, grads = ctypes.c_int64, ctypes.POINTER(_CQuantWeights), ctypes.POINTER(_CGrad)
+    for f in (lib.moe_quant_row_bytes, lib.moe_quant_scale_bytes):
+        f.restype = i64
+        f.argtypes = [i64]
+    lib.moe_quant_rows.restype = ctypes.c_int
+    lib.moe_quant_rows.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
+    lib.moe_quant_weights.restype = ctypes.c_int
+    lib.moe_quant_weights.argtypes = [vp, i32, i32, i32, i32] + [vp, i64] * 4 + [vp]
+    lib.moe_quant_gemm_workspace_bytes.restype = sz
+    lib.moe_quant_gemm_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.moe_quant_gemm.restype = ctypes.c_int
+    lib.moe_quant_gemm.argtypes = [i32, vp, i32, i32, i32] + [vp] * 6 + [sz, vp]
+    for f in (lib.moe_quant_expert_fwd_workspace_bytes, lib.moe_quant_expert_bwd_workspace_bytes):
+        f.restype = sz
+        f.argtypes = [shp, i32, i32]
+    lib.moe_quant_expert_fwd.restype = ctypes.c_int
+    lib.moe_quant_expert_fwd.argtypes = [shp, i32, vp, i32, vp, vp, vp, qw] + [vp] * 6 + [sz, vp]
+    lib.moe_quant_expert_bwd.restype = ctypes.c_int
+    lib.moe_quant_expert_bwd.argtypes = [shp, i32, vp, i32] + [vp] * 5 + [qw] + [vp] * 11 + [sz, vp]
+    lib.moe_grad_norm_workspace_bytes.restype = sz
+    lib.moe_grad_norm_workspace_bytes.argtypes = []
+    lib.moe_grad_norm.restype = ctypes.c_int
+    lib.moe_grad_norm.argtypes = [grads, i32, vp, vp, sz, vp]
+    lib.moe_grad_clip.restype = ctypes.c_int
+    lib.moe_grad_clip.argtypes = [grads, i32, vp, ctypes.c_float, vp]
     lib.moe_combine.restype = ctypes.c_int
     lib.moe_combine.argtypes = [shp, vp, vp, vp, vp, vp, vp]
     lib.moe_combine_bwd.restype = ctypes.c_int
@@ -462,6 +500,225 @@ def moe_combine_bwd(shape: MoEShape, dY, Yp, row_of, topk_w, dYp, dw, stream=Non
                                         _ptr(row_of, torch.int32, "row_of"), _ptr(topk_w, torch.float32, "topk_w"),
                                         _ptr(dYp, dt, "dYp"), _ptr(dw, torch.float32, "dw"), _stream(stream))
     _check(rc, "moe_combine_bwd")
+
+
+# ---- block-scaled 8-bit tensors: codes and exponent bytes are uint8 tensors
+def _value_dtype(t, what):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise MoEError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+    return MOE_F32 if t.dtype == torch.float32 else MOE_BF16
+
+
+def _sized(t, shape, what, dtype=torch.uint8):
+    """The pointer of a contiguous tensor of exactly this shape."""
+    if tuple(t.shape) != tuple(shape):
+        raise MoEError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _ptr(t, dtype, what)
+
+
+def _pitched(t, shape, what):
+    """Pointer and bytes between rows of a [groups, rows, bytes] tensor whose rows may be pieces of longer ones."""
+    if t is None:
+        return None, 0
+    if tuple(t.shape) != tuple(shape):
+        raise MoEError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_cuda or t.dtype != torch.uint8:
+        raise MoEError(f"{what} must be a uint8 tensor on the GPU")
+    rows = shape[1]
+    ld = t.stride(1) if rows > 1 else (t.stride(0) if shape[0] > 1 else shape[2])
+    if (shape[2] > 1 and t.stride(2) != 1) or (shape[0] > 1 and t.stride(0) != rows * ld):
+        raise MoEError(f"{what}: the bytes of a row must be adjacent, and groups follow each other")
+    return t.data_ptr(), ld
+
+
+def moe_quant_row_bytes(cols: int) -> int:
+    """Bytes of a row of codes: cols rounded up to whole blocks of 128."""
+    return int(load_library().moe_quant_row_bytes(int(cols)))
+
+
+def moe_quant_scale_bytes(cols: int) -> int:
+    """Bytes of a row of exponents: one a block of 128."""
+    return int(load_library().moe_quant_scale_bytes(int(cols)))
+
+
+def moe_quant_rows(X, Q, S, stream=None):
+    """Block-scaled rows of X [n_rows, cols] (f32 or bf16; rows may be strided): codes Q [n_rows, moe_quant_row_bytes(cols)], exponents
+    S [n_rows, moe_quant_scale_bytes(cols)]."""
+    dt = _value_dtype(X, "X")
+    if X.dim() != 2 or not X.is_cuda or (X.shape[1] > 1 and X.stride(1) != 1):
+        raise MoEError("X must be a matrix on the GPU whose rows' values are adjacent")
+    n, cols = X.shape
+    ldx = max(X.stride(0), cols) if n > 1 else cols
+    if n > 1 and X.stride(0) < cols:
+        raise MoEError("X: rows must not overlap")
+    rc = load_library().moe_quant_rows(X.data_ptr(), dt, n, cols, ldx, _sized(Q, (n, moe_quant_row_bytes(cols)), "Q"),
+                                       _sized(S, (n, moe_quant_scale_bytes(cols)), "S"), _stream(stream))
+    _check(rc, "moe_quant_rows")
+
+
+def moe_quant_weights(W, Q, S, Qt, St, stream=None):
+    """Block-scaled matrices of W [groups, K, N] (f32 or bf16): as stored, Q [groups, K, moe_quant_row_bytes(N)] and S [groups, ceil(K / 128),
+    moe_quant_scale_bytes(N)], and transposed, Qt [groups, N, moe_quant_row_bytes(K)] and St; either pair may be None."""
+    dt = _value_dtype(W, "W")
+    if W.dim() != 3:
+        raise MoEError("W must be [groups, K, N]")
+    g, K, N = W.shape
+    b = moe_quant_scale_bytes
+    args = []
+    for t, shape, what in ((Q, (g, K, moe_quant_row_bytes(N)), "Q"), (S, (g, b(K), b(N)), "S"),
+                           (Qt, (g, N, moe_quant_row_bytes(K)), "Qt"), (St, (g, b(N), b(K)), "St")):
+        args += _pitched(t, shape, what)
+    _check(load_library().moe_quant_weights(_ptr(W, None, "W"), dt, g, K, N, *args, _stream(stream)), "moe_quant_weights")
+
+
+def moe_quant_gemm_workspace_bytes(n_groups: int, n_rows: int, K: int, N: int) -> int:
+    return int(load_library().moe_quant_gemm_workspace_bytes(n_groups, n_rows, K, N))
+
+
+def moe_quant_gemm(offsets, K: int, A, As, B, Bs, C, ws, stream=None):
+    """C [n_rows, N] (bf16) = A B_g^T over the rows of every group: A, As from moe_quant_rows on rows of K values, B [groups, N, .], Bs the transposed
+    layout of moe_quant_weights; offsets [groups + 1], or None for one group."""
+    (n, N), g = C.shape, B.shape[0]
+    kb, rb = moe_quant_scale_bytes(K), moe_quant_row_bytes(K)
+    if offsets is not None:
+        _sized(offsets, (g + 1,), "offsets", torch.int32)
+    rc = load_library().moe_quant_gemm(g, _ptr(offsets, torch.int32, "offsets"), n, K, N, _sized(A, (n, rb), "A"), _sized(As, (n, kb), "As"),
+                                       _sized(B, (g, N, rb), "B"), _sized(Bs, (g, moe_quant_scale_bytes(N), kb), "Bs"),
+                                       _ptr(C, torch.bfloat16, "C"), _ptr(ws, None, "ws"), ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc, "moe_quant_gemm")
+
+
+class MoEQuantWeights:
+    """Block-scaled matrices of one set of experts in the layouts of the two passes (moe_quant_weights_t).
+
+    A training program makes one with its layer and calls update(Wg, Wu, Wd) after every optimiser step; a serving program calls update once
+    (backward=False: no layouts of the backward pass).  of_codes wraps codes and exponents that exist already."""
+
+    def __init__(self, shape: MoEShape, n_groups: int, gated: bool = True, backward: bool = True, device="cuda:0"):
+        d, F, n = shape.d, shape.d_ff, n_groups
+        self.shape, self.n_groups, self.gated, self.backward = shape, n, bool(gated), bool(backward)
+        b, r = moe_quant_scale_bytes, moe_quant_row_bytes
+        mats = 2 if gated else 1
+
+        def pair(rows, *cols):
+            return (torch.empty(n, rows, sum(r(c) for c in cols), dtype=torch.uint8, device=device),
+                    torch.empty(n, b(rows), sum(b(c) for c in cols), dtype=torch.uint8, device=device))
+
+        self.WgT, self.WuT, self.WdT = pair(F, d), pair(F, d) if gated else None, pair(d, F)
+        self.Wgu, self.Wd = (pair(d, *[F] * mats), pair(F, d)) if backward else (None, None)
+
+    @classmethod
+    def of_codes(cls, shape: MoEShape, n_groups: int, WgT, WuT, WdT):
+        """From (codes, exponents) of the transposed matrices: WgT, WuT [groups, d_ff, .], WdT [groups, d, .]; WuT None for two-matrix experts.
+        For the forward pass."""
+        self = cls.__new__(cls)
+        self.shape, self.n_groups, self.gated, self.backward = shape, n_groups, WuT is not None, False
+        self.WgT, self.WuT, self.WdT, self.Wgu, self.Wd = WgT, WuT, WdT, None, None
+        return self
+
+    def update(self, Wg, Wu, Wd, stream=None):
+        """Quantises the matrices Wg, Wu [groups, d, d_ff], Wd [groups, d_ff, d] (Wu None for two-matrix experts)."""
+        s, n = self.shape, self.n_groups
+        if (Wu is not None) != self.gated:
+            raise MoEError("Wu goes with gated experts")
+        for w, shape, what in ((Wg, (n, s.d, s.d_ff), "Wg"), (Wu, (n, s.d, s.d_ff), "Wu"), (Wd, (n, s.d_ff, s.d), "Wd")):
+            if w is not None and tuple(w.shape) != shape:
+                raise MoEError(f"{what} must have shape {shape}, got {tuple(w.shape)}")
+        rF, bF = moe_quant_row_bytes(s.d_ff), moe_quant_scale_bytes(s.d_ff)
+        for i, (w, t) in enumerate(((Wg, self.WgT), (Wu, self.WuT))):
+            if w is not None:
+                q, e = (self.Wgu[0][:, :, i * rF:(i + 1) * rF], self.Wgu[1][:, :, i * bF:(i + 1) * bF]) if self.Wgu else (None, None)
+                moe_quant_weights(w, q, e, *t, stream)
+        moe_quant_weights(Wd, *(self.Wd or (None, None)), *self.WdT, stream)
+
+    def _c(self, who, backward) -> _CQuantWeights:
+        s, n = self.shape, self.n_groups
+        b, r = moe_quant_scale_bytes, moe_quant_row_bytes
+        if backward and self.Wgu is None:
+            raise MoEError(f"{who}: these weights have no layouts of the backward pass")
+
+        def ptrs(pair, rows, cols, mats, what):
+            if pair is None:
+                return None, None
+            return (_sized(pair[0], (n, rows, mats * r(cols)), what), _sized(pair[1], (n, b(rows), mats * b(cols)), what + " exponents"))
+
+        d, F = s.d, s.d_ff
+        mats = 2 if self.gated else 1
+        return _CQuantWeights(*ptrs(self.WgT, F, d, 1, "WgT"), *ptrs(self.WuT, F, d, 1, "WuT"), *ptrs(self.WdT, d, F, 1, "WdT"),
+                              *ptrs(self.Wgu, d, F, mats, "Wgu"), *ptrs(self.Wd, F, d, 1, "Wd"), int(self.gated))
+
+
+def moe_quant_expert_fwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int) -> int:
+    return int(load_library().moe_quant_expert_fwd_workspace_bytes(ctypes.byref(shape.c()), n_groups, n_rows))
+
+
+def moe_quant_expert_bwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int) -> int:
+    return int(load_library().moe_quant_expert_bwd_workspace_bytes(ctypes.byref(shape.c()), n_groups, n_rows))
+
+
+def _quant_args(shape, n_groups, n_rows, src_of, Q, S, W, who):
+    if W.n_groups != n_groups or (W.shape.d, W.shape.d_ff) != (shape.d, shape.d_ff):
+        raise MoEError(f"{who}: the weights are those of {W.n_groups} experts of d={W.shape.d}, d_ff={W.shape.d_ff}")
+    rows = n_rows if src_of is None else shape.T
+    return (_sized(Q, (rows, moe_quant_row_bytes(shape.d)), "codes"), _sized(S, (rows, moe_quant_scale_bytes(shape.d)), "exponents"))
+
+
+def moe_quant_expert_fwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, XQ, XS, W: MoEQuantWeights, G, U, H, Yout, ws, plan=None, stream=None):
+    """Forward pass of routed experts on block-scaled operands; G, U and H None where no backward pass follows."""
+    bf = torch.bfloat16
+    q = _quant_args(shape, n_groups, n_rows, src_of, XQ, XS, W, "moe_quant_expert_fwd")
+    rc = load_library().moe_quant_expert_fwd(
+        ctypes.byref(shape.c()), n_groups, _ptr(offsets, torch.int32, "offsets"), n_rows, _ptr(src_of, torch.int32, "src_of"), *q,
+        ctypes.byref(W._c("moe_quant_expert_fwd", False)), _ptr(G, bf, "G"), _ptr(U, bf, "U"), _ptr(H, bf, "H"), _ptr(Yout, bf, "Yout"),
+        _ptr(plan, torch.uint8, "plan"), _ptr(ws, None, "ws"), ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc, "moe_quant_expert_fwd")
+
+
+def moe_quant_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, row_w, dYQ, dYS, Xin, W: MoEQuantWeights, G, U, H, dYin, dXin,
+                         active_ids, n_active, dWg_c, dWu_c, dWd_c, ws, stream=None):
+    """Backward pass of moe_quant_expert_fwd: input gradients on block-scaled operands, weight gradients in bf16."""
+    bf, i32 = torch.bfloat16, torch.int32
+    q = _quant_args(shape, n_groups, n_rows, src_of, dYQ, dYS, W, "moe_quant_expert_bwd")
+    rc = load_library().moe_quant_expert_bwd(
+        ctypes.byref(shape.c()), n_groups, _ptr(offsets, i32, "offsets"), n_rows, _ptr(src_of, i32, "src_of"),
+        _ptr(row_w, torch.float32, "row_w"), *q, _ptr(Xin, bf, "Xin"), ctypes.byref(W._c("moe_quant_expert_bwd", True)), _ptr(G, bf, "G"),
+        _ptr(U, bf, "U"), _ptr(H, bf, "H"), _ptr(dYin, bf, "dYin"), _ptr(dXin, bf, "dXin"), _ptr(active_ids, i32, "active_ids"),
+        _ptr(n_active, i32, "n_active"), _ptr(dWg_c, bf, "dWg_c"), _ptr(dWu_c, bf, "dWu_c"), _ptr(dWd_c, bf, "dWd_c"), _ptr(ws, None, "ws"),
+        ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc, "moe_quant_expert_bwd")
+
+
+# ---- gradients: lists of tensors, or of (tensor, n_active) for compacted ones [slots, ...]
+def _grad_list(grads, out=None):
+    c = (_CGrad * max(1, len(grads)))()
+    if out is not None and len(out) != len(grads):
+        raise MoEError(f"{len(grads)} gradients, {len(out)} outputs")
+    for i, x in enumerate(grads):
+        g, n_active = x if isinstance(x, (tuple, list)) else (x, None)
+        dt, o = _value_dtype(g, f"gradient {i}"), g if out is None else out[i]
+        if tuple(o.shape) != tuple(g.shape):
+            raise MoEError(f"output {i} must have shape {tuple(g.shape)}, got {tuple(o.shape)}")
+        slot = g.numel() // g.shape[0] if n_active is not None and g.dim() and g.shape[0] else 1
+        c[i] = _CGrad(_ptr(g, None, f"gradient {i}"), _ptr(o, g.dtype, f"output {i}"), g.numel(), _ptr(n_active, torch.int32, "n_active"), slot, dt)
+    return c
+
+
+def moe_grad_norm_workspace_bytes() -> int:
+    return int(load_library().moe_grad_norm_workspace_bytes())
+
+
+def moe_grad_norm(grads, norm, ws, stream=None):
+    """norm [1] = the norm of all gradients taken as one vector.  An entry is a tensor, or (tensor [slots, ...], n_active): a compacted
+    gradient, whose first n_active slots (a number on the GPU) count."""
+    rc = load_library().moe_grad_norm(_grad_list(grads), len(grads), _ptr(norm, torch.float32, "norm"), _ptr(ws, None, "ws"),
+                                      ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc, "moe_grad_norm")
+
+
+def moe_grad_clip(grads, norm, max_norm: float, out=None, stream=None):
+    """The same list times min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
+    rc = load_library().moe_grad_clip(_grad_list(grads, out), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
+    _check(rc, "moe_grad_clip")
 
 
 def moe_copy_probe(src: torch.Tensor, dst: torch.Tensor):

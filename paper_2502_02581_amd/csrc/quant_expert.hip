@@ -1,0 +1,344 @@
+// moe_quant_gemm, moe_quant_expert_fwd / _bwd: grouped products of block-scaled 8-bit tensors.
+#include "expert_impl.h"
+#include "quant_gemm.h"
+
+namespace moe {
+
+typedef __attribute__((ext_vector_type(8))) int32_t code_frag_t;  // 32 codes of a lane
+
+template <int NB, int EPI>
+__global__ __launch_bounds__(256) void quant_gemm_kernel(QuantGemm p) {
+  typedef Epilogue<bf16_t, NB, EPI> Epi;
+  constexpr int BN = 256 / NB, TN = 4 / NB;
+  const int ntn = (p.N + BN - 1) / BN;
+  const int n_mt = p.tiles ? *p.n_tiles : (p.n_rows + 255) / 256;
+  const int mt = blockIdx.x / ntn, nt = blockIdx.x - mt * ntn;
+  if (mt >= n_mt) return;
+  RowTile t;
+  if (p.tiles) t = p.tiles[mt];
+  else { t.group = 0; t.row0_in = mt * 256; t.rows = min(256, p.n_rows - t.row0_in); t.row0_out = t.row0_in; }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, h = lane >> 4;
+  const int rows = tile_rows(t), n0 = nt * BN + wave * TN * 16;
+  Epi epi;
+  for (int m0 = 0; m0 < rows; m0 += 16) {
+    const int r = t.row0_in + m0 + l;
+    const bool ok = m0 + l < rows;
+    const int64_t ar = ok ? (p.a_index ? p.a_index[r] / p.a_index_div : r) : 0;
+    f32x4_t acc[NB][TN];
+#pragma unroll
+    for (int b = 0; b < NB; b++)
+#pragma unroll
+      for (int j = 0; j < TN; j++) acc[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int kb = 0; kb < p.nk; kb++) {
+      code_frag_t a = {};
+      if (ok) a = *reinterpret_cast<const code_frag_t*>(p.A + ar * p.lda + kb * kQuantBlock + h * 32);
+      const int sa = ok ? p.As[ar * p.las + kb] : 127;
+#pragma unroll
+      for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) {
+          const int n = n0 + j * 16 + l;
+          code_frag_t w = {};
+          int sb = 127;
+          if (n < p.N) {
+            w = *reinterpret_cast<const code_frag_t*>(p.B[b] + t.group * p.b_group + (int64_t)n * p.ldb + kb * kQuantBlock + h * 32);
+            sb = p.Bs[b][t.group * p.bs_group + n / kQuantBlock * p.lbs + kb];
+          }
+          acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, acc[b][j], 0, 0, 0, sb, 0, sa);
+        }
+    }
+    if (!ok) continue;
+    const float scale = (EPI == EPI_SWIGLU_BWD || EPI == EPI_GELU_BWD) && p.c_scale ? p.c_scale[p.a_index[r]] : 1.f;
+#pragma unroll
+    for (int j = 0; j < TN; j++) {
+      const int n = n0 + j * 16 + h * 4;
+      if (n >= p.N) continue;
+      constexpr int NA = Epi::NAUX > 0 ? Epi::NAUX : 1;
+      const int64_t at = (int64_t)(t.row0_out + m0 + l) * p.ldc + n;
+      float v[NB][4], a[NA][4], o[Epi::NOUT][4];
+#pragma unroll
+      for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) v[b][q] = acc[b][j][q];
+#pragma unroll
+      for (int x = 0; x < Epi::NAUX; x++) Epi::unpack(*reinterpret_cast<const typename Epi::packed_t*>((const bf16_t*)p.in[x] + at), a[x]);
+      epi.apply(v, a, scale, o);
+#pragma unroll
+      for (int x = 0; x < Epi::NOUT; x++)
+        if (p.out[x]) Epi::pack((bf16_t*)p.out[x] + at, o[x]);
+    }
+  }
+}
+
+// At most max_tiles row tiles (the device knows how many there are).
+template <int NB, int EPI>
+static void launch_quant(const char* label, const QuantGemm& p, int max_tiles, hipStream_t st) {
+  const unsigned blocks = (unsigned)max_tiles * (unsigned)ceil_div(p.N, 256 / NB);
+  if (blocks == 0) return;
+  ProfScope prof(label, st);
+  hipLaunchKernelGGL((quant_gemm_kernel<NB, EPI>), dim3(blocks), dim3(256), 0, st, p);
+}
+
+// ------------------------------------------------------------------------------------ one product
+static int quant_tiles(int n_groups, int n_rows) { return max_row_tiles(MOE_BF16, n_groups, n_rows, INT32_MAX); }
+static size_t quant_plan_size(int n_groups, int n_rows) { return align_up(plan_bytes(n_groups, plan_cap(n_groups, n_rows) + 1), 256); }
+
+static int check_groups(int n_groups, int n_rows, const char* who) {
+  if (n_groups >= 1 && n_groups <= MOE_MAX_EXPERTS && n_rows >= 0 && n_rows < 1 << 30) return MOE_OK;
+  set_error("%s: bad n_groups=%d n_rows=%d", who, n_groups, n_rows);
+  return MOE_EINVAL;
+}
+// the tiles of a launch are counted in 32 bits
+static int check_launch(int n_groups, int n_rows, int64_t cols, const char* who) {
+  if ((quant_tiles(n_groups, n_rows) + 1) * (cols / 128 + 1) < (int64_t)1 << 31) return MOE_OK;
+  set_error("%s: %d rows of %lld columns are too many", who, n_rows, (long long)cols);
+  return MOE_EINVAL;
+}
+
+}  // namespace moe
+
+extern "C" size_t moe_quant_gemm_workspace_bytes(int32_t n_groups, int32_t n_rows, int32_t K, int32_t N) {
+  using namespace moe;
+  if (n_groups < 1 || n_groups > MOE_MAX_EXPERTS || n_rows < 0 || K < 1 || N < 1) return 0;
+  return quant_plan_size(n_groups, n_rows);
+}
+
+extern "C" int moe_quant_gemm(int32_t n_groups, const int32_t* offsets, int32_t n_rows, int32_t K, int32_t N, const void* A, const void* As,
+                              const void* B, const void* Bs, void* C, void* ws, size_t ws_bytes, void* stream) {
+  using namespace moe;
+  const int rc = check_groups(n_groups, n_rows, "moe_quant_gemm");
+  if (rc) return rc;
+  if (K < 1 || N < 1 || N % 8 || K > 1 << 24 || N > 1 << 24 || (!offsets && n_groups != 1)) {
+    set_error("moe_quant_gemm: bad K=%d N=%d n_groups=%d (N a multiple of 8; one group where there are no offsets)", K, N, n_groups);
+    return MOE_EINVAL;
+  }
+  if (!B || !Bs || !ws || (n_rows > 0 && (!A || !As || !C))) {
+    set_error("moe_quant_gemm: null pointer");
+    return MOE_EINVAL;
+  }
+  if (!aligned16(A) || !aligned16(B) || !aligned16(C) || !aligned16(ws)) {
+    set_error("moe_quant_gemm: every tensor must be 16-byte aligned");
+    return MOE_EINVAL;
+  }
+  const int rl = check_launch(n_groups, n_rows, N, "moe_quant_gemm");
+  if (rl) return rl;
+  const size_t need = moe_quant_gemm_workspace_bytes(n_groups, n_rows, K, N);
+  if (ws_bytes < need) {
+    set_error("moe_quant_gemm: workspace of %zu bytes, need %zu", ws_bytes, need);
+    return MOE_EWS;
+  }
+  if (n_rows == 0) return MOE_OK;
+  hipStream_t st = (hipStream_t)stream;
+  QuantGemm p = {};
+  int tiles = ceil_div(n_rows, 256);
+  if (offsets) {
+    const Plan pl = carve_plan(ws, n_groups, plan_cap(n_groups, n_rows));
+    launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
+    p.tiles = pl.tiles; p.n_tiles = pl.n_tiles;
+    tiles = quant_tiles(n_groups, n_rows);
+  }
+  p.n_rows = n_rows; p.N = N; p.nk = (int)quant_blocks(K);
+  p.A = (const uint8_t*)A; p.As = (const uint8_t*)As; p.lda = quant_row(K); p.las = p.nk;
+  p.B[0] = (const uint8_t*)B; p.Bs[0] = (const uint8_t*)Bs; p.ldb = p.lda; p.b_group = N * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(N) * p.lbs;
+  p.out[0] = C; p.ldc = N;
+  launch_quant<1, EPI_STORE>("quant_gemm", p, tiles, st);
+  return launch_status("moe_quant_gemm");
+}
+
+// ---------------------------------------------------------------------------------------- experts
+namespace moe {
+
+extern template void expert_dw_impl<PATH_BF16>(const BwdArgs&, hipStream_t);
+extern template void expert_dw_impl<PATH_BF16_TAIL>(const BwdArgs&, hipStream_t);
+extern template void expert_dw_impl<PATH_BF16_SMALL>(const BwdArgs&, hipStream_t);
+
+// Workspace, forward: plan, codes and exponents of H, H itself where the caller does not keep it.
+// Backward: plan, dG, dU, codes and exponents of [dG | dU].
+struct QuantSpace {
+  size_t plan, act, codes, scales;  // act: a bf16 matrix [n_rows, d_ff]; codes, scales: of one or (backward) two such matrices
+  QuantSpace(const moe_shape_t* s, int n_groups, int n_rows, int mats)
+      : plan(quant_plan_size(n_groups, n_rows)), act(align_up((size_t)n_rows * s->d_ff * 2, 256)),
+        codes(align_up((size_t)n_rows * mats * quant_row(s->d_ff), 256)), scales(align_up((size_t)n_rows * mats * quant_blocks(s->d_ff), 256)) {}
+  size_t fwd() const { return plan + act + codes + scales; }
+  size_t bwd() const { return plan + 2 * act + codes + scales; }
+};
+
+static int check_quant_expert(const moe_shape_t* s, int n_groups, const int32_t* offsets, int n_rows, const int32_t* src_of,
+                              const moe_quant_weights_t* W, bool bwd, const char* who) {
+  int rc = check_shape(s, who);
+  if (rc) return rc;
+  if (s->dtype != MOE_BF16) {
+    set_error("%s: the experts' saved tensors are bf16", who);
+    return MOE_EDTYPE;
+  }
+  rc = check_groups(n_groups, n_rows, who);
+  if (rc) return rc;
+  rc = check_launch(n_groups, n_rows, std::max(s->d, s->d_ff), who);
+  if (rc) return rc;
+  if (wide_rows(std::max(s->d, s->d_ff), 2)) {
+    set_error("%s: rows of d=%d, d_ff=%d values are too long", who, s->d, s->d_ff);
+    return MOE_EINVAL;
+  }
+  if (!offsets || !W) {
+    set_error("%s: null pointer", who);
+    return MOE_EINVAL;
+  }
+  if (src_of && n_rows != s->T * s->k) {
+    set_error("%s: rows read in place are T*k rows", who);
+    return MOE_EINVAL;
+  }
+  if (src_of && (int64_t)s->T * quant_row(s->d) >= ((int64_t)1 << 32) - 4096) {
+    set_error("%s: rows read in place must take less than 4 GiB (32-bit byte offsets)", who);
+    return MOE_EINVAL;
+  }
+  const void* fwd_ptrs[] = {W->WgT, W->WgT_s, W->WdT, W->WdT_s, W->WuT, W->WuT_s};
+  const void* bwd_ptrs[] = {W->Wgu, W->Wgu_s, W->Wd, W->Wd_s};
+  bool null = false, aligned = true;
+  if (bwd) {
+    for (const void* p : bwd_ptrs) null = null || !p;
+    aligned = aligned16(W->Wgu) && aligned16(W->Wd);
+  } else {
+    for (int i = 0; i < (W->gated ? 6 : 4); i++) null = null || !fwd_ptrs[i];
+    aligned = aligned16(W->WgT) && aligned16(W->WuT) && aligned16(W->WdT);
+  }
+  if (null || !aligned) {
+    set_error(null ? "%s: null pointer among the weights" : "%s: every tensor must be 16-byte aligned", who);
+    return MOE_EINVAL;
+  }
+  return MOE_OK;
+}
+static int fail_null(const char* who) {
+  set_error("%s: null pointer", who);
+  return MOE_EINVAL;
+}
+
+}  // namespace moe
+
+extern "C" size_t moe_quant_expert_fwd_workspace_bytes(const moe_shape_t* shape, int32_t n_groups, int32_t n_rows) {
+  using namespace moe;
+  if (!shape || n_groups < 1 || n_rows < 0 || shape->d_ff < 1) return 0;
+  return QuantSpace(shape, n_groups, n_rows, 1).fwd();
+}
+extern "C" size_t moe_quant_expert_bwd_workspace_bytes(const moe_shape_t* shape, int32_t n_groups, int32_t n_rows) {
+  using namespace moe;
+  if (!shape || n_groups < 1 || n_rows < 0 || shape->d_ff < 1) return 0;
+  return QuantSpace(shape, n_groups, n_rows, 2).bwd();
+}
+
+extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, const int32_t* offsets, int32_t n_rows, const int32_t* src_of,
+                                    const void* XQ, const void* XS, const moe_quant_weights_t* W, void* G, void* U, void* H, void* Yout,
+                                    const void* plan, void* ws, size_t ws_bytes, void* stream) {
+  using namespace moe;
+  static const char* who = "moe_quant_expert_fwd";
+  const int rc = check_quant_expert(shape, n_groups, offsets, n_rows, src_of, W, false, who);
+  if (rc) return rc;
+  const bool gated = W->gated != 0;
+  if (!ws || (n_rows > 0 && (!XQ || !XS || !Yout || (G && (!H || (gated && !U))) || (!G && H)))) return fail_null(who);
+  const void* ptrs[] = {XQ, G, U, H, Yout, plan, ws};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) {
+      set_error("%s: every tensor must be 16-byte aligned", who);
+      return MOE_EINVAL;
+    }
+  if (plan && (n_groups != shape->E || n_rows != shape->T * shape->k)) {
+    set_error("%s: a plan is that of the shape: E groups, T*k rows", who);
+    return MOE_EINVAL;
+  }
+  const QuantSpace sp(shape, n_groups, n_rows, 1);
+  if (ws_bytes < sp.fwd()) {
+    set_error("%s: workspace of %zu bytes, need %zu", who, ws_bytes, sp.fwd());
+    return MOE_EWS;
+  }
+  if (n_rows == 0) return MOE_OK;
+  hipStream_t st = (hipStream_t)stream;
+  const int d = shape->d, F = shape->d_ff, tiles = max_row_tiles(MOE_BF16, n_groups, n_rows, d);
+  const Plan pl = carve_plan(plan ? (void*)plan : ws, n_groups, plan_cap(n_groups, n_rows));
+  if (!plan) launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
+  char* w = (char*)ws + sp.plan;
+  void* act = H ? H : w;
+  uint8_t *HQ = (uint8_t*)w + sp.act, *HS = HQ + sp.codes;
+  QuantGemm p = {};
+  p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
+  p.N = F; p.nk = (int)quant_blocks(d);
+  p.A = (const uint8_t*)XQ; p.As = (const uint8_t*)XS; p.lda = quant_row(d); p.las = p.nk;
+  p.a_index = src_of; p.a_index_div = shape->k;
+  p.B[0] = (const uint8_t*)W->WgT; p.Bs[0] = (const uint8_t*)W->WgT_s; p.B[1] = (const uint8_t*)W->WuT; p.Bs[1] = (const uint8_t*)W->WuT_s;
+  p.ldb = p.lda; p.b_group = F * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(F) * p.lbs;
+  p.out[0] = G; p.out[1] = gated ? U : act; p.out[2] = act; p.ldc = F;
+  if (!G) p.out[0] = nullptr;
+  if (gated && !G) p.out[1] = nullptr;
+  if (gated) launch_quant<2, EPI_SWIGLU_FWD>("quant_fwd_gate_up", p, tiles, st);
+  else launch_quant<1, EPI_GELU_FWD>("quant_fwd_gate_up", p, tiles, st);
+  launch_quant_rows_bf16(act, n_rows, F, HQ, HS, quant_row(F), quant_blocks(F), st);
+  QuantGemm q = {};
+  q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.n_rows = n_rows;
+  q.N = d; q.nk = (int)quant_blocks(F);
+  q.A = HQ; q.As = HS; q.lda = quant_row(F); q.las = q.nk;
+  q.B[0] = (const uint8_t*)W->WdT; q.Bs[0] = (const uint8_t*)W->WdT_s;
+  q.ldb = q.lda; q.b_group = d * q.ldb; q.lbs = q.nk; q.bs_group = quant_blocks(d) * q.lbs;
+  q.out[0] = Yout; q.ldc = d;
+  launch_quant<1, EPI_STORE>("quant_fwd_down", q, tiles, st);
+  return launch_status(who);
+}
+
+extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, const int32_t* offsets, int32_t n_rows, const int32_t* src_of,
+                                    const float* row_w, const void* dYQ, const void* dYS, const void* Xin, const moe_quant_weights_t* W,
+                                    const void* G, const void* U, const void* H, const void* dYin, void* dXin, int32_t* active_ids,
+                                    int32_t* n_active, void* dWg_c, void* dWu_c, void* dWd_c, void* ws, size_t ws_bytes, void* stream) {
+  using namespace moe;
+  static const char* who = "moe_quant_expert_bwd";
+  const int rc = check_quant_expert(shape, n_groups, offsets, n_rows, src_of, W, true, who);
+  if (rc) return rc;
+  const bool gated = W->gated != 0;
+  if (!ws || !active_ids || !n_active || !dWg_c || (gated && !dWu_c) || !dWd_c || (!src_of != !row_w) ||
+      (n_rows > 0 && (!dYQ || !dYS || !Xin || !G || (gated && !U) || !H || !dYin || !dXin)))
+    return fail_null(who);
+  const void* ptrs[] = {dYQ, Xin, G, U, H, dYin, dXin, dWg_c, dWu_c, dWd_c, ws};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) {
+      set_error("%s: every tensor must be 16-byte aligned", who);
+      return MOE_EINVAL;
+    }
+  const QuantSpace sp(shape, n_groups, n_rows, 2);
+  if (ws_bytes < sp.bwd()) {
+    set_error("%s: workspace of %zu bytes, need %zu", who, ws_bytes, sp.bwd());
+    return MOE_EWS;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  const int d = shape->d, F = shape->d_ff, tiles = max_row_tiles(MOE_BF16, n_groups, n_rows, d);
+  const Plan pl = carve_plan(ws, n_groups, plan_cap(n_groups, n_rows));
+  launch_plan(offsets, n_groups, 256, pl, active_ids, n_active, st);
+  if (n_rows == 0) return launch_status(who);
+  char* dG = (char*)ws + sp.plan;
+  char* dU = dG + sp.act;
+  uint8_t *Q = (uint8_t*)dU + sp.act, *S = Q + sp.codes;
+  const int mats = gated ? 2 : 1;
+  QuantGemm p = {};
+  p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
+  p.N = F; p.nk = (int)quant_blocks(d);
+  p.A = (const uint8_t*)dYQ; p.As = (const uint8_t*)dYS; p.lda = quant_row(d); p.las = p.nk;
+  p.a_index = src_of; p.a_index_div = shape->k; p.c_scale = row_w;
+  p.B[0] = (const uint8_t*)W->Wd; p.Bs[0] = (const uint8_t*)W->Wd_s;
+  p.ldb = p.lda; p.b_group = F * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(F) * p.lbs;
+  p.in[0] = G; p.in[1] = U; p.out[0] = dG; p.out[1] = dU; p.ldc = F;
+  if (gated) launch_quant<1, EPI_SWIGLU_BWD>("quant_bwd_dh", p, tiles, st);
+  else launch_quant<1, EPI_GELU_BWD>("quant_bwd_dh", p, tiles, st);
+  launch_quant_rows_bf16(dG, n_rows, F, Q, S, mats * quant_row(F), mats * quant_blocks(F), st);
+  if (gated) launch_quant_rows_bf16(dU, n_rows, F, Q + quant_row(F), S + quant_blocks(F), mats * quant_row(F), mats * quant_blocks(F), st);
+  QuantGemm q = {};
+  q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.n_rows = n_rows;
+  q.N = d; q.nk = mats * (int)quant_blocks(F);
+  q.A = Q; q.As = S; q.lda = mats * quant_row(F); q.las = q.nk;
+  q.B[0] = (const uint8_t*)W->Wgu; q.Bs[0] = (const uint8_t*)W->Wgu_s;
+  q.ldb = q.lda; q.b_group = d * q.ldb; q.lbs = q.nk; q.bs_group = quant_blocks(d) * q.lbs;
+  q.out[0] = dXin; q.ldc = d;
+  launch_quant<1, EPI_STORE>("quant_bwd_dx", q, tiles, st);
+  BwdArgs a = {};
+  a.d = d; a.F = F; a.n_groups = n_groups; a.n_rows = n_rows; a.offsets = offsets;
+  a.Xin = Xin; a.Wu = gated ? W->Wgu : nullptr; a.G = G; a.U = U; a.H = H; a.dYin = dYin;
+  a.dWg = dWg_c; a.dWu = dWu_c; a.dWd = dWd_c; a.ws = (char*)ws; a.dG = dG; a.dU = dU;
+  if (small_tiles(MOE_BF16, n_groups, n_rows, d, F)) expert_dw_impl<PATH_BF16_SMALL>(a, st);
+  else if (d % 64 == 0 && F % 64 == 0) expert_dw_impl<PATH_BF16>(a, st);
+  else expert_dw_impl<PATH_BF16_TAIL>(a, st);
+  return launch_status(who);
+}

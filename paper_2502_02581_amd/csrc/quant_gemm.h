@@ -1,0 +1,29 @@
+// Argument blocks of the products of block-scaled tensors (see quant_format.h).
+#pragma once
+
+#include "gemm_plan.h"
+#include "quant_format.h"
+
+namespace moe {
+
+// C[rows, N] = A[rows, K] B_g[N, K]^T over the row tiles of a plan, or over n_rows rows of one group.  K is whole blocks: rows of codes
+// are padded with zeros.
+struct QuantGemm {
+  const RowTile* tiles;    // NULL: one group of n_rows rows
+  const int32_t* n_tiles;
+  int32_t n_rows;
+  int32_t N, nk;           // columns, blocks of K
+  const uint8_t *A, *As;   // rows of lda codes and las exponents
+  int64_t lda, las;
+  const int32_t* a_index;  // row r reads row a_index[r] / a_index_div (NULL: row r)
+  int32_t a_index_div;
+  const uint8_t *B[2], *Bs[2];  // [1]: second matrix of a dual product
+  int64_t ldb, b_group;         // bytes of a row, of a group
+  int64_t lbs, bs_group;        // the same of the exponents
+  void* out[3];
+  const void* in[2];
+  int64_t ldc;
+  const float* c_scale;    // activation-backward epilogues: row r is scaled by c_scale[a_index[r]]
+};
+
+}  // namespace moe
