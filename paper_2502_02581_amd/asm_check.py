@@ -145,6 +145,8 @@ def check_mfma_sources(lines: List[str], wait_states: int = 2) -> List[str]:
             continue
         ops = t.split(None, 1)[1].split(",")
         read = _vregs(ops[1]) | _vregs(ops[2])
+        if t.startswith("v_mfma_scale"):   # the exponents of both operands
+            read |= _vregs(ops[4]) | _vregs(ops[5])
         stack = [(j, 0) for j in preds[k]]
         while stack:
             j, ws = stack.pop()

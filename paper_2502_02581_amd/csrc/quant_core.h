@@ -1,0 +1,286 @@
+// Tile core of the products of block-scaled 8-bit tensors (quant_format.h): v_mfma_scale_f32_16x16x128_f8f6f4 with operands staged
+// through LDS.  Both operands are rows of K codes; a K step is one block of 128, so one exponent an operand row, which the instruction
+// applies.  C[m][n] = sum_k A[m][k] B[n][k], BM x 256 outputs of one product or BM x 128 of each of two that share A, four wavefronts.
+#pragma once
+
+#include "gemm_cores.h"
+#include "quant_gemm.h"
+
+namespace moe {
+
+// The rows of a tile: its valid ones, and where they are.
+struct QuantTile {
+  const uint8_t *a, *as;           // gathered rows: of the whole operand, else of the tile
+  uint32_t a_bytes, as_bytes;      // from there to the end of the valid data
+  RowMap map;
+  const uint8_t *b[2], *bs[2];     // first row of the tile; exponents of the tile's first 128 columns
+  int n_valid;                     // columns of the tile that there are
+};
+
+// An iteration t multiplies the tiles of block t of K.  A wave's share is TM x 8 accumulator tiles: its fragments of A (8 registers each: 32 codes a
+// lane) are all in registers, those of B in two halves, `lo` (the first product of a dual one) and `hi`.
+//   phase 1: A x lo, meanwhile hi(t) is read;
+//   barrier: every wave has read all it needs of t, and the tiles of t + 1 have landed;
+//   phase 2: A x hi, meanwhile lo(t + 1) is read, A(t + 1) fragment by fragment behind the last use of A(t)'s, and the loads of
+//            t + SLOTS are issued into the slot of t.
+// Every fragment is read from LDS once, and no register holds two blocks' values of the same fragment.  MFMAs are inline assembly with a memory
+// clobber, so that the order is the one written here (see MfmaDmaCore, whose loads, LDS layout and epilogue these are).
+template <int BM_, int NB, int SLOTS>
+struct QuantCore {
+  static constexpr int BM = BM_, BN = 256 / NB, BK = kQuantBlock;
+  static constexpr int WM = 2, WN = 2, NW = 4, NT = 256;
+  static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, HB = 4;  // HB: B tiles of a half
+  static constexpr int A_NI = BM / 32, B_NI = BN / 32;                // wave-wide 16-byte loads a wave and tile
+  static constexpr int A_BYTES = BM * BK, B_BYTES = BN * BK;
+  // a slot: A, B (both products), then a word per row of A with its exponent, and 64 words per wave and product with that of its columns
+  static constexpr int SA_AT = A_BYTES + NB * B_BYTES, SB_AT = SA_AT + BM * 4, SLOT_BYTES = SB_AT + NW * NB * 256;
+  static constexpr int LDS_BYTES = SLOTS * SLOT_BYTES;
+  static constexpr int L = A_NI + NB * B_NI + 1 + NB;  // loads a wave and iteration
+  static constexpr int H = TM * HB;                    // MFMAs of a phase
+  static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
+  static_assert((SLOTS - 1) * L <= 63, "the wait count must be encodable");
+  static_assert(TM >= 2 && NB * TN == 2 * HB, "shares of a wave");
+  typedef __attribute__((ext_vector_type(8))) int32_t frag_t;
+  typedef __attribute__((ext_vector_type(4))) int rsrc_t;
+  static constexpr uint32_t kNowhere = 0xffffff00u;
+
+  __device__ static __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
+
+  // (the words go through v_readfirstlane: see MfmaDmaCore::seek for the wait behind them)
+  __device__ static __forceinline__ rsrc_t desc(const uint8_t* base, uint32_t bytes) {
+    const uint64_t p = (uint64_t)base;
+    rsrc_t r;
+    r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)p);
+    r[1] = __builtin_amdgcn_readfirstlane((int)((uint32_t)(p >> 32) & 0xffffu));
+    r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+    r[3] = 0x00020000;
+    return r;
+  }
+  __device__ static __forceinline__ void move(rsrc_t& r, uint32_t step) {
+    const uint64_t p = (((uint64_t)(uint32_t)r[1] << 32) | (uint32_t)r[0]) + step;
+    r[0] = (int)(uint32_t)p;
+    r[1] = (int)(uint32_t)(p >> 32);
+  }
+  // Descriptors of the loads of one iteration.  Their bases step along K; what lies beyond the valid rows stays out of their range, because a row's
+  // stride is at least the bytes of K.  Once K is exhausted they are empty: loads deliver zeros.
+  struct Cursor {
+    rsrc_t a, as, b[NB], bs[NB];
+    int left;
+  };
+  __device__ static __forceinline__ void next(Cursor& c) {
+    move(c.a, BK);
+    move(c.as, 1);
+#pragma unroll
+    for (int x = 0; x < NB; x++) {
+      move(c.b[x], BK);
+      move(c.bs[x], 1);
+    }
+    if (--c.left == 0) {
+      c.a[2] = c.as[2] = 0;
+#pragma unroll
+      for (int x = 0; x < NB; x++) c.b[x][2] = c.bs[x][2] = 0;
+    }
+  }
+
+  // C += B A with operands exchanged, as in MfmaDmaCore: register r of lane l is C[m = l % 16][n = 4 * (l / 16) + r].
+  __device__ static __forceinline__ void mfma(f32x4_t& acc, const frag_t& b, const frag_t& a, int sb, int sa) {
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+                 : "+a"(acc)
+                 : "v"(b), "v"(a), "v"(sb), "v"(sa)
+                 : "memory");
+  }
+  // with a tile load in its shadow: the MFMA is the wait state between the write of M0 and the load
+  template <int plus, bool WORD>
+  __device__ static __forceinline__ void mfma_load(f32x4_t& acc, const frag_t& b, const frag_t& a, int sb, int sa, const rsrc_t& rsrc, uint32_t base,
+                                                   uint32_t voff) {
+    if constexpr (WORD)
+      asm volatile("s_add_u32 m0, %5, %6\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]\n\t"
+                   "buffer_load_ubyte %7, %8, 0 offen lds"
+                   : "+a"(acc)
+                   : "v"(b), "v"(a), "v"(sb), "v"(sa), "s"(base), "n"(plus), "v"(voff), "s"(rsrc)
+                   : "memory", "scc");
+    else
+      asm volatile("s_add_u32 m0, %5, %6\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]\n\t"
+                   "buffer_load_dwordx4 %7, %8, 0 offen lds"
+                   : "+a"(acc)
+                   : "v"(b), "v"(a), "v"(sb), "v"(sa), "s"(base), "n"(plus), "v"(voff), "s"(rsrc)
+                   : "memory", "scc");
+  }
+  template <int plus, bool WORD>
+  __device__ static __forceinline__ void load(const rsrc_t& rsrc, uint32_t base, uint32_t voff) {
+    if constexpr (WORD)
+      asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_ubyte %2, %3, 0 offen lds" : : "s"(base), "n"(plus), "v"(voff), "s"(rsrc) : "memory", "scc");
+    else
+      asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds" : : "s"(base), "n"(plus), "v"(voff), "s"(rsrc) : "memory", "scc");
+  }
+
+  template <typename P> __device__ static __forceinline__ P lds(uint32_t at) {
+    return *(const __attribute__((address_space(3))) P*)(uintptr_t)at;
+  }
+
+  template <class Epi>
+  __device__ static __forceinline__ void run(char* smem, int nk, const QuantTile& t, int64_t lda, int64_t las, int64_t ldb, const Epi& epi) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm0 = (wave / WN) * (BM / WM), wn0 = (wave % WN) * (BN / WN);
+    f32x4_t acc[NB][TM][TN];
+
+    // ---- loads: the j-th of a wave fills the 1 KB piece wave + 4 j of a tile, eight rows, lane by lane; pieces swizzled as in MfmaDmaCore
+    const int row = wave * 8 + (lane >> 3);
+    const uint32_t col = (uint32_t)(((lane & 7) ^ swizzle(row)) << 4);
+    uint32_t voa[A_NI], vob[B_NI];
+    const int srow = (wave * 64 + lane) & (BM - 1);  // waves beyond the rows load them again
+    uint32_t vos;
+    if (t.map.gathered()) {
+#pragma unroll
+      for (int j = 0; j < A_NI; j++) {
+        const int r = row + 32 * j;
+        voa[j] = r < t.map.rows ? (uint32_t)t.map(r) * (uint32_t)lda + col : kNowhere;
+      }
+      vos = srow < t.map.rows ? (uint32_t)t.map(srow) * (uint32_t)las : kNowhere;
+    } else {
+#pragma unroll
+      for (int j = 0; j < A_NI; j++) voa[j] = (uint32_t)(row + 32 * j) * (uint32_t)lda + col;
+      vos = srow < t.map.rows ? (uint32_t)srow * (uint32_t)las : kNowhere;
+    }
+#pragma unroll
+    for (int j = 0; j < B_NI; j++) vob[j] = (uint32_t)(row + 32 * j) * (uint32_t)ldb + col;
+    const uint32_t zero = 0;
+    Cursor c;
+    const uint32_t k_bytes = (uint32_t)nk * BK;
+    c.a = desc(t.a, t.a_bytes);
+    c.as = desc(t.as, t.as_bytes);
+#pragma unroll
+    for (int x = 0; x < NB; x++) {
+      c.b[x] = desc(t.b[x], (uint32_t)(t.n_valid - 1) * (uint32_t)ldb + k_bytes);
+      // columns of this wave that do not exist have no exponents either
+      c.bs[x] = desc(t.bs[x] + (NB == 1 ? (int64_t)(wn0 / kQuantBlock) * nk : 0), wn0 < t.n_valid ? (uint32_t)nk : 0u);
+    }
+    c.left = nk;
+#pragma unroll
+    for (int x = 0; x < NB; x++) asm volatile("" : "+s"(c.b[x]), "+s"(c.bs[x]) : : "memory");
+    asm volatile("s_nop 4" : "+s"(c.a), "+s"(c.as) : : "memory");
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    // LDS addresses of a slot's pieces of this wave (16-byte loads, words of A's exponents, of B's)
+    const uint32_t p16 = lds0 + (uint32_t)wave * 1024u, pa = lds0 + SA_AT + (uint32_t)((wave * 64) & (BM - 1)) * 4u, pb = lds0 + SB_AT + (uint32_t)wave * (NB * 256u);
+    // load number n of an iteration: A, then B, then the exponents; `at`: the slot's offset
+    auto each_load = [&](auto n_c, uint32_t at, auto&& f) __attribute__((always_inline)) {
+      constexpr int n = decltype(n_c)::value;
+      if constexpr (n < A_NI) f(std::integral_constant<int, n * 4096>(), std::false_type(), c.a, p16 + at, voa[n]);
+      else if constexpr (n < A_NI + NB * B_NI) {
+        constexpr int x = (n - A_NI) / B_NI, j = (n - A_NI) % B_NI;
+        f(std::integral_constant<int, A_BYTES + x * B_BYTES + j * 4096>(), std::false_type(), c.b[x], p16 + at, vob[j]);
+      } else if constexpr (n == A_NI + NB * B_NI) f(std::integral_constant<int, 0>(), std::true_type(), c.as, pa + at, vos);
+      else {
+        constexpr int x = n - (A_NI + NB * B_NI + 1);
+        f(std::integral_constant<int, x * 256>(), std::true_type(), c.bs[x], pb + at, zero);
+      }
+    };
+    auto issue = [&](auto n_c, uint32_t at) __attribute__((always_inline)) {
+      each_load(n_c, at, [&](auto plus, auto word, const rsrc_t& r, uint32_t base, uint32_t vo) __attribute__((always_inline)) {
+        load<decltype(plus)::value, decltype(word)::value>(r, base, vo);
+      });
+    };
+    for (int s = 0; s < SLOTS; s++) {
+      static_for<L>([&](auto n) __attribute__((always_inline)) { issue(n, (uint32_t)(s * SLOT_BYTES)); });
+      next(c);
+    }
+#pragma unroll
+    for (int x = 0; x < NB; x++)
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) acc[x][i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // (pinned: see MfmaDmaCore)
+#pragma unroll
+    for (int x = 0; x < NB; x++)
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) asm volatile("" : "+a"(acc[x][i][j])::"memory");
+    asm volatile("s_nop 7" ::: "memory");
+
+    // ---- fragments: lane l holds 32 codes of row l % 16: the 16-byte pieces l / 16 and 4 + l / 16 (any order of K that both operands share will do)
+    const int fr = lane & 15, h = lane >> 4;
+    uint32_t ao[2], bo[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+      ao[q] = lds0 + (uint32_t)((wm0 + fr) * BK + (((4 * q + h) ^ swizzle(wm0 + fr)) << 4));
+      bo[q] = lds0 + A_BYTES + (uint32_t)((wn0 + fr) * BK + (((4 * q + h) ^ swizzle(wn0 + fr)) << 4));
+    }
+    const uint32_t sao = lds0 + SA_AT + (uint32_t)(wm0 + fr) * 4u, sbo = pb + (uint32_t)lane * 4u;
+    frag_t fa[TM], fl[HB], fh[HB];
+    int sa[TM], sl, sh;
+    auto frag = [&](const uint32_t (&o)[2], uint32_t at, uint32_t plus) __attribute__((always_inline)) {
+      const u32x4_t p = lds<u32x4_t>(o[0] + at + plus), q = lds<u32x4_t>(o[1] + at + plus);
+      return __builtin_bit_cast(frag_t, __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto read_a = [&](auto i_c, uint32_t at) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_c)::value;
+      sa[i] = lds<int32_t>(sao + at + i * 64);
+      fa[i] = frag(ao, at, i * 16 * BK);
+    };
+    auto read_lo = [&](auto j_c, uint32_t at) __attribute__((always_inline)) {
+      constexpr int j = decltype(j_c)::value;
+      if constexpr (j == 0) sl = lds<int32_t>(sbo + at);
+      fl[j] = frag(bo, at, j * 16 * BK);
+    };
+    auto read_hi = [&](auto j_c, uint32_t at) __attribute__((always_inline)) {
+      constexpr int j = decltype(j_c)::value;
+      if constexpr (j == 0) sh = lds<int32_t>(sbo + at + (NB - 1) * 256);
+      fh[j] = frag(bo, at, NB == 2 ? B_BYTES + j * 16 * BK : (HB + j) * 16 * BK);
+    };
+    auto landed = [&](auto n) __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(n)::value) : "memory");
+      __syncthreads();
+    };
+    landed(std::integral_constant<int, (SLOTS - 1) * L>());
+    static_for<HB>([&](auto j) __attribute__((always_inline)) { read_lo(j, 0); });
+    static_for<TM - 1>([&](auto i) __attribute__((always_inline)) { read_a(i, 0); });
+
+    uint32_t cur = 0;
+    for (int it = 0; it < nk; it++) {
+      const uint32_t nxt = cur == (SLOTS - 1) * SLOT_BYTES ? 0u : cur + SLOT_BYTES;
+      static_for<2 * H>([&](auto slot_c) __attribute__((always_inline)) {
+        constexpr int s = decltype(slot_c)::value, m = s % H, i = m / HB, j = m % HB, step = H / 8 > 0 ? H / 8 : 1;
+        if constexpr (s < H) {
+          if constexpr (s == 0) read_a(std::integral_constant<int, TM - 1>(), cur);
+          if constexpr (m % step == 0 && m / step < HB) read_hi(std::integral_constant<int, m / step>(), cur);
+          mfma(acc[0][i][j], fl[j], fa[i], sl, sa[i]);
+        } else {
+          if constexpr (m == 0) landed(std::integral_constant<int, (SLOTS - 2) * L>());
+          if constexpr (m % step == 0 && m / step < HB) read_lo(std::integral_constant<int, m / step>(), nxt);
+          if constexpr (m > 0 && j == 0) read_a(std::integral_constant<int, i - 1>(), nxt);
+          constexpr int n0 = m * L / H, n1 = (m + 1) * L / H;
+          f32x4_t& x = NB == 2 ? acc[NB - 1][i][j] : acc[0][i][TN - HB + j];
+          if constexpr (n1 > n0) {
+            each_load(std::integral_constant<int, n0>(), cur, [&](auto plus, auto word, const rsrc_t& r, uint32_t base, uint32_t vo) __attribute__((always_inline)) {
+              mfma_load<decltype(plus)::value, decltype(word)::value>(x, fh[j], fa[i], sh, sa[i], r, base, vo);
+            });
+            static_for<n1 - n0 - 1>([&](auto y) __attribute__((always_inline)) { issue(std::integral_constant<int, n0 + 1 + decltype(y)::value>(), cur); });
+          } else {
+            mfma(x, fh[j], fa[i], sh, sa[i]);
+          }
+        }
+      });
+      next(c);
+      cur = nxt;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // (the wait behind the last MFMA, and the order of accumulator copies behind it: see MfmaDmaCore; these MFMAs take twice as long)
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15"
+                 : "+a"(acc[NB - 1][TM - 1][TN - 1])
+                 :
+                 : "memory");
+#pragma unroll
+    for (int x = 0; x < NB; x++)
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) asm volatile("" : "+a"(acc[x][i][j])::"memory");
+    __syncthreads();
+    TileEpilogue<NB, TM, TN, NW, LDS_BYTES, true>::run(smem, acc, epi, wave, lane, wm0, wn0);
+  }
+};
+
+}  // namespace moe

@@ -1,83 +1,97 @@
 // moe_quant_gemm, moe_quant_expert_fwd / _bwd: grouped products of block-scaled 8-bit tensors.
 #include "expert_impl.h"
-#include "quant_gemm.h"
+#include "quant_core.h"
 
 namespace moe {
 
-typedef __attribute__((ext_vector_type(8))) int32_t code_frag_t;  // 32 codes of a lane
+// ------------------------------------------------------------------------------------------ kernel
+// Of an epilogue's outputs the last one alone: H of a forward pass that keeps nothing for a backward pass.
+template <class E>
+struct LastOutput : E {
+  static constexpr int NOUT = 1;
+  template <int NB, int NA>
+  __device__ __forceinline__ void apply(const float (&v)[NB][4], const float (&a)[NA][4], float sc, float (&o)[1][4]) const {
+    float all[E::NOUT][4];
+    E::apply(v, a, sc, all);
+#pragma unroll
+    for (int q = 0; q < 4; q++) o[0][q] = all[E::NOUT - 1][q];
+  }
+};
 
-template <int NB, int EPI>
-__global__ __launch_bounds__(256) void quant_gemm_kernel(QuantGemm p) {
-  typedef Epilogue<bf16_t, NB, EPI> Epi;
-  constexpr int BN = 256 / NB, TN = 4 / NB;
+template <class Core, class Epi, int NB>
+__device__ __forceinline__ void quant_tile(const QuantGemm& p, const RowTile& t, int nt, char* smem) {
+  const int rows = tile_rows(t), n0 = nt * Core::BN;
+  QuantTile q;
+  q.map = {p.a_index, p.a_index ? p.a_index_div : 1, t.row0_in, rows};
+  const int64_t row0 = p.a_index ? 0 : t.row0_in;
+  const uint32_t last = (uint32_t)((p.a_index ? p.a_src_rows : rows) - 1);
+  q.a = p.A + row0 * p.lda;
+  q.as = p.As + row0 * p.las;
+  q.a_bytes = last * (uint32_t)p.lda + (uint32_t)p.nk * kQuantBlock;
+  q.as_bytes = last * (uint32_t)p.las + (uint32_t)p.nk;
+#pragma unroll
+  for (int x = 0; x < NB; x++) {
+    q.b[x] = p.B[x] + t.group * p.b_group + n0 * p.ldb;
+    q.bs[x] = p.Bs[x] + t.group * p.bs_group + n0 / kQuantBlock * p.lbs;
+  }
+  q.n_valid = min(Core::BN, p.N - n0);
+  Epi epi;
+  const int64_t c_off = ((int64_t)t.row0_out * p.ldc + n0) * Epi::OES;
+#pragma unroll
+  for (int x = 0; x < Epi::NOUT; x++) epi.out[x] = (char*)p.out[x] + c_off;
+#pragma unroll
+  for (int x = 0; x < Epi::NAUX; x++) epi.in[x] = (const char*)p.in[x] + c_off;
+  epi.ldc = p.ldc;
+  epi.rows = rows;
+  epi.n_valid = q.n_valid;
+  epi.scale = p.c_scale;
+  epi.index = p.a_index + t.row0_in;
+  Core::run(smem, p.nk, q, p.lda, p.las, p.ldb, epi);
+}
+
+// Heights of the tiles: 256, and for what is left of a group 128 and 64 (tiles of up to 64 rows are bound by streaming the matrix, whatever
+// their height).
+template <int NB> using QuantTall = QuantCore<256, NB, 2>;
+template <int NB> using QuantMid = QuantCore<128, NB, 3>;
+template <int NB> using QuantShort = QuantCore<64, NB, 3>;
+
+// Tiles are dealt to the XCDs as in row_gemm_block: band by band of kBandRows row tiles, column by column within a band, runs of 32 (launches of
+// few rounds: of 8) consecutive tiles to an XCD.
+template <int NB, class Epi>
+__global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
+  extern __shared__ __align__(16) char smem[];
+  constexpr int BN = 256 / NB;
   const int ntn = (p.N + BN - 1) / BN;
   const int n_mt = p.tiles ? *p.n_tiles : (p.n_rows + 255) / 256;
-  const int mt = blockIdx.x / ntn, nt = blockIdx.x - mt * ntn;
-  if (mt >= n_mt) return;
+  const int total = n_mt * ntn, rounds = total >> 8, per_band = kBandRows * ntn;
+  const int xcd = blockIdx.x & 7, round = blockIdx.x >> 8, b = (blockIdx.x >> 3) & 31;
+  int q = round << 8;
+  if (round < rounds) q += rounds > kFineRounds && round < rounds - 1 ? (xcd << 5) + b : ((b >> 3) << 6) + (xcd << 3) + (b & 7);
+  else q += (b << 3) + xcd;
+  if (q >= total) return;
+  const int band = q / per_band, r = q - band * per_band, high = min(kBandRows, n_mt - band * kBandRows);
+  const int mt = band * kBandRows + r % high, nt = r / high;
   RowTile t;
   if (p.tiles) t = p.tiles[mt];
-  else { t.group = 0; t.row0_in = mt * 256; t.rows = min(256, p.n_rows - t.row0_in); t.row0_out = t.row0_in; }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, h = lane >> 4;
-  const int rows = tile_rows(t), n0 = nt * BN + wave * TN * 16;
-  Epi epi;
-  for (int m0 = 0; m0 < rows; m0 += 16) {
-    const int r = t.row0_in + m0 + l;
-    const bool ok = m0 + l < rows;
-    const int64_t ar = ok ? (p.a_index ? p.a_index[r] / p.a_index_div : r) : 0;
-    f32x4_t acc[NB][TN];
-#pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-      for (int j = 0; j < TN; j++) acc[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int kb = 0; kb < p.nk; kb++) {
-      code_frag_t a = {};
-      if (ok) a = *reinterpret_cast<const code_frag_t*>(p.A + ar * p.lda + kb * kQuantBlock + h * 32);
-      const int sa = ok ? p.As[ar * p.las + kb] : 127;
-#pragma unroll
-      for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int j = 0; j < TN; j++) {
-          const int n = n0 + j * 16 + l;
-          code_frag_t w = {};
-          int sb = 127;
-          if (n < p.N) {
-            w = *reinterpret_cast<const code_frag_t*>(p.B[b] + t.group * p.b_group + (int64_t)n * p.ldb + kb * kQuantBlock + h * 32);
-            sb = p.Bs[b][t.group * p.bs_group + n / kQuantBlock * p.lbs + kb];
-          }
-          acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, acc[b][j], 0, 0, 0, sb, 0, sa);
-        }
-    }
-    if (!ok) continue;
-    const float scale = (EPI == EPI_SWIGLU_BWD || EPI == EPI_GELU_BWD) && p.c_scale ? p.c_scale[p.a_index[r]] : 1.f;
-#pragma unroll
-    for (int j = 0; j < TN; j++) {
-      const int n = n0 + j * 16 + h * 4;
-      if (n >= p.N) continue;
-      constexpr int NA = Epi::NAUX > 0 ? Epi::NAUX : 1;
-      const int64_t at = (int64_t)(t.row0_out + m0 + l) * p.ldc + n;
-      float v[NB][4], a[NA][4], o[Epi::NOUT][4];
-#pragma unroll
-      for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int q = 0; q < 4; q++) v[b][q] = acc[b][j][q];
-#pragma unroll
-      for (int x = 0; x < Epi::NAUX; x++) Epi::unpack(*reinterpret_cast<const typename Epi::packed_t*>((const bf16_t*)p.in[x] + at), a[x]);
-      epi.apply(v, a, scale, o);
-#pragma unroll
-      for (int x = 0; x < Epi::NOUT; x++)
-        if (p.out[x]) Epi::pack((bf16_t*)p.out[x] + at, o[x]);
-    }
-  }
+  else { t.group = 0; t.row0_in = t.row0_out = mt * 256; t.rows = min(256, p.n_rows - t.row0_in); }
+  t.group = __builtin_amdgcn_readfirstlane(t.group);
+  t.row0_in = __builtin_amdgcn_readfirstlane(t.row0_in);
+  t.rows = __builtin_amdgcn_readfirstlane(t.rows);
+  t.row0_out = __builtin_amdgcn_readfirstlane(t.row0_out);
+  if (tile_rows(t) > 128) quant_tile<QuantTall<NB>, Epi, NB>(p, t, nt, smem);
+  else if (tile_rows(t) > 64) quant_tile<QuantMid<NB>, Epi, NB>(p, t, nt, smem);
+  else quant_tile<QuantShort<NB>, Epi, NB>(p, t, nt, smem);
 }
 
 // At most max_tiles row tiles (the device knows how many there are).
-template <int NB, int EPI>
+template <int NB, class Epi>
 static void launch_quant(const char* label, const QuantGemm& p, int max_tiles, hipStream_t st) {
-  const unsigned blocks = (unsigned)max_tiles * (unsigned)ceil_div(p.N, 256 / NB);
+  const unsigned blocks = row_block_count(max_tiles, p.N, 256 / NB);
   if (blocks == 0) return;
-  ProfScope prof(label, st);
-  hipLaunchKernelGGL((quant_gemm_kernel<NB, EPI>), dim3(blocks), dim3(256), 0, st, p);
+  constexpr int kLds = std::max({QuantTall<NB>::LDS_BYTES, QuantMid<NB>::LDS_BYTES, QuantShort<NB>::LDS_BYTES});
+  launch_gemm<quant_gemm_kernel<NB, Epi>>(label, blocks, 256, kLds, st, p);
 }
+template <int NB, int EPI> using Epi8 = Epilogue<bf16_t, NB, EPI>;
 
 // ------------------------------------------------------------------------------------ one product
 static int quant_tiles(int n_groups, int n_rows) { return max_row_tiles(MOE_BF16, n_groups, n_rows, INT32_MAX); }
@@ -108,7 +122,7 @@ extern "C" int moe_quant_gemm(int32_t n_groups, const int32_t* offsets, int32_t 
   using namespace moe;
   const int rc = check_groups(n_groups, n_rows, "moe_quant_gemm");
   if (rc) return rc;
-  if (K < 1 || N < 1 || N % 8 || K > 1 << 24 || N > 1 << 24 || (!offsets && n_groups != 1)) {
+  if (K < 1 || N < 1 || N % 8 || K > 1 << 22 || N > 1 << 22 || (!offsets && n_groups != 1)) {
     set_error("moe_quant_gemm: bad K=%d N=%d n_groups=%d (N a multiple of 8; one group where there are no offsets)", K, N, n_groups);
     return MOE_EINVAL;
   }
@@ -141,7 +155,7 @@ extern "C" int moe_quant_gemm(int32_t n_groups, const int32_t* offsets, int32_t 
   p.A = (const uint8_t*)A; p.As = (const uint8_t*)As; p.lda = quant_row(K); p.las = p.nk;
   p.B[0] = (const uint8_t*)B; p.Bs[0] = (const uint8_t*)Bs; p.ldb = p.lda; p.b_group = N * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(N) * p.lbs;
   p.out[0] = C; p.ldc = N;
-  launch_quant<1, EPI_STORE>("quant_gemm", p, tiles, st);
+  launch_quant<1, Epi8<1, EPI_STORE>>("quant_gemm", p, tiles, st);
   return launch_status("moe_quant_gemm");
 }
 
@@ -175,7 +189,8 @@ static int check_quant_expert(const moe_shape_t* s, int n_groups, const int32_t*
   if (rc) return rc;
   rc = check_launch(n_groups, n_rows, std::max(s->d, s->d_ff), who);
   if (rc) return rc;
-  if (wide_rows(std::max(s->d, s->d_ff), 2)) {
+  // (256 rows of [dG | dU] codes, and of bf16 outputs, within 32-bit byte offsets)
+  if (512 * quant_row(std::max(s->d, s->d_ff)) >= ((int64_t)1 << 32) - 4096) {
     set_error("%s: rows of d=%d, d_ff=%d values are too long", who, s->d, s->d_ff);
     return MOE_EINVAL;
   }
@@ -261,14 +276,21 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
   p.N = F; p.nk = (int)quant_blocks(d);
   p.A = (const uint8_t*)XQ; p.As = (const uint8_t*)XS; p.lda = quant_row(d); p.las = p.nk;
-  p.a_index = src_of; p.a_index_div = shape->k;
+  p.a_index = src_of; p.a_index_div = shape->k; p.a_src_rows = shape->T;
   p.B[0] = (const uint8_t*)W->WgT; p.Bs[0] = (const uint8_t*)W->WgT_s; p.B[1] = (const uint8_t*)W->WuT; p.Bs[1] = (const uint8_t*)W->WuT_s;
   p.ldb = p.lda; p.b_group = F * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(F) * p.lbs;
-  p.out[0] = G; p.out[1] = gated ? U : act; p.out[2] = act; p.ldc = F;
-  if (!G) p.out[0] = nullptr;
-  if (gated && !G) p.out[1] = nullptr;
-  if (gated) launch_quant<2, EPI_SWIGLU_FWD>("quant_fwd_gate_up", p, tiles, st);
-  else launch_quant<1, EPI_GELU_FWD>("quant_fwd_gate_up", p, tiles, st);
+  p.ldc = F;
+  typedef Epi8<2, EPI_SWIGLU_FWD> Gated;
+  typedef Epi8<1, EPI_GELU_FWD> Plain;
+  if (G) {
+    p.out[0] = G; p.out[1] = gated ? U : act; p.out[2] = act;
+    if (gated) launch_quant<2, Gated>("quant_fwd_gate_up", p, tiles, st);
+    else launch_quant<1, Plain>("quant_fwd_gate_up", p, tiles, st);
+  } else {
+    p.out[0] = act;
+    if (gated) launch_quant<2, LastOutput<Gated>>("quant_fwd_gate_up", p, tiles, st);
+    else launch_quant<1, LastOutput<Plain>>("quant_fwd_gate_up", p, tiles, st);
+  }
   launch_quant_rows_bf16(act, n_rows, F, HQ, HS, quant_row(F), quant_blocks(F), st);
   QuantGemm q = {};
   q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.n_rows = n_rows;
@@ -277,7 +299,7 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   q.B[0] = (const uint8_t*)W->WdT; q.Bs[0] = (const uint8_t*)W->WdT_s;
   q.ldb = q.lda; q.b_group = d * q.ldb; q.lbs = q.nk; q.bs_group = quant_blocks(d) * q.lbs;
   q.out[0] = Yout; q.ldc = d;
-  launch_quant<1, EPI_STORE>("quant_fwd_down", q, tiles, st);
+  launch_quant<1, Epi8<1, EPI_STORE>>("quant_fwd_down", q, tiles, st);
   return launch_status(who);
 }
 
@@ -317,12 +339,12 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
   p.N = F; p.nk = (int)quant_blocks(d);
   p.A = (const uint8_t*)dYQ; p.As = (const uint8_t*)dYS; p.lda = quant_row(d); p.las = p.nk;
-  p.a_index = src_of; p.a_index_div = shape->k; p.c_scale = row_w;
+  p.a_index = src_of; p.a_index_div = shape->k; p.a_src_rows = shape->T; p.c_scale = row_w;
   p.B[0] = (const uint8_t*)W->Wd; p.Bs[0] = (const uint8_t*)W->Wd_s;
   p.ldb = p.lda; p.b_group = F * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(F) * p.lbs;
   p.in[0] = G; p.in[1] = U; p.out[0] = dG; p.out[1] = dU; p.ldc = F;
-  if (gated) launch_quant<1, EPI_SWIGLU_BWD>("quant_bwd_dh", p, tiles, st);
-  else launch_quant<1, EPI_GELU_BWD>("quant_bwd_dh", p, tiles, st);
+  if (gated) launch_quant<1, Epi8<1, EPI_SWIGLU_BWD>>("quant_bwd_dh", p, tiles, st);
+  else launch_quant<1, Epi8<1, EPI_GELU_BWD>>("quant_bwd_dh", p, tiles, st);
   launch_quant_rows_bf16(dG, n_rows, F, Q, S, mats * quant_row(F), mats * quant_blocks(F), st);
   if (gated) launch_quant_rows_bf16(dU, n_rows, F, Q + quant_row(F), S + quant_blocks(F), mats * quant_row(F), mats * quant_blocks(F), st);
   QuantGemm q = {};
@@ -332,7 +354,7 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   q.B[0] = (const uint8_t*)W->Wgu; q.Bs[0] = (const uint8_t*)W->Wgu_s;
   q.ldb = q.lda; q.b_group = d * q.ldb; q.lbs = q.nk; q.bs_group = quant_blocks(d) * q.lbs;
   q.out[0] = dXin; q.ldc = d;
-  launch_quant<1, EPI_STORE>("quant_bwd_dx", q, tiles, st);
+  launch_quant<1, Epi8<1, EPI_STORE>>("quant_bwd_dx", q, tiles, st);
   BwdArgs a = {};
   a.d = d; a.F = F; a.n_groups = n_groups; a.n_rows = n_rows; a.offsets = offsets;
   a.Xin = Xin; a.Wu = gated ? W->Wgu : nullptr; a.G = G; a.U = U; a.H = H; a.dYin = dYin;

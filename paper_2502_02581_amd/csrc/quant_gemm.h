@@ -16,7 +16,7 @@ struct QuantGemm {
   const uint8_t *A, *As;   // rows of lda codes and las exponents
   int64_t lda, las;
   const int32_t* a_index;  // row r reads row a_index[r] / a_index_div (NULL: row r)
-  int32_t a_index_div;
+  int32_t a_index_div, a_src_rows;  // of so many rows
   const uint8_t *B[2], *Bs[2];  // [1]: second matrix of a dual product
   int64_t ldb, b_group;         // bytes of a row, of a group
   int64_t lbs, bs_group;        // the same of the exponents
