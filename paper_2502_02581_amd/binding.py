@@ -777,16 +777,23 @@ class MoEHotPath:
     d = 2048, 60 experts, 4 shared: 2.16 ms against 2.19).  Where common launches are not possible (one set gated, the
     other not; rows too long for the tile cores) the shared experts' calls follow the routed ones', or, with
     overlap_shared, go to a second stream of the same (default) priority beside them and join before the combine.
+
+    With quant (bf16 layers) the routed experts run on block-scaled operands: forward() and backward() take a MoEQuantWeights in the place of
+    Wg, and None for Wu and Wd.  Tokens and their gradients are quantised once, in their own order, and read in place.  Shared experts stay in
+    bf16; their calls go beside the routed ones as above.
     """
 
     def __init__(self, shape: MoEShape, n_shared: int = 0, d_ff_shared: int = 0, device="cuda:0",
-                 overlap_shared: bool = False, aux_alpha: float = 0.0, gather: bool = False, fused: bool = True):
+                 overlap_shared: bool = False, aux_alpha: float = 0.0, gather: bool = False, fused: bool = True, quant: bool = False):
         self.shape, self.S, self.Fs, self.device = shape, n_shared, d_ff_shared, torch.device(device)
         self.gather = bool(gather)  # routed experts read X and dY through src_of (moe_expert_*_gather)
         # gate, dispatch and auxiliary loss through moe_route_dispatch / moe_route_aux_bwd (fewer launches)
         self.fused = bool(fused)
         self.aux_alpha = float(aux_alpha)
         self.overlap = bool(overlap_shared and n_shared)
+        self.quant = bool(quant)
+        if self.quant and shape.dtype != "bf16":
+            raise MoEError("quant goes with bf16 layers")
         s, dt, dev = shape, shape.torch_dtype, self.device
         A = s.T * s.k
         i32 = dict(dtype=torch.int32, device=dev)
@@ -805,6 +812,11 @@ class MoEHotPath:
             "dWd_c": torch.empty(s.E, s.d_ff, s.d, **f),
         }
         self.ws_routed = max(moe_expert_fwd_workspace_bytes(s, s.E, A, False), moe_expert_bwd_workspace_bytes(s, s.E, A, False))
+        if self.quant:
+            rows = lambda: (torch.empty(s.T, moe_quant_row_bytes(s.d), dtype=torch.uint8, device=dev),
+                            torch.empty(s.T, moe_quant_scale_bytes(s.d), dtype=torch.uint8, device=dev))
+            (self.b["XQ"], self.b["XS"]), (self.b["dYQ"], self.b["dYS"]) = rows(), rows()
+            self.ws_routed = max(self.ws_routed, moe_quant_expert_fwd_workspace_bytes(s, s.E, A), moe_quant_expert_bwd_workspace_bytes(s, s.E, A))
         ws = max(moe_dispatch_workspace_bytes(s), moe_route_dispatch_workspace_bytes(s), self.ws_routed)
         if self.aux_alpha > 0:
             self.b.update({"aux_P": torch.empty(s.E, dtype=torch.float32, device=dev),
@@ -843,7 +855,7 @@ class MoEHotPath:
     def _fork(self, Wu, Wsu, stream):
         """With overlap_shared, where the two sets cannot run in common launches: the main stream, once the side stream waits
         for everything already queued on it.  None otherwise."""
-        if not self.overlap or ((Wu is None) == (Wsu is None) and not self.long_rows):
+        if not self.overlap or (not self.quant and (Wu is None) == (Wsu is None) and not self.long_rows):
             return None
         main = torch.cuda.current_stream(self.device) if stream is None else \
             stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=self.device)
@@ -855,9 +867,14 @@ class MoEHotPath:
         self.ev_join.record(self.side)
         main.wait_event(self.ev_join)
 
-    def forward(self, logits, X, Wg, Wu, Wd, Wsg=None, Wsu=None, Wsd=None, stream=None):
+    def _check_weights(self, Wg, Wu, Wd):
+        if self.quant != isinstance(Wg, MoEQuantWeights) or (self.quant and (Wu is not None or Wd is not None)):
+            raise MoEError("a layer with quant takes a MoEQuantWeights in the place of Wg, None for Wu and Wd; any other layer the matrices")
+
+    def forward(self, logits, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None):
         s, b = self.shape, self.b
         A = s.T * s.k
+        self._check_weights(Wg, Wu, Wd)
         main = self._fork(Wu, Wsu, stream)
         stream = _stream(stream)
         self._logits = logits  # the gate's backward reads them again
@@ -878,19 +895,27 @@ class MoEHotPath:
             if main:
                 moe_expert_fwd(self.sshape, self.S, None, s.T, X, Wsg, Wsu, Wsd, b["Gs"], b["Us"], b["Hs"], b["Ysh"],
                                ws_shared["ws"], self.side)
-            moe_experts_fwd(s, dict(d_ff=s.d_ff, n_groups=s.E, n_rows=A, offsets=b["offsets"],
-                                    src_of=b["src_of"] if self.gather else None, Xin=X if self.gather else b["Xp"], Wg=Wg,
-                                    Wu=Wu, Wd=Wd, G=b["G"], U=b["U"], H=b["H"], Yout=b["Yp"],
-                                    plan=self.plan if self.fused else None, **ws), shared, stream)
+            if self.quant:
+                moe_quant_rows(X, b["XQ"], b["XS"], stream)
+                moe_quant_expert_fwd(s, s.E, b["offsets"], A, b["src_of"], b["XQ"], b["XS"], Wg, b["G"], b["U"] if Wg.gated else None, b["H"],
+                                     b["Yp"], ws["ws"], self.plan if self.fused else None, stream)
+                if shared:
+                    moe_expert_fwd(self.sshape, self.S, None, s.T, X, Wsg, Wsu, Wsd, b["Gs"], b["Us"], b["Hs"], b["Ysh"], ws_shared["ws"], stream)
+            else:
+                moe_experts_fwd(s, dict(d_ff=s.d_ff, n_groups=s.E, n_rows=A, offsets=b["offsets"],
+                                        src_of=b["src_of"] if self.gather else None, Xin=X if self.gather else b["Xp"], Wg=Wg,
+                                        Wu=Wu, Wd=Wd, G=b["G"], U=b["U"], H=b["H"], Yout=b["Yp"],
+                                        plan=self.plan if self.fused else None, **ws), shared, stream)
         finally:   # a refused call must not leave the caller's tensors in use on a stream that nothing waits for
             if main:
                 self._join(main)
         moe_combine(s, b["Yp"], b["row_of"], b["topk_w"], b["Ysh"] if self.S else None, b["Y"], stream)
         return b["Y"]
 
-    def backward(self, dY, X, Wg, Wu, Wd, Wsg=None, Wsu=None, Wsd=None, stream=None):
+    def backward(self, dY, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None):
         s, b = self.shape, self.b
         A = s.T * s.k
+        self._check_weights(Wg, Wu, Wd)
         main = self._fork(Wu, Wsu, stream)
         stream = _stream(stream)
         ws, ws_shared = self._ws_pieces()
@@ -903,10 +928,20 @@ class MoEHotPath:
             if main:
                 moe_expert_bwd(self.sshape, self.S, None, s.T, X, Wsg, Wsu, Wsd, b["Gs"], b["Us"], b["Hs"], dY, b["dXsh"],
                                b["s_active_ids"], b["s_n_active"], b["dWsg"], b["dWsu"], b["dWsd"], ws_shared["ws"], self.side)
-            moe_experts_bwd(s, dict(d_ff=s.d_ff, n_groups=s.E, n_rows=A, offsets=b["offsets"], Xin=b["Xp"], Wg=Wg, Wu=Wu, Wd=Wd,
-                                    G=b["G"], U=b["U"], H=b["H"], dYin=b["dYp"], dXin=b["dXp"], active_ids=b["active_ids"],
-                                    n_active=b["n_active"], dWg_c=b["dWg_c"], dWu_c=b["dWu_c"], dWd_c=b["dWd_c"], **in_place,
-                                    **ws), shared, stream)
+            if self.quant:
+                moe_quant_rows(dY, b["dYQ"], b["dYS"], stream)
+                gated = Wg.gated
+                moe_quant_expert_bwd(s, s.E, b["offsets"], A, b["src_of"], b["topk_w"], b["dYQ"], b["dYS"], b["Xp"], Wg, b["G"],
+                                     b["U"] if gated else None, b["H"], b["dYp"], b["dXp"], b["active_ids"], b["n_active"], b["dWg_c"],
+                                     b["dWu_c"] if gated else None, b["dWd_c"], ws["ws"], stream)
+                if shared:
+                    moe_expert_bwd(self.sshape, self.S, None, s.T, X, Wsg, Wsu, Wsd, b["Gs"], b["Us"], b["Hs"], dY, b["dXsh"], b["s_active_ids"],
+                                   b["s_n_active"], b["dWsg"], b["dWsu"], b["dWsd"], ws_shared["ws"], stream)
+            else:
+                moe_experts_bwd(s, dict(d_ff=s.d_ff, n_groups=s.E, n_rows=A, offsets=b["offsets"], Xin=b["Xp"], Wg=Wg, Wu=Wu, Wd=Wd,
+                                        G=b["G"], U=b["U"], H=b["H"], dYin=b["dYp"], dXin=b["dXp"], active_ids=b["active_ids"],
+                                        n_active=b["n_active"], dWg_c=b["dWg_c"], dWu_c=b["dWu_c"], dWd_c=b["dWd_c"], **in_place,
+                                        **ws), shared, stream)
         finally:
             if main:
                 self._join(main)
@@ -919,3 +954,10 @@ class MoEHotPath:
             if self.aux_alpha > 0:
                 moe_aux_loss_bwd(s, self._logits, b["counts"], self.aux_alpha, 1.0, True, b["dlogits"], stream)
         return b["dX"]
+
+    def gradients(self, gated: bool = True, gated_shared: bool = True):
+        """The weight gradients of the last backward pass, as moe_grad_norm and moe_grad_clip take them."""
+        b = self.b
+        names = ["dWg_c"] + (["dWu_c"] if gated else []) + ["dWd_c"]
+        shared = (["dWsg"] + (["dWsu"] if gated_shared else []) + ["dWsd"]) if self.S else []
+        return [(b[n], b["n_active"]) for n in names] + [b[n] for n in shared]

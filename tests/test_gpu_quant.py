@@ -146,11 +146,8 @@ GEMM_CASES = [
 ]
 
 
-@pytest.mark.parametrize("counts,K,N", GEMM_CASES)
-@pytest.mark.parametrize("dense", [False, True])
-def test_gemm(counts, K, N, dense):
-    if dense and len(counts) > 1:
-        pytest.skip("without offsets there is one group")
+@pytest.mark.parametrize("counts,K,N,dense", [(*c, False) for c in GEMM_CASES] + [(*c, True) for c in GEMM_CASES if len(c[0]) == 1])
+def test_gemm(counts, K, N, dense):   # dense: without offsets, one group
     m = moe()
     g = torch.Generator().manual_seed(sum(counts) * 7 + K + N)
     E, before, behind = len(counts), (0 if dense else 2), (0 if dense else 5)   # rows of no group on both sides
@@ -418,3 +415,108 @@ def test_refusals_of_the_binding():
         L.weights.update(L.W[0], None, L.W[2])
     with pytest.raises(m.MoEError, match="workspace"):
         m.moe_quant_expert_fwd(L.shape, 4, L.off, L.n, L.src, *L.xq, L.weights, L.G, L.U, L.H, L.Y, L.ws[:16])
+
+
+# --------------------------------------------------------------------------------------------- layer
+@pytest.mark.parametrize("T,E,k,d,F,S,Fs,overlap,fused,gated,gated_s", [
+    (1, 8, 2, 128, 64, 0, 0, False, True, True, True), (130, 6, 2, 256, 200, 0, 0, False, True, True, True),
+    (300, 5, 3, 136, 264, 2, 72, False, True, True, True), (257, 4, 2, 128, 128, 1, 64, True, True, True, False),
+    (200, 6, 2, 200, 136, 1, 128, True, False, False, True), (0, 4, 2, 64, 64, 1, 64, False, True, True, True)])
+def test_layer(T, E, k, d, F, S, Fs, overlap, fused, gated, gated_s):
+    """MoEHotPath with quant: the routed experts are the separate calls bit for bit, the shared ones those of the layer without; then the clipping
+    of its gradients against their 64-bit norm."""
+    m = moe()
+    shape = m.MoEShape(T, d, E, k, F, "bf16", "softmax", True)
+    g = torch.Generator().manual_seed(T + d)
+    bf = lambda *s, std=1.0: (torch.randn(*s, generator=g) * std).to(torch.bfloat16).to(DEV)
+    X, dY, logits = bf(T, d), bf(T, d), torch.randn(T, E, generator=g).to(DEV)
+    W = [bf(E, d, F, std=d ** -0.5), bf(E, d, F, std=d ** -0.5) if gated else None, bf(E, F, d, std=F ** -0.5)]
+    Ws = [bf(S, d, Fs, std=d ** -0.5), bf(S, d, Fs, std=d ** -0.5) if gated_s else None, bf(S, Fs, d, std=Fs ** -0.5)] if S else [None] * 3
+    weights = m.MoEQuantWeights(shape, E, gated=gated)
+    weights.update(*W)
+    hp = m.MoEHotPath(shape, S, Fs, DEV, overlap_shared=overlap, aux_alpha=0.001, fused=fused, quant=True)
+    for t in hp.b.values():
+        if t.dtype == torch.bfloat16:
+            t.zero_()
+    hp.forward(logits, X, weights, None, None, *Ws)
+    hp.backward(dY, X, weights, None, None, *Ws)
+    torch.cuda.synchronize()
+    b, A = hp.b, T * k
+    ref = m.MoEHotPath(shape, S, Fs, DEV, aux_alpha=0.001, fused=fused)
+    ref.forward(logits, X, *W, *Ws)
+    ref.backward(dY, X, *W, *Ws)
+    same = lambda x, y: torch.equal(x.view(torch.int16) if x.dtype == torch.bfloat16 else x, y.view(torch.int16) if y.dtype == torch.bfloat16 else y)
+    for n in ("topk_idx", "topk_w", "counts", "offsets", "src_of", "Xp", "active_ids", "n_active"):
+        assert same(b[n], ref.b[n]), n
+    if S:   # (common launches of bf16 sets may sum in other parts)
+        for n in ("Ysh", "dXsh", "dWsg", "dWsd"):
+            assert T == 0 or rel(np_of(b[n]), np_of(ref.b[n])) <= 2.0 ** -7, n
+    if T:
+        new = {n: torch.zeros_like(b[n]) for n in ("G", "U", "H", "Yp", "dXp", "dWg_c", "dWu_c", "dWd_c", "active_ids", "n_active")}
+        xq, dq = ((u8(T, m.moe_quant_row_bytes(d)), u8(T, m.moe_quant_scale_bytes(d))) for _ in range(2))
+        ws = u8(max(m.moe_quant_expert_fwd_workspace_bytes(shape, E, A), m.moe_quant_expert_bwd_workspace_bytes(shape, E, A)))
+        m.moe_quant_rows(X, *xq)
+        m.moe_quant_rows(dY, *dq)
+        U = new["U"] if gated else None
+        m.moe_quant_expert_fwd(shape, E, b["offsets"], A, b["src_of"], *xq, weights, new["G"], U, new["H"], new["Yp"], ws)
+        m.moe_quant_expert_bwd(shape, E, b["offsets"], A, b["src_of"], b["topk_w"], *dq, b["Xp"], weights, b["G"], b["U"] if gated else None, b["H"],
+                               b["dYp"], new["dXp"], new["active_ids"], new["n_active"], new["dWg_c"], new["dWu_c"] if gated else None, new["dWd_c"], ws)
+        for n in new:
+            assert same(new[n], b[n]), n
+        # and near the layer in bf16: an operand of e4m3 is off by at most 2^-4 of itself, three lie one behind the other on the longest way
+        for n in ("Y", "dX"):
+            assert rel(np_of(b[n]), np_of(ref.b[n])) <= 3 * 2.0 ** -4, n
+    grads = hp.gradients(gated, gated_s)
+    n = int(b["n_active"].item())
+    flat = [np_of(t[0][:n]) if isinstance(t, tuple) else np_of(t) for t in grads]
+    total = float(np.sqrt(sum((x ** 2).sum() for x in flat)))
+    norm, nws = torch.zeros(1, device=DEV), u8(m.moe_grad_norm_workspace_bytes())
+    m.moe_grad_norm(grads, norm, nws)
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total
+    m.moe_grad_clip(grads, norm, 0.5 * total)
+    m.moe_grad_norm(grads, norm, nws)
+    assert abs(float(norm) - 0.5 * total) <= 2.0 ** -8 * total + 1e-6   # every value rounded to bf16 again
+    with pytest.raises(m.MoEError, match="MoEQuantWeights"):
+        hp.forward(logits, X, *W, *Ws)
+    with pytest.raises(m.MoEError, match="MoEQuantWeights"):
+        ref.backward(dY, X, weights, None, None, *Ws)
+
+
+def test_layer_in_a_graph():
+    """A captured forward and backward pass of the layer between eager ones, the weights quantised anew in between."""
+    m = moe()
+    T, E, k, d, F = 150, 6, 2, 256, 136
+    shape = m.MoEShape(T, d, E, k, F, "bf16", "softmax", True)
+    g = torch.Generator().manual_seed(9)
+    bf = lambda *s, std=1.0: (torch.randn(*s, generator=g) * std).to(torch.bfloat16).to(DEV)
+    X, dY, logits = bf(T, d), bf(T, d), torch.randn(T, E, generator=g).to(DEV)
+    W = [bf(E, d, F, std=d ** -0.5), bf(E, d, F, std=d ** -0.5), bf(E, F, d, std=F ** -0.5)]
+    weights = m.MoEQuantWeights(shape, E)
+    hp = m.MoEHotPath(shape, 0, 0, DEV, quant=True)
+    step = lambda: (weights.update(*W), hp.forward(logits, X, weights), hp.backward(dY, X, weights))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    names = ("Y", "dX", "dlogits", "dWg_c", "dWu_c", "dWd_c")
+    n = int(hp.b["n_active"].item())
+    pick = lambda: [hp.b[x][:n].clone() if x.endswith("_c") else hp.b[x].clone() for x in names]
+    for i in range(3):
+        W[0].mul_(0.9)
+        X.mul_(1.1)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = pick()
+        for x in names:
+            hp.b[x].zero_()
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(got, pick())), i
+
+
+def test_layer_refuses_fp32():
+    m = moe()
+    with pytest.raises(m.MoEError, match="bf16"):
+        m.MoEHotPath(m.MoEShape(8, 64, 4, 2, 64, "f32"), quant=True)
