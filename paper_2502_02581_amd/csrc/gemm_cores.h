@@ -12,6 +12,7 @@
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "moe_common.h"
@@ -83,6 +84,14 @@ __device__ __forceinline__ void static_for(F f) {
 // copied out one by one.
 // ROWS: rows of a block.  MT: rows of a tile, one per lane % MT; its columns are four for every lane of a row, lane / MT by lane / MT.
 // AHEAD: the next block's inputs are loaded under a block's arithmetic (two blocks per CU have no registers for them).
+// Epilogues with a member `quantises` (see quant_core.h) also get every finished piece of a row, by quantise<output>(piece, row, first column); where
+// their STORES is false the pieces are not written themselves.
+template <class Epi, class = void> struct Quantises : std::false_type {
+  static constexpr bool stores = true;
+};
+template <class Epi> struct Quantises<Epi, std::void_t<typename Epi::quantises>> : std::true_type {
+  static constexpr bool stores = Epi::STORES;
+};
 template <int NB, int TM, int TN, int NW, int LDS, bool AGPR, int ROWS = 32, int MT = 16, bool AHEAD = true>
 struct TileEpilogue {
   static constexpr int HP = 64 / MT, CT = 4 * HP;  // lanes of a row, columns of a tile
@@ -143,9 +152,18 @@ struct TileEpilogue {
             __builtin_amdgcn_raw_buffer_store_b128(r[x][p], make_rsrc(epi.out[x], extent), g0 + (i * ROWS + p * RPP) * ldb, 0,
                                                    decltype(hint)::value);
       };
-      if (!col_ok) return;
-      if (RB >= 128 && epi.stream()) put(std::integral_constant<int, 2>());
-      else put(std::integral_constant<int, 0>());
+      if constexpr (Quantises<Epi>::stores) {
+        if (col_ok) {
+          if (RB >= 128 && epi.stream()) put(std::integral_constant<int, 2>());
+          else put(std::integral_constant<int, 0>());
+        }
+      }
+      if constexpr (Quantises<Epi>::value) {
+        static_for<NOUT>([&](auto x) __attribute__((always_inline)) {
+#pragma unroll
+          for (int p = 0; p < NPASS; p++) epi.template quantise<decltype(x)::value>(r[decltype(x)::value][p], wm0 + i * ROWS + p * RPP + rrow, c0);
+        });
+      }
     };
     if (NAUX > 0 && AHEAD) load_aux(0);
     float scale[TM];

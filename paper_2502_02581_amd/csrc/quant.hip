@@ -32,17 +32,30 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ X
   const int lane = threadIdx.x & 15;
   for (uint32_t b = blockIdx.x * 16 + (threadIdx.x >> 4); b < n_blocks; b += gridDim.x * 16) {
     const uint32_t row = b / per_row, kb = b - row * per_row, c0 = kb * kQuantBlock + lane * 8;
-    float v[8];
-    load8<T, VEC>(X + (int64_t)row * ldx + c0, cols - (int)c0, v);
-    uint32_t m = 0;
+    const T* x = X + (int64_t)row * ldx + c0;
+    uint2 codes;
+    int e;
+    if constexpr (VEC && sizeof(T) == 2) {
+      uint32_t v[4] = {0, 0, 0, 0};
+      if (c0 + 8 <= (uint32_t)cols) {
+        const uint4 t = *reinterpret_cast<const uint4*>(x);
+        v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+      } else {
+        for (int i = 0; i < cols - (int)c0; i++) v[i / 2] |= (uint32_t)x[i] << (16 * (i % 2));
+      }
+      e = quant_block_bf16(v, codes);
+    } else {
+      float v[8];
+      load8<T, VEC>(x, cols - (int)c0, v);
+      uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) m = max(m, finite_bits(v[i]));
-#pragma unroll
-    for (int x = 8; x >= 1; x >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, x, 16));
-    const int e = quant_exponent(m);
-    const float f = quant_factor(e);
-    const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-    *reinterpret_cast<uint2*>(Q + (int64_t)row * ldq + c0) = make_uint2(quant_codes(lo, f), quant_codes(hi, f));
+      for (int i = 0; i < 8; i++) m = max(m, finite_bits(v[i]));
+      e = quant_exponent((uint32_t)row_max16((int)m));
+      const float f = quant_factor(e);
+      const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+      codes = make_uint2(quant_codes(lo, f), quant_codes(hi, f));
+    }
+    *reinterpret_cast<uint2*>(Q + (int64_t)row * ldq + c0) = codes;
     if (lane == 0) S[(int64_t)row * lds + kb] = (uint8_t)e;
   }
 }
@@ -151,10 +164,6 @@ static void launch_quant_rows(const void* X, int dtype, int n_rows, int cols, in
   }
 #undef MOE_QUANT_ROWS
 }
-void launch_quant_rows_bf16(const void* X, int n_rows, int cols, uint8_t* Q, uint8_t* S, int64_t ldq, int64_t lds, hipStream_t st) {
-  launch_quant_rows(X, MOE_BF16, n_rows, cols, cols, Q, S, ldq, lds, st);
-}
-
 }  // namespace moe
 
 extern "C" int64_t moe_quant_row_bytes(int64_t cols) { return cols < 1 ? 0 : moe::quant_row(cols); }

@@ -8,6 +8,32 @@
 
 namespace moe {
 
+// An epilogue E whose last NQ outputs are quantised, too (128 columns of a row are the pieces of sixteen lanes), as moe_quant_rows would quantise the
+// bf16 values.  KEEP: the bf16 outputs are written.
+template <class E, int NQ, bool KEEP>
+struct QuantOut : E {
+  typedef void quantises;
+  static constexpr bool STORES = KEEP;
+  uint8_t *q[NQ], *s[NQ];  // codes and exponents, from the tile's first row and column on
+  uint32_t ldq, lds;
+  int q_valid;             // columns from the tile's first one on that rows of codes have (whole blocks)
+  template <int x>
+  __device__ __forceinline__ void quantise(const u32x4_t& piece, int row, int col) const {
+    if constexpr (x >= E::NOUT - NQ) {
+      constexpr int n = x - (E::NOUT - NQ);
+      // (beyond the last column there may be what other rows' NaN left)
+      const bool there = col < E::n_valid;
+      const uint32_t v[4] = {there ? piece[0] : 0u, there ? piece[1] : 0u, there ? piece[2] : 0u, there ? piece[3] : 0u};
+      uint2 c;
+      const int e = quant_block_bf16(v, c);
+      if (row < E::rows && col < q_valid) {
+        *reinterpret_cast<uint2*>(q[n] + ((uint32_t)row * ldq + (uint32_t)col)) = c;
+        if ((col & (kQuantBlock - 1)) == 0) s[n][(uint32_t)row * lds + (uint32_t)col / kQuantBlock] = (uint8_t)e;
+      }
+    }
+  }
+};
+
 // The rows of a tile: its valid ones, and where they are.
 struct QuantTile {
   const uint8_t *a, *as;           // gathered rows: of the whole operand, else of the tile
@@ -17,8 +43,9 @@ struct QuantTile {
   int n_valid;                     // columns of the tile that there are
 };
 
-// An iteration t multiplies the tiles of block t of K.  A wave's share is TM x 8 accumulator tiles: its fragments of A (8 registers each: 32 codes a
-// lane) are all in registers, those of B in two halves, `lo` (the first product of a dual one) and `hi`.
+// An iteration t multiplies the tiles of block t of K.  A wave's fragments of A (8 registers each: 32 codes a lane) are all in registers, those
+// of B in two halves, `lo` (the first product of a dual one) and `hi`.  The waves of a dual product lie one below the other, so that each has whole blocks
+// of 128 columns of what it computes from both, which it may have to quantise.
 //   phase 1: A x lo, meanwhile hi(t) is read;
 //   barrier: every wave has read all it needs of t, and the tiles of t + 1 have landed;
 //   phase 2: A x hi, meanwhile lo(t + 1) is read, A(t + 1) fragment by fragment behind the last use of A(t)'s, and the loads of
@@ -28,8 +55,8 @@ struct QuantTile {
 template <int BM_, int NB, int SLOTS>
 struct QuantCore {
   static constexpr int BM = BM_, BN = 256 / NB, BK = kQuantBlock;
-  static constexpr int WM = 2, WN = 2, NW = 4, NT = 256;
-  static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, HB = 4;  // HB: B tiles of a half
+  static constexpr int WN = NB == 2 ? 1 : 2, WM = 4 / WN, NW = 4, NT = 256;
+  static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, HB = NB * TN / 2;  // HB: B tiles of a half
   static constexpr int A_NI = BM / 32, B_NI = BN / 32;                // wave-wide 16-byte loads a wave and tile
   static constexpr int A_BYTES = BM * BK, B_BYTES = BN * BK;
   // a slot: A, B (both products), then a word per row of A with its exponent, and 64 words per wave and product with that of its columns
@@ -39,7 +66,7 @@ struct QuantCore {
   static constexpr int H = TM * HB;                    // MFMAs of a phase
   static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
   static_assert((SLOTS - 1) * L <= 63, "the wait count must be encodable");
-  static_assert(TM >= 2 && NB * TN == 2 * HB, "shares of a wave");
+  static_assert(BN / WN == kQuantBlock, "the columns of a wave are one block");
   typedef __attribute__((ext_vector_type(8))) int32_t frag_t;
   typedef __attribute__((ext_vector_type(4))) int rsrc_t;
   static constexpr uint32_t kNowhere = 0xffffff00u;
@@ -242,7 +269,7 @@ struct QuantCore {
     for (int it = 0; it < nk; it++) {
       const uint32_t nxt = cur == (SLOTS - 1) * SLOT_BYTES ? 0u : cur + SLOT_BYTES;
       static_for<2 * H>([&](auto slot_c) __attribute__((always_inline)) {
-        constexpr int s = decltype(slot_c)::value, m = s % H, i = m / HB, j = m % HB, step = H / 8 > 0 ? H / 8 : 1;
+        constexpr int s = decltype(slot_c)::value, m = s % H, i = m / HB, j = m % HB, step = std::max(H / (2 * HB), 1);
         if constexpr (s < H) {
           if constexpr (s == 0) read_a(std::integral_constant<int, TM - 1>(), cur);
           if constexpr (m % step == 0 && m / step < HB) read_hi(std::integral_constant<int, m / step>(), cur);
@@ -279,7 +306,7 @@ struct QuantCore {
 #pragma unroll
         for (int j = 0; j < TN; j++) asm volatile("" : "+a"(acc[x][i][j])::"memory");
     __syncthreads();
-    TileEpilogue<NB, TM, TN, NW, LDS_BYTES, true>::run(smem, acc, epi, wave, lane, wm0, wn0);
+    TileEpilogue<NB, TM, TN, NW, LDS_BYTES, true, TM == 1 ? 16 : 32>::run(smem, acc, epi, wave, lane, wm0, wn0);
   }
 };
 

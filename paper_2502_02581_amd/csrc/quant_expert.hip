@@ -18,6 +18,20 @@ struct LastOutput : E {
   }
 };
 
+template <class E, int NQ, bool KEEP>
+__device__ __forceinline__ void set_quantised(QuantOut<E, NQ, KEEP>& epi, const QuantGemm& p, int64_t row0, int n0) {
+#pragma unroll
+  for (int x = 0; x < NQ; x++) {
+    epi.q[x] = p.q[x] + row0 * p.ldq + n0;
+    epi.s[x] = p.qs[x] + row0 * p.lds + n0 / kQuantBlock;
+  }
+  epi.ldq = (uint32_t)p.ldq;
+  epi.lds = (uint32_t)p.lds;
+  epi.q_valid = (p.N + kQuantBlock - 1) / kQuantBlock * kQuantBlock - n0;
+}
+template <class E>
+__device__ __forceinline__ void set_quantised(E&, const QuantGemm&, int64_t, int) {}
+
 template <class Core, class Epi, int NB>
 __device__ __forceinline__ void quant_tile(const QuantGemm& p, const RowTile& t, int nt, char* smem) {
   const int rows = tile_rows(t), n0 = nt * Core::BN;
@@ -46,6 +60,7 @@ __device__ __forceinline__ void quant_tile(const QuantGemm& p, const RowTile& t,
   epi.n_valid = q.n_valid;
   epi.scale = p.c_scale;
   epi.index = p.a_index + t.row0_in;
+  set_quantised(epi, p, t.row0_out, n0);
   Core::run(smem, p.nk, q, p.lda, p.las, p.ldb, epi);
 }
 
@@ -166,14 +181,13 @@ extern template void expert_dw_impl<PATH_BF16>(const BwdArgs&, hipStream_t);
 extern template void expert_dw_impl<PATH_BF16_TAIL>(const BwdArgs&, hipStream_t);
 extern template void expert_dw_impl<PATH_BF16_SMALL>(const BwdArgs&, hipStream_t);
 
-// Workspace, forward: plan, codes and exponents of H, H itself where the caller does not keep it.
-// Backward: plan, dG, dU, codes and exponents of [dG | dU].
+// Workspace: plan; codes and exponents of H (forward) or of [dG | dU]; backward: dG and dU in bf16, for the weight gradients.
 struct QuantSpace {
-  size_t plan, act, codes, scales;  // act: a bf16 matrix [n_rows, d_ff]; codes, scales: of one or (backward) two such matrices
+  size_t plan, act, codes, scales;
   QuantSpace(const moe_shape_t* s, int n_groups, int n_rows, int mats)
       : plan(quant_plan_size(n_groups, n_rows)), act(align_up((size_t)n_rows * s->d_ff * 2, 256)),
         codes(align_up((size_t)n_rows * mats * quant_row(s->d_ff), 256)), scales(align_up((size_t)n_rows * mats * quant_blocks(s->d_ff), 256)) {}
-  size_t fwd() const { return plan + act + codes + scales; }
+  size_t fwd() const { return plan + codes + scales; }
   size_t bwd() const { return plan + 2 * act + codes + scales; }
 };
 
@@ -269,9 +283,7 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   const int d = shape->d, F = shape->d_ff, tiles = max_row_tiles(MOE_BF16, n_groups, n_rows, d);
   const Plan pl = carve_plan(plan ? (void*)plan : ws, n_groups, plan_cap(n_groups, n_rows));
   if (!plan) launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
-  char* w = (char*)ws + sp.plan;
-  void* act = H ? H : w;
-  uint8_t *HQ = (uint8_t*)w + sp.act, *HS = HQ + sp.codes;
+  uint8_t *HQ = (uint8_t*)ws + sp.plan, *HS = HQ + sp.codes;
   QuantGemm p = {};
   p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
   p.N = F; p.nk = (int)quant_blocks(d);
@@ -280,18 +292,18 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   p.B[0] = (const uint8_t*)W->WgT; p.Bs[0] = (const uint8_t*)W->WgT_s; p.B[1] = (const uint8_t*)W->WuT; p.Bs[1] = (const uint8_t*)W->WuT_s;
   p.ldb = p.lda; p.b_group = F * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(F) * p.lbs;
   p.ldc = F;
+  p.q[0] = HQ; p.qs[0] = HS; p.ldq = quant_row(F); p.lds = quant_blocks(F);
   typedef Epi8<2, EPI_SWIGLU_FWD> Gated;
   typedef Epi8<1, EPI_GELU_FWD> Plain;
   if (G) {
-    p.out[0] = G; p.out[1] = gated ? U : act; p.out[2] = act;
-    if (gated) launch_quant<2, Gated>("quant_fwd_gate_up", p, tiles, st);
-    else launch_quant<1, Plain>("quant_fwd_gate_up", p, tiles, st);
+    p.out[0] = G; p.out[1] = gated ? U : H; p.out[2] = H;
+    if (gated) launch_quant<2, QuantOut<Gated, 1, true>>("quant_fwd_gate_up", p, tiles, st);
+    else launch_quant<1, QuantOut<Plain, 1, true>>("quant_fwd_gate_up", p, tiles, st);
+  } else if (gated) {
+    launch_quant<2, QuantOut<LastOutput<Gated>, 1, false>>("quant_fwd_gate_up", p, tiles, st);
   } else {
-    p.out[0] = act;
-    if (gated) launch_quant<2, LastOutput<Gated>>("quant_fwd_gate_up", p, tiles, st);
-    else launch_quant<1, LastOutput<Plain>>("quant_fwd_gate_up", p, tiles, st);
+    launch_quant<1, QuantOut<LastOutput<Plain>, 1, false>>("quant_fwd_gate_up", p, tiles, st);
   }
-  launch_quant_rows_bf16(act, n_rows, F, HQ, HS, quant_row(F), quant_blocks(F), st);
   QuantGemm q = {};
   q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.n_rows = n_rows;
   q.N = d; q.nk = (int)quant_blocks(F);
@@ -333,7 +345,7 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   if (n_rows == 0) return launch_status(who);
   char* dG = (char*)ws + sp.plan;
   char* dU = dG + sp.act;
-  uint8_t *Q = (uint8_t*)dU + sp.act, *S = Q + sp.codes;
+  uint8_t *Q = (uint8_t*)dU + sp.act, *S = Q + sp.codes;  // a row of [dG | dU]
   const int mats = gated ? 2 : 1;
   QuantGemm p = {};
   p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
@@ -343,10 +355,10 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   p.B[0] = (const uint8_t*)W->Wd; p.Bs[0] = (const uint8_t*)W->Wd_s;
   p.ldb = p.lda; p.b_group = F * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(F) * p.lbs;
   p.in[0] = G; p.in[1] = U; p.out[0] = dG; p.out[1] = dU; p.ldc = F;
-  if (gated) launch_quant<1, Epi8<1, EPI_SWIGLU_BWD>>("quant_bwd_dh", p, tiles, st);
-  else launch_quant<1, Epi8<1, EPI_GELU_BWD>>("quant_bwd_dh", p, tiles, st);
-  launch_quant_rows_bf16(dG, n_rows, F, Q, S, mats * quant_row(F), mats * quant_blocks(F), st);
-  if (gated) launch_quant_rows_bf16(dU, n_rows, F, Q + quant_row(F), S + quant_blocks(F), mats * quant_row(F), mats * quant_blocks(F), st);
+  p.q[0] = Q; p.qs[0] = S; p.q[1] = Q + quant_row(F); p.qs[1] = S + quant_blocks(F);
+  p.ldq = mats * quant_row(F); p.lds = mats * quant_blocks(F);
+  if (gated) launch_quant<1, QuantOut<Epi8<1, EPI_SWIGLU_BWD>, 2, true>>("quant_bwd_dh", p, tiles, st);
+  else launch_quant<1, QuantOut<Epi8<1, EPI_GELU_BWD>, 1, true>>("quant_bwd_dh", p, tiles, st);
   QuantGemm q = {};
   q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.n_rows = n_rows;
   q.N = d; q.nk = mats * (int)quant_blocks(F);

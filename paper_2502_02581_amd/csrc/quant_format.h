@@ -27,19 +27,42 @@ __device__ __forceinline__ int quant_exponent(uint32_t maximum) {
   return max((int)(maximum >> 23) - 8 + ((maximum & 0x7fffffu) > 0x600000u), 1);
 }
 __device__ __forceinline__ float quant_factor(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }  // 2^-e
-// Four codes: nearest, ties to even, subnormal codes included; the scaled values are at most 448, so nothing saturates.  Infinities and
-// NaN become the NaN code.
+// Four codes: nearest, ties to even, subnormal codes included; the scaled values are at most 448, so none saturates.  The conversion makes NaN codes of
+// infinities and NaN.
 __device__ __forceinline__ uint32_t quant_codes(const float (&x)[4], float f) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, w, true);
-  uint32_t r = (uint32_t)w;
-#pragma unroll
-  for (int i = 0; i < 4; i++)
-    if ((__float_as_uint(x[i]) & 0x7fffffffu) >= 0x7f800000u) r |= 0x7fu << (8 * i);
-  return r;
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, w, true);
 }
-
-// quantises rows of bf16 values into rows of `ldq` codes and `lds` exponents (see moe_quant_rows)
-void launch_quant_rows_bf16(const void* X, int n_rows, int cols, uint8_t* Q, uint8_t* S, int64_t ldq, int64_t lds, hipStream_t st);
+// maximum over the sixteen lanes of a row, in all of them (in-register rotations: exchanges through LDS cost 46 us of a 124 us launch whose
+// epilogue quantises two outputs)
+__device__ __forceinline__ int row_max16(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, false));
+  return max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false));
+}
+// A block of 128 bf16 values, eight in each of sixteen lanes: the lane's codes and the block's exponent byte.  With 0x80 added to their magnitudes
+// infinities and NaN are negative 16-bit numbers and lose against every finite value.
+__device__ __forceinline__ int quant_block_bf16(const uint32_t (&v)[4], uint2& codes) {
+  typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+  i16x2_t m = {0x80, 0x80};
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const u16x2_t t = __builtin_bit_cast(u16x2_t, v[i] & 0x7fff7fffu) + u16x2_t{0x80, 0x80};
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(i16x2_t, t));
+  }
+  const int e = quant_exponent((uint32_t)(row_max16(max((int)m[0], (int)m[1])) - 0x80) << 16);
+  const float scale = __uint_as_float((uint32_t)e << 23);  // 2^e: the conversion divides by it
+  i16x2_t c[2] = {};
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[2 * i]), scale, false);
+    c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[2 * i + 1]), scale, true);
+  }
+  codes = make_uint2(__builtin_bit_cast(uint32_t, c[0]), __builtin_bit_cast(uint32_t, c[1]));
+  return e;
+}
 
 }  // namespace moe

@@ -23,6 +23,8 @@ struct QuantGemm {
   void* out[3];
   const void* in[2];
   int64_t ldc;
+  uint8_t *q[2], *qs[2];   // where the quantised outputs go (QuantOut): rows of ldq codes and lds exponents, the bytes of whole blocks of N
+  int64_t ldq, lds;
   const float* c_scale;    // activation-backward epilogues: row r is scaled by c_scale[a_index[r]]
 };
 

@@ -210,7 +210,7 @@ def test_gemm_exponents_at_the_ends():
 # T, E, k, d, d_ff, gated, rows read in place
 EXPERTS = [(1, 4, 1, 64, 64, True, True), (1, 8, 4, 128, 136, True, True), (16, 12, 4, 256, 192, True, True), (33, 3, 1, 136, 72, False, False),
            (300, 6, 3, 200, 264, True, True), (150, 2, 1, 1000, 328, False, True), (600, 5, 2, 256, 384, True, False), (1100, 3, 1, 384, 128, True, True),
-           (64, 40, 2, 128, 256, True, True)]
+           (64, 40, 2, 128, 256, True, True), (700, 2, 1, 128, 136, True, True), (520, 2, 1, 264, 648, False, False)]
 
 
 def routed(T, E, k, seed):
@@ -332,6 +332,28 @@ def test_experts_backward(case):
                 assert rel(np_of(t[slot]), a[x:y].T @ b[x:y]) <= 2.0 ** -7
     for t in L.dW:
         assert t is None or bool(torch.isnan(t[n:].float()).all())   # slots of no expert are not written
+
+
+@pytest.mark.parametrize("gated", [True, False])
+def test_infinities_stay_in_their_rows(gated):
+    """A token with an infinity and one with NaN: their own rows come out as NaN, all others with the bits they have without them."""
+    L = Layer(40, 3, 1, 136, 72, gated, False)
+    L.forward()
+    L.backward()
+    torch.cuda.synchronize()
+    outs = (L.G, L.U, L.H, L.Y, L.dX) if gated else (L.G, L.H, L.Y, L.dX)
+    ref = [t.clone() for t in outs]
+    m = moe()
+    L.x[7, 5], L.x[20, 100] = float("inf"), float("nan")
+    L.dy[31, 3] = float("nan")
+    m.moe_quant_rows(L.x, *L.xq)
+    m.moe_quant_rows(L.dy, *L.dyq)
+    L.forward()
+    L.backward()
+    for t, r in zip(outs, ref):
+        bad = [7, 20, 31] if t is L.dX else [7, 20]
+        good = [i for i in range(40) if i not in bad]
+        assert torch.equal(t[good].view(torch.int16), r[good].view(torch.int16)) and bool(torch.isnan(t[bad].float()).all())
 
 
 def test_gradient_against_differences():
