@@ -4,6 +4,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 from typing import Dict, Optional
 
 import torch
@@ -511,7 +512,9 @@ def _value_dtype(t, what):
 
 def _sized(t, shape, what, dtype=torch.uint8):
     """The pointer of a contiguous tensor of exactly this shape."""
-    if tuple(t.shape) != tuple(shape):
+    if t is None:
+        raise MoEError(f"{what} must be a tensor")
+    if t.shape != shape:
         raise MoEError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return _ptr(t, dtype, what)
 
@@ -532,13 +535,13 @@ def _pitched(t, shape, what):
 
 
 def moe_quant_row_bytes(cols: int) -> int:
-    """Bytes of a row of codes: cols rounded up to whole blocks of 128."""
-    return int(load_library().moe_quant_row_bytes(int(cols)))
+    """Bytes of a row of codes: cols rounded up to whole blocks of 128 (the library's answer, without a call)."""
+    return -(-cols // 128) * 128
 
 
 def moe_quant_scale_bytes(cols: int) -> int:
-    """Bytes of a row of exponents: one a block of 128."""
-    return int(load_library().moe_quant_scale_bytes(int(cols)))
+    """Bytes of a row of exponents: one a block of 128 (the library's answer, without a call)."""
+    return -(-cols // 128)
 
 
 def moe_quant_rows(X, Q, S, stream=None):
@@ -606,6 +609,7 @@ class MoEQuantWeights:
 
         self.WgT, self.WuT, self.WdT = pair(F, d), pair(F, d) if gated else None, pair(d, F)
         self.Wgu, self.Wd = (pair(d, *[F] * mats), pair(F, d)) if backward else (None, None)
+        self._seal()
 
     @classmethod
     def of_codes(cls, shape: MoEShape, n_groups: int, WgT, WuT, WdT):
@@ -614,6 +618,7 @@ class MoEQuantWeights:
         self = cls.__new__(cls)
         self.shape, self.n_groups, self.gated, self.backward = shape, n_groups, WuT is not None, False
         self.WgT, self.WuT, self.WdT, self.Wgu, self.Wd = WgT, WuT, WdT, None, None
+        self._seal()
         return self
 
     def update(self, Wg, Wu, Wd, stream=None):
@@ -631,11 +636,10 @@ class MoEQuantWeights:
                 moe_quant_weights(w, q, e, *t, stream)
         moe_quant_weights(Wd, *(self.Wd or (None, None)), *self.WdT, stream)
 
-    def _c(self, who, backward) -> _CQuantWeights:
+    def _seal(self):
+        """Checks the tensors and makes their C form, once: they stay the object's for as long as it lives."""
         s, n = self.shape, self.n_groups
         b, r = moe_quant_scale_bytes, moe_quant_row_bytes
-        if backward and self.Wgu is None:
-            raise MoEError(f"{who}: these weights have no layouts of the backward pass")
 
         def ptrs(pair, rows, cols, mats, what):
             if pair is None:
@@ -644,8 +648,8 @@ class MoEQuantWeights:
 
         d, F = s.d, s.d_ff
         mats = 2 if self.gated else 1
-        return _CQuantWeights(*ptrs(self.WgT, F, d, 1, "WgT"), *ptrs(self.WuT, F, d, 1, "WuT"), *ptrs(self.WdT, d, F, 1, "WdT"),
-                              *ptrs(self.Wgu, d, F, mats, "Wgu"), *ptrs(self.Wd, F, d, 1, "Wd"), int(self.gated))
+        self.c = _CQuantWeights(*ptrs(self.WgT, F, d, 1, "WgT"), *ptrs(self.WuT, F, d, 1, "WuT"), *ptrs(self.WdT, d, F, 1, "WdT"),
+                                *ptrs(self.Wgu, d, F, mats, "Wgu"), *ptrs(self.Wd, F, d, 1, "Wd"), int(self.gated))
 
 
 def moe_quant_expert_fwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int) -> int:
@@ -669,7 +673,7 @@ def moe_quant_expert_fwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, XQ,
     q = _quant_args(shape, n_groups, n_rows, src_of, XQ, XS, W, "moe_quant_expert_fwd")
     rc = load_library().moe_quant_expert_fwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, torch.int32, "offsets"), n_rows, _ptr(src_of, torch.int32, "src_of"), *q,
-        ctypes.byref(W._c("moe_quant_expert_fwd", False)), _ptr(G, bf, "G"), _ptr(U, bf, "U"), _ptr(H, bf, "H"), _ptr(Yout, bf, "Yout"),
+        ctypes.byref(W.c), _ptr(G, bf, "G"), _ptr(U, bf, "U"), _ptr(H, bf, "H"), _ptr(Yout, bf, "Yout"),
         _ptr(plan, torch.uint8, "plan"), _ptr(ws, None, "ws"), ws.numel() * ws.element_size(), _stream(stream))
     _check(rc, "moe_quant_expert_fwd")
 
@@ -678,10 +682,12 @@ def moe_quant_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, row
                          active_ids, n_active, dWg_c, dWu_c, dWd_c, ws, stream=None):
     """Backward pass of moe_quant_expert_fwd: input gradients on block-scaled operands, weight gradients in bf16."""
     bf, i32 = torch.bfloat16, torch.int32
+    if W.Wgu is None:
+        raise MoEError("moe_quant_expert_bwd: these weights have no layouts of the backward pass")
     q = _quant_args(shape, n_groups, n_rows, src_of, dYQ, dYS, W, "moe_quant_expert_bwd")
     rc = load_library().moe_quant_expert_bwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, i32, "offsets"), n_rows, _ptr(src_of, i32, "src_of"),
-        _ptr(row_w, torch.float32, "row_w"), *q, _ptr(Xin, bf, "Xin"), ctypes.byref(W._c("moe_quant_expert_bwd", True)), _ptr(G, bf, "G"),
+        _ptr(row_w, torch.float32, "row_w"), *q, _ptr(Xin, bf, "Xin"), ctypes.byref(W.c), _ptr(G, bf, "G"),
         _ptr(U, bf, "U"), _ptr(H, bf, "H"), _ptr(dYin, bf, "dYin"), _ptr(dXin, bf, "dXin"), _ptr(active_ids, i32, "active_ids"),
         _ptr(n_active, i32, "n_active"), _ptr(dWg_c, bf, "dWg_c"), _ptr(dWu_c, bf, "dWu_c"), _ptr(dWd_c, bf, "dWd_c"), _ptr(ws, None, "ws"),
         ws.numel() * ws.element_size(), _stream(stream))
@@ -690,17 +696,34 @@ def moe_quant_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, row
 
 # ---- gradients: lists of tensors, or of (tensor, n_active) for compacted ones [slots, ...]
 def _grad_list(grads, out=None):
-    c = (_CGrad * max(1, len(grads)))()
+    """The C form of a list of gradients: its members as one buffer of whole numbers, which for many small tensors takes half the time of
+    structures one by one."""
     if out is not None and len(out) != len(grads):
         raise MoEError(f"{len(grads)} gradients, {len(out)} outputs")
+    members = []
     for i, x in enumerate(grads):
-        g, n_active = x if isinstance(x, (tuple, list)) else (x, None)
-        dt, o = _value_dtype(g, f"gradient {i}"), g if out is None else out[i]
-        if tuple(o.shape) != tuple(g.shape):
-            raise MoEError(f"output {i} must have shape {tuple(g.shape)}, got {tuple(o.shape)}")
-        slot = g.numel() // g.shape[0] if n_active is not None and g.dim() and g.shape[0] else 1
-        c[i] = _CGrad(_ptr(g, None, f"gradient {i}"), _ptr(o, g.dtype, f"output {i}"), g.numel(), _ptr(n_active, torch.int32, "n_active"), slot, dt)
-    return c
+        n_active, slot = None, 1
+        if not isinstance(x, torch.Tensor):
+            x, n_active = x
+        dt = x.dtype
+        if not (dt is torch.float32 or dt is torch.bfloat16):
+            raise MoEError(f"gradient {i} must be float32 or bfloat16, got {dt}")
+        if not x.is_cuda or not x.is_contiguous():
+            raise MoEError(f"gradient {i} must live on the GPU and be contiguous")
+        g = o = x.data_ptr()
+        n = x.numel()
+        if out is not None:
+            y = out[i]
+            if y.dtype is not dt or y.shape != x.shape or not y.is_cuda or not y.is_contiguous():
+                raise MoEError(f"output {i} must be a contiguous {dt} tensor on the GPU of shape {tuple(x.shape)}")
+            o = y.data_ptr()
+        if n_active is not None:
+            slot = n // x.shape[0] if n else 1
+            n_active = _ptr(n_active, torch.int32, "n_active")
+        members += (g, o, n, n_active or 0, slot, MOE_F32 if dt is torch.float32 else MOE_BF16)
+    if not members:
+        return (_CGrad * 1)()
+    return (_CGrad * len(grads)).from_buffer(bytearray(struct.pack(f"={len(members)}q", *members)))
 
 
 def moe_grad_norm_workspace_bytes() -> int:

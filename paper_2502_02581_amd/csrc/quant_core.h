@@ -146,7 +146,7 @@ struct QuantCore {
   }
 
   template <class Epi>
-  __device__ static __forceinline__ void run(char* smem, int nk, const QuantTile& t, int64_t lda, int64_t las, int64_t ldb, const Epi& epi) {
+  __device__ static __forceinline__ void run(char* smem, int nk, const QuantTile& t, int64_t lda, int64_t las, int64_t ldb, int64_t lbs, const Epi& epi) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm0 = (wave / WN) * (BM / WM), wn0 = (wave % WN) * (BN / WN);
@@ -181,7 +181,7 @@ struct QuantCore {
     for (int x = 0; x < NB; x++) {
       c.b[x] = desc(t.b[x], (uint32_t)(t.n_valid - 1) * (uint32_t)ldb + k_bytes);
       // columns of this wave that do not exist have no exponents either
-      c.bs[x] = desc(t.bs[x] + (NB == 1 ? (int64_t)(wn0 / kQuantBlock) * nk : 0), wn0 < t.n_valid ? (uint32_t)nk : 0u);
+      c.bs[x] = desc(t.bs[x] + (NB == 1 ? (wn0 / kQuantBlock) * lbs : 0), wn0 < t.n_valid ? (uint32_t)nk : 0u);
     }
     c.left = nk;
 #pragma unroll

@@ -5,6 +5,7 @@
 namespace moe {
 
 // ------------------------------------------------------------------------------------------ kernel
+template <int NB, int EPI> using Epi8 = Epilogue<bf16_t, NB, EPI>;
 // Of an epilogue's outputs the last one alone: H of a forward pass that keeps nothing for a backward pass.
 template <class E>
 struct LastOutput : E {
@@ -32,27 +33,30 @@ __device__ __forceinline__ void set_quantised(QuantOut<E, NQ, KEEP>& epi, const 
 template <class E>
 __device__ __forceinline__ void set_quantised(E&, const QuantGemm&, int64_t, int) {}
 
-template <class Core, class Epi, int NB>
-__device__ __forceinline__ void quant_tile(const QuantGemm& p, const RowTile& t, int nt, char* smem) {
+// Blocks [k0, k0 + nk) of K; a part of a sum: `part`.
+template <class Core, class Epi, int NB, bool PART = false>
+__device__ __forceinline__ void quant_tile(const QuantGemm& p, const RowTile& t, int nt, char* smem, int part = 0) {
   const int rows = tile_rows(t), n0 = nt * Core::BN;
+  const int k0 = PART ? part * p.k_part : 0, nk = PART ? min(p.k_part, p.nk - k0) : p.nk;
   QuantTile q;
   q.map = {p.a_index, p.a_index ? p.a_index_div : 1, t.row0_in, rows};
   const int64_t row0 = p.a_index ? 0 : t.row0_in;
   const uint32_t last = (uint32_t)((p.a_index ? p.a_src_rows : rows) - 1);
-  q.a = p.A + row0 * p.lda;
-  q.as = p.As + row0 * p.las;
-  q.a_bytes = last * (uint32_t)p.lda + (uint32_t)p.nk * kQuantBlock;
-  q.as_bytes = last * (uint32_t)p.las + (uint32_t)p.nk;
+  q.a = p.A + row0 * p.lda + k0 * kQuantBlock;
+  q.as = p.As + row0 * p.las + k0;
+  q.a_bytes = last * (uint32_t)p.lda + (uint32_t)nk * kQuantBlock;
+  q.as_bytes = last * (uint32_t)p.las + (uint32_t)nk;
 #pragma unroll
   for (int x = 0; x < NB; x++) {
-    q.b[x] = p.B[x] + t.group * p.b_group + n0 * p.ldb;
-    q.bs[x] = p.Bs[x] + t.group * p.bs_group + n0 / kQuantBlock * p.lbs;
+    q.b[x] = p.B[x] + t.group * p.b_group + n0 * p.ldb + k0 * kQuantBlock;
+    q.bs[x] = p.Bs[x] + t.group * p.bs_group + n0 / kQuantBlock * p.lbs + k0;
   }
   q.n_valid = min(Core::BN, p.N - n0);
   Epi epi;
   const int64_t c_off = ((int64_t)t.row0_out * p.ldc + n0) * Epi::OES;
 #pragma unroll
-  for (int x = 0; x < Epi::NOUT; x++) epi.out[x] = (char*)p.out[x] + c_off;
+  for (int x = 0; x < Epi::NOUT; x++)
+    epi.out[x] = (PART ? (char*)(p.part + (int64_t)(part * NB + x) * p.n_rows * p.N) : (char*)p.out[x]) + c_off;
 #pragma unroll
   for (int x = 0; x < Epi::NAUX; x++) epi.in[x] = (const char*)p.in[x] + c_off;
   epi.ldc = p.ldc;
@@ -61,7 +65,7 @@ __device__ __forceinline__ void quant_tile(const QuantGemm& p, const RowTile& t,
   epi.scale = p.c_scale;
   epi.index = p.a_index + t.row0_in;
   set_quantised(epi, p, t.row0_out, n0);
-  Core::run(smem, p.nk, q, p.lda, p.las, p.ldb, epi);
+  Core::run(smem, nk, q, p.lda, p.las, p.ldb, p.lbs, epi);
 }
 
 // Heights of the tiles: 256, and for what is left of a group 128 and 64 (tiles of up to 64 rows are bound by streaming the matrix, whatever
@@ -77,7 +81,7 @@ __global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
   extern __shared__ __align__(16) char smem[];
   constexpr int BN = 256 / NB;
   const int ntn = (p.N + BN - 1) / BN;
-  const int n_mt = p.tiles ? *p.n_tiles : (p.n_rows + 255) / 256;
+  const int n_mt = *p.n_tiles;
   const int total = n_mt * ntn, rounds = total >> 8, per_band = kBandRows * ntn;
   const int xcd = blockIdx.x & 7, round = blockIdx.x >> 8, b = (blockIdx.x >> 3) & 31;
   int q = round << 8;
@@ -86,9 +90,7 @@ __global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
   if (q >= total) return;
   const int band = q / per_band, r = q - band * per_band, high = min(kBandRows, n_mt - band * kBandRows);
   const int mt = band * kBandRows + r % high, nt = r / high;
-  RowTile t;
-  if (p.tiles) t = p.tiles[mt];
-  else { t.group = 0; t.row0_in = t.row0_out = mt * 256; t.rows = min(256, p.n_rows - t.row0_in); }
+  RowTile t = p.tiles[mt];
   t.group = __builtin_amdgcn_readfirstlane(t.group);
   t.row0_in = __builtin_amdgcn_readfirstlane(t.row0_in);
   t.rows = __builtin_amdgcn_readfirstlane(t.rows);
@@ -96,6 +98,157 @@ __global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
   if (tile_rows(t) > 128) quant_tile<QuantTall<NB>, Epi, NB>(p, t, nt, smem);
   else if (tile_rows(t) > 64) quant_tile<QuantMid<NB>, Epi, NB>(p, t, nt, smem);
   else quant_tile<QuantShort<NB>, Epi, NB>(p, t, nt, smem);
+}
+
+// Calls of few rows (quant_small): tiles of 64 rows, found in the offsets by the blocks themselves, which costs about a microsecond where a plan takes a
+// launch of seven.
+template <int NB, class Epi>
+__global__ __launch_bounds__(256, 1) void quant_small_gemm_kernel(QuantGemm p) {
+  extern __shared__ __align__(16) char smem[];
+  constexpr int BN = 256 / NB, BM = 64;
+  const int ntn = (p.N + BN - 1) / BN, mt = blockIdx.x / ntn, nt = blockIdx.x - mt * ntn;
+  // four groups a thread: the tiles before them, by shuffles and through LDS
+  __shared__ int32_t wsum[4], found[3];
+  const int g0 = threadIdx.x * 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int off[5], n = 0;
+#pragma unroll
+  for (int i = 0; i < 5; i++) off[i] = p.offsets[min(g0 + i, p.n_groups)];
+#pragma unroll
+  for (int i = 0; i < 4; i++) n += (max(off[i + 1] - off[i], 0) + BM - 1) / BM;
+  int end = n;
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) {
+    const int u = __shfl_up(end, m, kWave);
+    if (lane >= m) end += u;
+  }
+  if (lane == kWave - 1) wsum[wave] = end;
+  if (threadIdx.x < 3) found[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 3; w++) end += w < wave ? wsum[w] : 0;
+  int first = end - n;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int c = max(off[i + 1] - off[i], 0), k = (c + BM - 1) / BM;
+    if (mt >= first && mt < first + k) {
+      found[0] = g0 + i;
+      found[1] = off[i] + (mt - first) * BM;
+      found[2] = min(BM, c - (mt - first) * BM);
+    }
+    first += k;
+  }
+  __syncthreads();
+  RowTile t;
+  t.group = __builtin_amdgcn_readfirstlane(found[0]);
+  t.row0_in = __builtin_amdgcn_readfirstlane(found[1]);
+  t.rows = __builtin_amdgcn_readfirstlane(found[2]);
+  if (t.rows == 0) return;
+  t.row0_out = t.row0_in;
+  quant_tile<QuantShort<NB>, Epi, NB>(p, t, nt, smem);
+}
+
+// One group of n_rows rows: tiles of one height, in parts along K or not; those of a last round that is not full cut into 2 or 4 lower ones.
+template <class Epi, bool PART>
+__global__ __launch_bounds__(256, 1) void quant_direct_gemm_kernel(QuantGemm p) {
+  extern __shared__ __align__(16) char smem[];
+  const int ntn = (p.N + 255) / 256, n_mt = (p.n_rows + p.height - 1) / p.height;
+  const int part = PART ? blockIdx.x / p.part_blocks : 0, block = PART ? blockIdx.x - part * p.part_blocks : blockIdx.x;
+  const int total = n_mt * ntn, rounds = total >> 8, full = rounds << 8, per_band = kBandRows * ntn;
+  // (the order of the tiles: see quant_gemm_kernel)
+  const int xcd = block & 7, round = block >> 8, b = (block >> 3) & 31;
+  int q = block, piece = 0, pieces = 1;
+  if (block < full) {
+    q = (round << 8) + (rounds > kFineRounds && round < rounds - 1 ? (xcd << 5) + b : ((b >> 3) << 6) + (xcd << 3) + (b & 7));
+  } else {
+    pieces = p.tail;
+    q = full + (block - full) / pieces;
+    piece = (block - full) % pieces;
+  }
+  if (q >= total) return;
+  const int band = q / per_band, r = q - band * per_band, high = min(kBandRows, n_mt - band * kBandRows);
+  const int nt = r / high, height = p.height / pieces;
+  RowTile t;
+  t.group = 0;
+  t.row0_in = t.row0_out = (band * kBandRows + r % high) * p.height + piece * height;
+  t.rows = min(height, p.n_rows - t.row0_in);
+  if (t.rows <= 0) return;
+  if (t.rows > 128) quant_tile<QuantTall<1>, Epi, 1, PART>(p, t, nt, smem, part);
+  else if (t.rows > 64) quant_tile<QuantMid<1>, Epi, 1, PART>(p, t, nt, smem, part);
+  else quant_tile<QuantShort<1>, Epi, 1, PART>(p, t, nt, smem, part);
+}
+
+// Calls of up to 512 rows, of up to 1024 over eight groups or more: above, a group's tiles read its matrix too often.  (Forward passes with a plan and so, us:
+// d = 2048, 60 experts of 1408, 32 rows 36 and 32, 512 90 and 82, 1024 98 and 98, 2048 124 and 134; d = 1024, 8 experts of 2816, 32 rows 34 and 32,
+// 512 46 and 45, 1024 65 and 48, 2048 75 and 70, 4096 100 and 109; products of K = 4096, N = 6400, 4 groups, 512 rows 50 and 40, 1024 59 and 72.
+// Sums in parts, joined by another launch, gain where a call has four rows (K = 2048, N = 1408: 13.8 and 11.6 us) and lose from eight on.)
+static bool quant_small(int n_groups, int n_rows) { return n_rows <= 512 || (n_groups >= 8 && n_rows <= 1024); }
+template <int NB, class Epi>
+static void launch_small(const char* label, const QuantGemm& p, hipStream_t st) {
+  const int tiles = p.n_rows / 64 + std::min(p.n_groups, p.n_rows);  // at most
+  launch_gemm<quant_small_gemm_kernel<NB, Epi>>(label, (unsigned)(tiles * ceil_div(p.N, 256 / NB)), 256, QuantShort<NB>::LDS_BYTES, st, p);
+}
+
+// A product of one group: height and parts by an estimate in microseconds, of a block of K (`iter`) and of what a tile takes besides (`fixed`).
+struct DirectQuant {
+  int height = 256, parts = 1, tail = 1;
+  double us = 0;
+};
+static DirectQuant direct_quant(int n_rows, int N, int nk) {
+  static const int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  static const double kIter[] = {1.45, 0.9, 0.6}, kFixed[] = {7, 6, 5};
+  const int only_h = MOE_KNOB("MOE_Q_HEIGHT", 0), only_p = MOE_KNOB("MOE_Q_PARTS", 0), only_t = MOE_KNOB("MOE_Q_TAIL", 0);
+  DirectQuant best;
+  for (int h = 0; h < 3; h++)
+    for (int parts : kParts) {
+      if (parts > 1 && (2 * parts > nk || (int64_t)n_rows * N > (int64_t)1 << 24)) continue;
+      DirectQuant c;
+      c.height = 256 >> h;
+      if ((only_h && only_h != c.height) || (only_p && only_p != parts)) continue;
+      const int its = ceil_div(nk, parts);
+      c.parts = ceil_div(nk, its);
+      const int64_t tiles = (int64_t)ceil_div(n_rows, c.height) * ceil_div(N, 256), blocks = tiles * c.parts;
+      const auto tile_us = [&](int k) { return kFixed[k] + its * kIter[k]; };
+      c.us = (double)(blocks / 256) * tile_us(h);
+      const int rest = (int)(blocks % 256);
+      if (rest > 0) {
+        double last = tile_us(h);
+        if (c.parts == 1)
+          for (int k = h + 1; k < 3; k++)
+            if ((rest << (k - h)) <= 256 && (only_t ? only_t == 1 << (k - h) : tile_us(k) < last)) {
+              last = tile_us(k);
+              c.tail = 1 << (k - h);
+            }
+        c.us += last;
+      }
+      if (c.parts > 1) c.us += 7 + 4e-6 / 4 * c.parts * n_rows * N;
+      if (best.us == 0 || c.us < best.us) best = c;
+    }
+  return best;
+}
+static size_t direct_part_bytes(int n_rows, int N, int nk) {
+  if (n_rows == 0) return 0;
+  const int parts = direct_quant(n_rows, N, nk).parts;
+  return parts == 1 ? 0 : align_up((size_t)parts * n_rows * N * 4, 256);
+}
+static void launch_direct(const char* label, QuantGemm p, float* part, hipStream_t st) {
+  const DirectQuant c = direct_quant(p.n_rows, p.N, p.nk);
+  p.height = c.height;
+  p.tail = c.tail;
+  p.n_parts = c.parts;
+  p.k_part = ceil_div(p.nk, c.parts);
+  p.part = part;
+  const int tiles = ceil_div(p.n_rows, c.height) * ceil_div(p.N, 256);
+  p.part_blocks = (tiles / 256 + (tiles % 256 > 0 && c.tail == 1)) * 256 + (c.tail > 1 ? tiles % 256 * c.tail : 0);
+  constexpr int kLds = std::max({QuantTall<1>::LDS_BYTES, QuantMid<1>::LDS_BYTES, QuantShort<1>::LDS_BYTES});
+  if (c.parts == 1) {
+    launch_gemm<quant_direct_gemm_kernel<Epi8<1, EPI_STORE>, false>>(label, (unsigned)p.part_blocks, 256, kLds, st, p);
+    return;
+  }
+  p.part_blocks = tiles;
+  QuantGemm q = p;
+  q.ldc = p.N;
+  launch_gemm<quant_direct_gemm_kernel<Epi8<1, EPI_PART>, true>>(label, (unsigned)(tiles * c.parts), 256, kLds, st, q);
+  launch_reduce<bf16_t, 1, EPI_STORE>(part, c.parts, (int64_t)p.n_rows * p.N, p.out, nullptr, st);
 }
 
 // At most max_tiles row tiles (the device knows how many there are).
@@ -106,8 +259,6 @@ static void launch_quant(const char* label, const QuantGemm& p, int max_tiles, h
   constexpr int kLds = std::max({QuantTall<NB>::LDS_BYTES, QuantMid<NB>::LDS_BYTES, QuantShort<NB>::LDS_BYTES});
   launch_gemm<quant_gemm_kernel<NB, Epi>>(label, blocks, 256, kLds, st, p);
 }
-template <int NB, int EPI> using Epi8 = Epilogue<bf16_t, NB, EPI>;
-
 // ------------------------------------------------------------------------------------ one product
 static int quant_tiles(int n_groups, int n_rows) { return max_row_tiles(MOE_BF16, n_groups, n_rows, INT32_MAX); }
 static size_t quant_plan_size(int n_groups, int n_rows) { return align_up(plan_bytes(n_groups, plan_cap(n_groups, n_rows) + 1), 256); }
@@ -129,7 +280,7 @@ static int check_launch(int n_groups, int n_rows, int64_t cols, const char* who)
 extern "C" size_t moe_quant_gemm_workspace_bytes(int32_t n_groups, int32_t n_rows, int32_t K, int32_t N) {
   using namespace moe;
   if (n_groups < 1 || n_groups > MOE_MAX_EXPERTS || n_rows < 0 || K < 1 || N < 1) return 0;
-  return quant_plan_size(n_groups, n_rows);
+  return std::max(quant_plan_size(n_groups, n_rows), n_groups == 1 ? direct_part_bytes(n_rows, N, (int)quant_blocks(K)) : 0);
 }
 
 extern "C" int moe_quant_gemm(int32_t n_groups, const int32_t* offsets, int32_t n_rows, int32_t K, int32_t N, const void* A, const void* As,
@@ -159,18 +310,21 @@ extern "C" int moe_quant_gemm(int32_t n_groups, const int32_t* offsets, int32_t 
   if (n_rows == 0) return MOE_OK;
   hipStream_t st = (hipStream_t)stream;
   QuantGemm p = {};
-  int tiles = ceil_div(n_rows, 256);
-  if (offsets) {
-    const Plan pl = carve_plan(ws, n_groups, plan_cap(n_groups, n_rows));
-    launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
-    p.tiles = pl.tiles; p.n_tiles = pl.n_tiles;
-    tiles = quant_tiles(n_groups, n_rows);
-  }
-  p.n_rows = n_rows; p.N = N; p.nk = (int)quant_blocks(K);
+  p.n_rows = n_rows; p.n_groups = n_groups; p.N = N; p.nk = (int)quant_blocks(K);
   p.A = (const uint8_t*)A; p.As = (const uint8_t*)As; p.lda = quant_row(K); p.las = p.nk;
   p.B[0] = (const uint8_t*)B; p.Bs[0] = (const uint8_t*)Bs; p.ldb = p.lda; p.b_group = N * p.ldb; p.lbs = p.nk; p.bs_group = quant_blocks(N) * p.lbs;
   p.out[0] = C; p.ldc = N;
-  launch_quant<1, Epi8<1, EPI_STORE>>("quant_gemm", p, tiles, st);
+  if (!offsets) {
+    launch_direct("quant_gemm", p, (float*)ws, st);
+  } else if (quant_small(n_groups, n_rows)) {
+    p.offsets = offsets;
+    launch_small<1, Epi8<1, EPI_STORE>>("quant_gemm", p, st);
+  } else {
+    const Plan pl = carve_plan(ws, n_groups, plan_cap(n_groups, n_rows));
+    launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
+    p.tiles = pl.tiles; p.n_tiles = pl.n_tiles;
+    launch_quant<1, Epi8<1, EPI_STORE>>("quant_gemm", p, quant_tiles(n_groups, n_rows), st);
+  }
   return launch_status("moe_quant_gemm");
 }
 
@@ -245,12 +399,12 @@ static int fail_null(const char* who) {
 
 extern "C" size_t moe_quant_expert_fwd_workspace_bytes(const moe_shape_t* shape, int32_t n_groups, int32_t n_rows) {
   using namespace moe;
-  if (!shape || n_groups < 1 || n_rows < 0 || shape->d_ff < 1) return 0;
+  if (!shape || n_groups < 1 || n_rows < 0 || shape->d < 1 || shape->d_ff < 1) return 0;
   return QuantSpace(shape, n_groups, n_rows, 1).fwd();
 }
 extern "C" size_t moe_quant_expert_bwd_workspace_bytes(const moe_shape_t* shape, int32_t n_groups, int32_t n_rows) {
   using namespace moe;
-  if (!shape || n_groups < 1 || n_rows < 0 || shape->d_ff < 1) return 0;
+  if (!shape || n_groups < 1 || n_rows < 0 || shape->d < 1 || shape->d_ff < 1) return 0;
   return QuantSpace(shape, n_groups, n_rows, 2).bwd();
 }
 
@@ -281,11 +435,12 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   if (n_rows == 0) return MOE_OK;
   hipStream_t st = (hipStream_t)stream;
   const int d = shape->d, F = shape->d_ff, tiles = max_row_tiles(MOE_BF16, n_groups, n_rows, d);
+  const bool small = quant_small(n_groups, n_rows);
   const Plan pl = carve_plan(plan ? (void*)plan : ws, n_groups, plan_cap(n_groups, n_rows));
-  if (!plan) launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
+  if (!plan && !small) launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
   uint8_t *HQ = (uint8_t*)ws + sp.plan, *HS = HQ + sp.codes;
   QuantGemm p = {};
-  p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
+  p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.offsets = offsets; p.n_rows = n_rows; p.n_groups = n_groups;
   p.N = F; p.nk = (int)quant_blocks(d);
   p.A = (const uint8_t*)XQ; p.As = (const uint8_t*)XS; p.lda = quant_row(d); p.las = p.nk;
   p.a_index = src_of; p.a_index_div = shape->k; p.a_src_rows = shape->T;
@@ -295,23 +450,30 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   p.q[0] = HQ; p.qs[0] = HS; p.ldq = quant_row(F); p.lds = quant_blocks(F);
   typedef Epi8<2, EPI_SWIGLU_FWD> Gated;
   typedef Epi8<1, EPI_GELU_FWD> Plain;
+  auto gate_up = [&](auto nb, auto epi) {
+    if (small) launch_small<decltype(nb)::value, decltype(epi)>("quant_fwd_gate_up", p, st);
+    else launch_quant<decltype(nb)::value, decltype(epi)>("quant_fwd_gate_up", p, tiles, st);
+  };
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 2> two;
   if (G) {
     p.out[0] = G; p.out[1] = gated ? U : H; p.out[2] = H;
-    if (gated) launch_quant<2, QuantOut<Gated, 1, true>>("quant_fwd_gate_up", p, tiles, st);
-    else launch_quant<1, QuantOut<Plain, 1, true>>("quant_fwd_gate_up", p, tiles, st);
+    if (gated) gate_up(two, QuantOut<Gated, 1, true>());
+    else gate_up(one, QuantOut<Plain, 1, true>());
   } else if (gated) {
-    launch_quant<2, QuantOut<LastOutput<Gated>, 1, false>>("quant_fwd_gate_up", p, tiles, st);
+    gate_up(two, QuantOut<LastOutput<Gated>, 1, false>());
   } else {
-    launch_quant<1, QuantOut<LastOutput<Plain>, 1, false>>("quant_fwd_gate_up", p, tiles, st);
+    gate_up(one, QuantOut<LastOutput<Plain>, 1, false>());
   }
   QuantGemm q = {};
-  q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.n_rows = n_rows;
+  q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.offsets = offsets; q.n_rows = n_rows; q.n_groups = n_groups;
   q.N = d; q.nk = (int)quant_blocks(F);
   q.A = HQ; q.As = HS; q.lda = quant_row(F); q.las = q.nk;
   q.B[0] = (const uint8_t*)W->WdT; q.Bs[0] = (const uint8_t*)W->WdT_s;
   q.ldb = q.lda; q.b_group = d * q.ldb; q.lbs = q.nk; q.bs_group = quant_blocks(d) * q.lbs;
   q.out[0] = Yout; q.ldc = d;
-  launch_quant<1, Epi8<1, EPI_STORE>>("quant_fwd_down", q, tiles, st);
+  if (small) launch_small<1, Epi8<1, EPI_STORE>>("quant_fwd_down", q, st);
+  else launch_quant<1, Epi8<1, EPI_STORE>>("quant_fwd_down", q, tiles, st);
   return launch_status(who);
 }
 

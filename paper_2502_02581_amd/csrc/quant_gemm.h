@@ -6,12 +6,15 @@
 
 namespace moe {
 
-// C[rows, N] = A[rows, K] B_g[N, K]^T over the row tiles of a plan, or over n_rows rows of one group.  K is whole blocks: rows of codes
-// are padded with zeros.
+// C[rows, N] = A[rows, K] B_g[N, K]^T over the row tiles of a plan, or (no plan) over the rows of groups that offsets delimit, or (neither) over n_rows
+// rows of one group.  K is whole blocks: rows of codes are padded with zeros.
 struct QuantGemm {
-  const RowTile* tiles;    // NULL: one group of n_rows rows
-  const int32_t* n_tiles;
-  int32_t n_rows;
+  const RowTile* tiles;
+  const int32_t *n_tiles, *offsets;
+  int32_t n_rows, n_groups;
+  int32_t height, tail;                  // one group: rows of a tile (256, 128 or 64); pieces (1, 2 or 4) that tiles of the last round are cut into
+  int32_t n_parts, k_part, part_blocks;  // K is summed in n_parts parts of k_part blocks; launch blocks of a part
+  float* part;                           // n_parts > 1: fp32 sums [n_parts][n_rows][N]
   int32_t N, nk;           // columns, blocks of K
   const uint8_t *A, *As;   // rows of lda codes and las exponents
   int64_t lda, las;

@@ -22,6 +22,9 @@ def text(lib):
 def test_sizes(lib):
     assert [moe.moe_quant_row_bytes(n) for n in (1, 127, 128, 129, 1000)] == [128, 128, 128, 256, 1024]
     assert [moe.moe_quant_scale_bytes(n) for n in (1, 127, 128, 129, 1000)] == [1, 1, 1, 2, 8]
+    for n in list(range(1, 300)) + [4096, 4097, 1 << 22]:   # the binding's arithmetic is the library's
+        assert (moe.moe_quant_row_bytes(n), moe.moe_quant_scale_bytes(n)) == (lib.moe_quant_row_bytes(n), lib.moe_quant_scale_bytes(n))
+    assert ctypes.sizeof(_CGrad) == 48   # whole 64-bit words, as the binding packs them
     assert lib.moe_quant_row_bytes(0) == 0 and lib.moe_quant_scale_bytes(-3) == 0
     assert moe.moe_quant_gemm_workspace_bytes(0, 10, 8, 8) == 0 and moe.moe_quant_gemm_workspace_bytes(4, 10, 128, 128) > 0
 
