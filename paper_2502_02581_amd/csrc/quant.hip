@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ X
       } else {
         for (int i = 0; i < cols - (int)c0; i++) v[i / 2] |= (uint32_t)x[i] << (16 * (i % 2));
       }
-      e = quant_block_bf16(v, codes);
+      e = quant_block_bf16(v, 0xffffffffu, codes);
     } else {
       float v[8];
       load8<T, VEC>(x, cols - (int)c0, v);

@@ -357,8 +357,8 @@ static int check_quant_expert(const moe_shape_t* s, int n_groups, const int32_t*
   if (rc) return rc;
   rc = check_launch(n_groups, n_rows, std::max(s->d, s->d_ff), who);
   if (rc) return rc;
-  // (256 rows of [dG | dU] codes, and of bf16 outputs, within 32-bit byte offsets)
-  if (512 * quant_row(std::max(s->d, s->d_ff)) >= ((int64_t)1 << 32) - 4096) {
+  // (256 rows of [dG | dU] codes, and of bf16 outputs, within 2 GiB: QuantOut)
+  if (512 * quant_row(std::max(s->d, s->d_ff)) >= (int64_t)1 << 31) {
     set_error("%s: rows of d=%d, d_ff=%d values are too long", who, s->d, s->d_ff);
     return MOE_EINVAL;
   }

@@ -42,15 +42,17 @@ __device__ __forceinline__ int row_max16(int v) {
   return max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false));
 }
 // A block of 128 bf16 values, eight in each of sixteen lanes: the lane's codes and the block's exponent byte.  With 0x80 added to their magnitudes
-// infinities and NaN are negative 16-bit numbers and lose against every finite value.
-__device__ __forceinline__ int quant_block_bf16(const uint32_t (&v)[4], uint2& codes) {
+// infinities and NaN are negative 16-bit numbers and lose against every finite value.  `there`: 0xffffffff, or 0 in lanes whose values are not part of
+// the block (codes of zero).
+__device__ __forceinline__ int quant_block_bf16(const uint32_t (&v)[4], uint32_t there, uint2& codes) {
   typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
   typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
   typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
   i16x2_t m = {0x80, 0x80};
+  const uint32_t magnitude = 0x7fff7fffu & there;
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    const u16x2_t t = __builtin_bit_cast(u16x2_t, v[i] & 0x7fff7fffu) + u16x2_t{0x80, 0x80};
+    const u16x2_t t = __builtin_bit_cast(u16x2_t, v[i] & magnitude) + u16x2_t{0x80, 0x80};
     m = __builtin_elementwise_max(m, __builtin_bit_cast(i16x2_t, t));
   }
   const int e = quant_exponent((uint32_t)(row_max16(max((int)m[0], (int)m[1])) - 0x80) << 16);
@@ -61,7 +63,7 @@ __device__ __forceinline__ int quant_block_bf16(const uint32_t (&v)[4], uint2& c
     c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[2 * i]), scale, false);
     c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[2 * i + 1]), scale, true);
   }
-  codes = make_uint2(__builtin_bit_cast(uint32_t, c[0]), __builtin_bit_cast(uint32_t, c[1]));
+  codes = make_uint2(__builtin_bit_cast(uint32_t, c[0]) & there, __builtin_bit_cast(uint32_t, c[1]) & there);
   return e;
 }
 
