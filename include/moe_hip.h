@@ -354,7 +354,7 @@ int moe_combine_bwd(const moe_shape_t* shape, const void* dY, const void* Yp, co
  *            (bytes between rows; a group's rows follow those of the group before)
  *
  * moe_quant_gemm -- grouped product over variable row counts: C[r, n] = sum_k A[r, k] B_g[n, k] for the rows r of group g,
- *   offsets [n_groups + 1] as in moe_expert_fwd, or NULL: one group of n_rows rows.
+ *   offsets [n_groups + 1] as in moe_expert_fwd (ascending, within 0 and n_rows), or NULL: one group of n_rows rows.
  *   A, As: rows of K values (moe_quant_rows);  B, Bs: [n_groups, N, K] (Qt, St of moe_quant_weights on [n_groups, K, N]), tight rows;
  *   C [n_rows, N] bf16, N a multiple of 8; K and N up to 2^22.  Rows outside the offsets' range are not touched.
  *   Sums are fp32.  The matrix instruction adds products of eight neighbouring values of K after aligning them to the largest, with 13 bits below it;
@@ -362,7 +362,7 @@ int moe_combine_bwd(const moe_shape_t* shape, const void* dY, const void* Yp, co
  *   ws >= moe_quant_gemm_workspace_bytes(n_groups, n_rows, K, N)
  *
  * moe_quant_expert_fwd / moe_quant_expert_bwd -- moe_expert_fwd / _bwd of routed experts whose products (but those of the weight gradients) run on
- *   block-scaled operands; bf16 only.  quant() is moe_quant_rows:
+ *   block-scaled operands; bf16 only, d and d_ff below 2^22.  quant() is moe_quant_rows:
  *   forward:  G = XQ_e Wg[e], U = XQ_e Wu[e], H = silu(G) * U, Yout_e = quant(H) Wd[e];  two-matrix experts (gated = 0): H = gelu(G).
  *     H is rounded to bf16 before it is quantised, so that the H that is kept is the one that was used.
  *     src_of != NULL: row r is row src_of[r] / shape->k of XQ, the tokens in their own order (n_rows = T*k); NULL: XQ has n_rows rows.
@@ -404,7 +404,7 @@ int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, const int32
 /*
  * moe_grad_norm / moe_grad_clip -- the norm of many gradients taken as one vector, and their clipping to it.
  *   norm = sqrt(sum of the squares of all values), summed in 64 bits in a fixed order (two calls give the same bits), rounded to f32
- *   out  = g * min(1, max_norm / (norm + 1e-6)), the factor in f32, rounded to the gradient's type
+ *   out  = g * min(1, max_norm / (norm + 1e-6)), the factor rounded to f32, the product to the gradient's type
  * A gradient is n values, f32 or bf16, 16-byte aligned.  With n_active (device) it is the first min(n, n_active[0] * slot) of them: the compacted weight
  * gradients of moe_expert_bwd, whose number only the GPU knows; values behind those are neither read nor written.
  * out may be g itself (then nothing is written where the factor is 1), and must not overlap any gradient otherwise; moe_grad_norm does not

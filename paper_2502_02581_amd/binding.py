@@ -519,6 +519,12 @@ def _sized(t, shape, what, dtype=torch.uint8):
     return _ptr(t, dtype, what)
 
 
+def _here(t, who):
+    """Refuses tensors of another GPU than the current one, on which the call would launch."""
+    if t.device.index != torch.cuda.current_device():
+        raise MoEError(f"{who}: the tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
 def _pitched(t, shape, what):
     """Pointer and bytes between rows of a [groups, rows, bytes] tensor whose rows may be pieces of longer ones."""
     if t is None:
@@ -554,6 +560,7 @@ def moe_quant_rows(X, Q, S, stream=None):
     ldx = max(X.stride(0), cols) if n > 1 else cols
     if n > 1 and X.stride(0) < cols:
         raise MoEError("X: rows must not overlap")
+    _here(X, "moe_quant_rows")
     rc = load_library().moe_quant_rows(X.data_ptr(), dt, n, cols, ldx, _sized(Q, (n, moe_quant_row_bytes(cols)), "Q"),
                                        _sized(S, (n, moe_quant_scale_bytes(cols)), "S"), _stream(stream))
     _check(rc, "moe_quant_rows")
@@ -568,6 +575,8 @@ def moe_quant_weights(W, Q, S, Qt, St, stream=None):
     g, K, N = W.shape
     b = moe_quant_scale_bytes
     args = []
+    _ptr(W, None, "W")
+    _here(W, "moe_quant_weights")
     for t, shape, what in ((Q, (g, K, moe_quant_row_bytes(N)), "Q"), (S, (g, b(K), b(N)), "S"),
                            (Qt, (g, N, moe_quant_row_bytes(K)), "Qt"), (St, (g, b(N), b(K)), "St")):
         args += _pitched(t, shape, what)
@@ -583,6 +592,7 @@ def moe_quant_gemm(offsets, K: int, A, As, B, Bs, C, ws, stream=None):
     layout of moe_quant_weights; offsets [groups + 1], or None for one group."""
     (n, N), g = C.shape, B.shape[0]
     kb, rb = moe_quant_scale_bytes(K), moe_quant_row_bytes(K)
+    _here(C, "moe_quant_gemm")
     if offsets is not None:
         _sized(offsets, (g + 1,), "offsets", torch.int32)
     rc = load_library().moe_quant_gemm(g, _ptr(offsets, torch.int32, "offsets"), n, K, N, _sized(A, (n, rb), "A"), _sized(As, (n, kb), "As"),
@@ -664,6 +674,7 @@ def _quant_args(shape, n_groups, n_rows, src_of, Q, S, W, who):
     if W.n_groups != n_groups or (W.shape.d, W.shape.d_ff) != (shape.d, shape.d_ff):
         raise MoEError(f"{who}: the weights are those of {W.n_groups} experts of d={W.shape.d}, d_ff={W.shape.d_ff}")
     rows = n_rows if src_of is None else shape.T
+    _here(Q, who)
     return (_sized(Q, (rows, moe_quant_row_bytes(shape.d)), "codes"), _sized(S, (rows, moe_quant_scale_bytes(shape.d)), "exponents"))
 
 
@@ -700,7 +711,7 @@ def _grad_list(grads, out=None):
     structures one by one."""
     if out is not None and len(out) != len(grads):
         raise MoEError(f"{len(grads)} gradients, {len(out)} outputs")
-    members = []
+    members, counters = [], {}   # (a counter serves the tensors of a layer: looked at once)
     for i, x in enumerate(grads):
         n_active, slot = None, 1
         if not isinstance(x, torch.Tensor):
@@ -719,7 +730,9 @@ def _grad_list(grads, out=None):
             o = y.data_ptr()
         if n_active is not None:
             slot = n // x.shape[0] if n else 1
-            n_active = _ptr(n_active, torch.int32, "n_active")
+            if id(n_active) not in counters:
+                counters[id(n_active)] = _ptr(n_active, torch.int32, "n_active")
+            n_active = counters[id(n_active)]
         members += (g, o, n, n_active or 0, slot, MOE_F32 if dt is torch.float32 else MOE_BF16)
     if not members:
         return (_CGrad * 1)()
@@ -733,6 +746,7 @@ def moe_grad_norm_workspace_bytes() -> int:
 def moe_grad_norm(grads, norm, ws, stream=None):
     """norm [1] = the norm of all gradients taken as one vector.  An entry is a tensor, or (tensor [slots, ...], n_active): a compacted
     gradient, whose first n_active slots (a number on the GPU) count."""
+    _here(norm, "moe_grad_norm")
     rc = load_library().moe_grad_norm(_grad_list(grads), len(grads), _ptr(norm, torch.float32, "norm"), _ptr(ws, None, "ws"),
                                       ws.numel() * ws.element_size(), _stream(stream))
     _check(rc, "moe_grad_norm")
@@ -740,6 +754,7 @@ def moe_grad_norm(grads, norm, ws, stream=None):
 
 def moe_grad_clip(grads, norm, max_norm: float, out=None, stream=None):
     """The same list times min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
+    _here(norm, "moe_grad_clip")
     rc = load_library().moe_grad_clip(_grad_list(grads, out), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
     _check(rc, "moe_grad_clip")
 

@@ -109,9 +109,12 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* out, int64_t from, in
 }
 __global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(GradList l, const float* norm, float max_norm) {
   // (a norm that is NaN makes the factor NaN, so that it is seen in the gradients, too)
-  const float f0 = max_norm / (*norm + 1e-6f), f = f0 >= 1.f ? 1.f : f0;
-  for (uint32_t c = blockIdx.x; c < l.first[l.count]; c += gridDim.x) {
-    const Chunk k = find_chunk(l, c);
+  const double f0 = (double)max_norm / ((double)*norm + 1e-6);
+  const float f = f0 >= 1. ? 1.f : (float)f0;
+  // The last chunks first: the norm's pass has left them in the memory-side cache.
+  const uint32_t n = l.first[l.count];
+  for (uint32_t c = blockIdx.x; c < n; c += gridDim.x) {
+    const Chunk k = find_chunk(l, n - 1 - c);
     if (k.from >= k.to || (f == 1.f && l.g[k.t] == l.out[k.t])) continue;
     if (l.f32 >> k.t & 1) chunk_scale((const float*)l.g[k.t], (float*)l.out[k.t], k.from, k.to, f);
     else chunk_scale((const bf16_t*)l.g[k.t], (bf16_t*)l.out[k.t], k.from, k.to, f);
@@ -203,9 +206,11 @@ extern "C" int moe_grad_clip(const moe_grad_t* grads, int32_t n, const float* no
   }
   hipStream_t st = (hipStream_t)stream;
   bool any = false;
-  for (int i = 0; i < n;) {
+  for (int i = n; i > 0;) {  // (see grad_scale_kernel for the order)
+    const int from = std::max(i - kGradsPerLaunch, 0);
     GradList l;
-    i = fill_list(l, grads, n, i);
+    fill_list(l, grads, i, from);
+    i = from;
     if (l.count == 0) continue;
     any = true;
     ProfScope prof("grad_scale_kernel", st);

@@ -68,6 +68,9 @@ struct QuantCore {
   static constexpr int LDS_BYTES = SLOTS * SLOT_BYTES;
   static constexpr int L = A_NI + NB * B_NI + 1 + NB;  // loads a wave and iteration
   static constexpr int H = TM * HB;                    // MFMAs of a phase
+  // MFMA ahead of which the fragments of t have been read; the loads of t + SLOTS are spread from there on, up to END
+  static constexpr int FREE = std::min(HB * std::max(H / (2 * HB), 1), H), END = 2 * H - (SLOTS == 2 ? H * 3 / 8 : 0);
+  static constexpr int loads_before(int s) { return s <= FREE ? 0 : s >= END ? L : (s - FREE) * L / (END - FREE); }
   static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
   static_assert((SLOTS - 1) * L <= 63, "the wait count must be encodable");
   static_assert(BN / WN == kQuantBlock, "the columns of a wave are one block");
@@ -274,24 +277,29 @@ struct QuantCore {
       const uint32_t nxt = cur == (SLOTS - 1) * SLOT_BYTES ? 0u : cur + SLOT_BYTES;
       static_for<2 * H>([&](auto slot_c) __attribute__((always_inline)) {
         constexpr int s = decltype(slot_c)::value, m = s % H, i = m / HB, j = m % HB, step = std::max(H / (2 * HB), 1);
+        constexpr int n0 = loads_before(s), n1 = loads_before(s + 1);
+        if constexpr (s == FREE && FREE < H) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __syncthreads();
+        }
+        if constexpr (s == H) landed(std::integral_constant<int, (SLOTS - 2) * L + n0>());
         if constexpr (s < H) {
           if constexpr (s == 0) read_a(std::integral_constant<int, TM - 1>(), cur);
           if constexpr (m % step == 0 && m / step < HB) read_hi(std::integral_constant<int, m / step>(), cur);
-          mfma(acc[0][i][j], fl[j], fa[i], sl, sa[i]);
         } else {
-          if constexpr (m == 0) landed(std::integral_constant<int, (SLOTS - 2) * L>());
           if constexpr (m % step == 0 && m / step < HB) read_lo(std::integral_constant<int, m / step>(), nxt);
           if constexpr (m > 0 && j == 0) read_a(std::integral_constant<int, i - 1>(), nxt);
-          constexpr int n0 = m * L / H, n1 = (m + 1) * L / H;
-          f32x4_t& x = NB == 2 ? acc[NB - 1][i][j] : acc[0][i][TN - HB + j];
-          if constexpr (n1 > n0) {
-            each_load(std::integral_constant<int, n0>(), cur, [&](auto plus, auto word, const rsrc_t& r, uint32_t base, uint32_t vo) __attribute__((always_inline)) {
-              mfma_load<decltype(plus)::value, decltype(word)::value>(x, fh[j], fa[i], sh, sa[i], r, base, vo);
-            });
-            static_for<n1 - n0 - 1>([&](auto y) __attribute__((always_inline)) { issue(std::integral_constant<int, n0 + 1 + decltype(y)::value>(), cur); });
-          } else {
-            mfma(x, fh[j], fa[i], sh, sa[i]);
-          }
+        }
+        f32x4_t& x = s < H ? acc[0][i][j] : NB == 2 ? acc[NB - 1][i][j] : acc[0][i][TN - HB + j];
+        const frag_t& fb = s < H ? fl[j] : fh[j];
+        const int sb = s < H ? sl : sh;
+        if constexpr (n1 > n0) {
+          each_load(std::integral_constant<int, n0>(), cur, [&](auto plus, auto word, const rsrc_t& r, uint32_t base, uint32_t vo) __attribute__((always_inline)) {
+            mfma_load<decltype(plus)::value, decltype(word)::value>(x, fb, fa[i], sb, sa[i], r, base, vo);
+          });
+          static_for<n1 - n0 - 1>([&](auto y) __attribute__((always_inline)) { issue(std::integral_constant<int, n0 + 1 + decltype(y)::value>(), cur); });
+        } else {
+          mfma(x, fb, fa[i], sb, sa[i]);
         }
       });
       next(c);

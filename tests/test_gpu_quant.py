@@ -417,9 +417,19 @@ def test_experts_in_a_graph_and_on_another_stream():
         torch.cuda.synchronize()
 
 
-def test_refusals_of_the_binding():
+def test_refusals_of_the_binding(monkeypatch):
     m = moe()
     L = Layer(20, 4, 2, 64, 64, True, True)
+    with monkeypatch.context() as other:   # as if another GPU were the current one
+        other.setattr(torch.cuda, "current_device", lambda: 1)
+        with pytest.raises(m.MoEError, match="current device"):
+            m.moe_quant_rows(L.X, *L.xq)
+        with pytest.raises(m.MoEError, match="current device"):
+            L.weights.update(*L.W)
+        with pytest.raises(m.MoEError, match="current device"):
+            L.forward()
+        with pytest.raises(m.MoEError, match="current device"):
+            m.moe_grad_norm([], torch.zeros(1, device=DEV), L.ws)
     with pytest.raises(m.MoEError, match="shape"):
         m.moe_quant_rows(torch.randn(4, 64, device=DEV), u8(4, 64), u8(4, 1))
     with pytest.raises(m.MoEError, match="float32 or bfloat16"):
