@@ -39,12 +39,12 @@ __device__ __forceinline__ Chunk find_chunk(const GradList& l, uint32_t c) {
 }
 
 // Squares are summed in 64 bits: no overflow or underflow for any finite gradient, and an error that is far below the result's rounding
-// whatever the number of values.  A lane has eight loads of 16 bytes in flight; its partial sum, the block's and those of the blocks are added in a
+// whatever the number of values.  A lane has eight loads of 16 bytes in flight and four sums; its partial sum, the block's and those of the blocks are added in a
 // fixed order, so two calls give the same bits.
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* g, int64_t from, int64_t to) {
-  constexpr int N = Vec16<T>::N, U = 4;
-  double s = 0;
+  constexpr int N = Vec16<T>::N, U = 8;
+  double t[4] = {};
   int64_t i = from + (int64_t)threadIdx.x * N;
   for (; i + (int64_t)(U - 1) * kGradThreads * N + N <= to; i += (int64_t)U * kGradThreads * N) {
     float v[U][N];
@@ -53,8 +53,9 @@ __device__ __forceinline__ double chunk_squares(const T* g, int64_t from, int64_
 #pragma unroll
     for (int u = 0; u < U; u++)
 #pragma unroll
-      for (int j = 0; j < N; j++) s = fma((double)v[u][j], (double)v[u][j], s);
+      for (int j = 0; j < N; j++) t[j & 3] = fma((double)v[u][j], (double)v[u][j], t[j & 3]);
   }
+  double s = (t[0] + t[1]) + (t[2] + t[3]);
   for (; i < to; i += (int64_t)kGradThreads * N)
     for (int j = 0; j < N && i + j < to; j++) {
       const double x = Elem<T>::load(g + i + j);

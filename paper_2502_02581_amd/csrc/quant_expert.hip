@@ -88,7 +88,13 @@ __global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
   if (round < rounds) q += rounds > kFineRounds && round < rounds - 1 ? (xcd << 5) + b : ((b >> 3) << 6) + (xcd << 3) + (b & 7);
   else q += (b << 3) + xcd;
   if (q >= total) return;
-  const int band = q / per_band, r = q - band * per_band, high = min(kBandRows, n_mt - band * kBandRows);
+  // Launches of four rounds and more take bands two from the front, one from the back, until a third of them have come from the back: short tiles, bound
+  // by streaming their matrices, beside tall ones.  (The last band, which may have fewer rows, stays the last.  Longest first and so, us: gate/up of
+  // 16384 rows, d = 2048, 60 experts of 1408, Zipf loads, 202 and 184, of 32768 264 and 252, down 137 and 136; 16384 rows, d = 7168, 128 experts of 2048 870
+  // and 876, down 472 and 457; launches of two to three rounds lose, gate/up of 9003 rows, d = 1000, 24 experts of 1368, 74 and 83, dH 75 and 93.)
+  const int at = q / per_band, r = q - at * per_band, bands = n_mt / kBandRows, from_back = rounds >= 4 ? bands / 3 : 0, mixed = 3 * from_back;
+  const int band = at >= bands ? at : at >= mixed ? at - from_back : at % 3 == 2 ? bands - 1 - at / 3 : at / 3 * 2 + at % 3;
+  const int high = min(kBandRows, n_mt - band * kBandRows);
   const int mt = band * kBandRows + r % high, nt = r / high;
   RowTile t = p.tiles[mt];
   t.group = __builtin_amdgcn_readfirstlane(t.group);

@@ -143,6 +143,8 @@ GEMM_CASES = [
     ([1], 8, 8), ([1], 128, 16), ([16], 256, 64), ([17], 1000, 136), ([5, 0, 3], 136, 40), ([0, 0, 1], 128, 128), ([0, 0], 64, 64),
     ([64, 65, 63, 1, 0, 128], 384, 264), ([257, 3, 96], 512, 520), ([300, 200, 140, 33], 256, 256), ([513], 640, 384), ([700, 0, 130, 15, 16, 31], 200, 200),
     ([1] * 40, 256, 128), ([2, 0] * 30, 1408, 72), ([256, 512, 128], 128, 256), ([33], 4096, 48), ([1], 7168, 512), ([16], 7168, 256), ([100], 2304, 640),
+    ([300], 7168, 256), ([5000], 128, 4096),            # one group: parts of tall tiles, a last round cut into low ones
+    ([37 * i % 300 for i in range(60)], 128, 4096),     # four rounds of tiles: the order that mixes heights
 ]
 
 
