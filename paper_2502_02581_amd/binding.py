@@ -590,6 +590,8 @@ def moe_quant_gemm_workspace_bytes(n_groups: int, n_rows: int, K: int, N: int) -
 def moe_quant_gemm(offsets, K: int, A, As, B, Bs, C, ws, stream=None):
     """C [n_rows, N] (bf16) = A B_g^T over the rows of every group: A, As from moe_quant_rows on rows of K values, B [groups, N, .], Bs the transposed
     layout of moe_quant_weights; offsets [groups + 1], or None for one group."""
+    if C.dim() != 2 or B.dim() != 3:
+        raise MoEError("C must be [n_rows, N], B [groups, N, .]")
     (n, N), g = C.shape, B.shape[0]
     kb, rb = moe_quant_scale_bytes(K), moe_quant_row_bytes(K)
     _here(C, "moe_quant_gemm")
@@ -706,9 +708,9 @@ def moe_quant_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, row
 
 
 # ---- gradients: lists of tensors, or of (tensor, n_active) for compacted ones [slots, ...]
-def _grad_list(grads, out=None):
+def _grad_list(grads, out=None, written=False):
     """The C form of a list of gradients: its members as one buffer of whole numbers, which for many small tensors takes half the time of
-    structures one by one."""
+    structures one by one.  written: no tensor may be an output twice."""
     if out is not None and len(out) != len(grads):
         raise MoEError(f"{len(grads)} gradients, {len(out)} outputs")
     members, counters = [], {}   # (a counter serves the tensors of a layer: looked at once)
@@ -729,11 +731,17 @@ def _grad_list(grads, out=None):
                 raise MoEError(f"output {i} must be a contiguous {dt} tensor on the GPU of shape {tuple(x.shape)}")
             o = y.data_ptr()
         if n_active is not None:
+            if x.dim() == 0:
+                raise MoEError(f"gradient {i} must be [slots, ...]")
             slot = n // x.shape[0] if n else 1
             if id(n_active) not in counters:
                 counters[id(n_active)] = _ptr(n_active, torch.int32, "n_active")
             n_active = counters[id(n_active)]
         members += (g, o, n, n_active or 0, slot, MOE_F32 if dt is torch.float32 else MOE_BF16)
+    if written:
+        outs = [o for o, n in zip(members[1::6], members[2::6]) if n]
+        if len(set(outs)) != len(outs):
+            raise MoEError("a tensor is there twice")
     if not members:
         return (_CGrad * 1)()
     return (_CGrad * len(grads)).from_buffer(bytearray(struct.pack(f"={len(members)}q", *members)))
@@ -755,7 +763,7 @@ def moe_grad_norm(grads, norm, ws, stream=None):
 def moe_grad_clip(grads, norm, max_norm: float, out=None, stream=None):
     """The same list times min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
     _here(norm, "moe_grad_clip")
-    rc = load_library().moe_grad_clip(_grad_list(grads, out), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
+    rc = load_library().moe_grad_clip(_grad_list(grads, out, written=True), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
     _check(rc, "moe_grad_clip")
 
 

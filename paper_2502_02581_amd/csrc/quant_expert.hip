@@ -202,14 +202,12 @@ struct DirectQuant {
 static DirectQuant direct_quant(int n_rows, int N, int nk) {
   static const int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
   static const double kIter[] = {1.45, 0.9, 0.6}, kFixed[] = {7, 6, 5};
-  const int only_h = MOE_KNOB("MOE_Q_HEIGHT", 0), only_p = MOE_KNOB("MOE_Q_PARTS", 0), only_t = MOE_KNOB("MOE_Q_TAIL", 0);
   DirectQuant best;
   for (int h = 0; h < 3; h++)
     for (int parts : kParts) {
       if (parts > 1 && (2 * parts > nk || (int64_t)n_rows * N > (int64_t)1 << 24)) continue;
       DirectQuant c;
       c.height = 256 >> h;
-      if ((only_h && only_h != c.height) || (only_p && only_p != parts)) continue;
       const int its = ceil_div(nk, parts);
       c.parts = ceil_div(nk, its);
       const int64_t tiles = (int64_t)ceil_div(n_rows, c.height) * ceil_div(N, 256), blocks = tiles * c.parts;
@@ -220,7 +218,7 @@ static DirectQuant direct_quant(int n_rows, int N, int nk) {
         double last = tile_us(h);
         if (c.parts == 1)
           for (int k = h + 1; k < 3; k++)
-            if ((rest << (k - h)) <= 256 && (only_t ? only_t == 1 << (k - h) : tile_us(k) < last)) {
+            if ((rest << (k - h)) <= 256 && tile_us(k) < last) {
               last = tile_us(k);
               c.tail = 1 << (k - h);
             }

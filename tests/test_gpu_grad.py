@@ -134,3 +134,11 @@ def test_refusals():
         m.moe_grad_clip([x[1:]], norm, 1.0)
     with pytest.raises(m.MoEError, match="float32 or bfloat16"):
         m.moe_grad_clip([x.half()], norm, 1.0)
+    with pytest.raises(m.MoEError, match="twice"):
+        m.moe_grad_clip([x, x], norm, 1.0)
+    with pytest.raises(m.MoEError, match="twice"):
+        m.moe_grad_clip([x, x.clone()], norm, 1.0, [x, x])
+    with pytest.raises(m.MoEError, match="slots"):
+        m.moe_grad_norm([(x[0], torch.ones(1, dtype=torch.int32, device=DEV))], norm, torch.empty(1 << 14, dtype=torch.uint8, device=DEV))
+    with pytest.raises(m.MoEError, match="GPU"):
+        m.moe_grad_norm([torch.ones(3)], norm, ws)
