@@ -1048,10 +1048,12 @@ void expert_bwd_impl(const BwdArgs* r, const BwdArgs* s, hipStream_t st) {
 }
 
 // The weight gradients of expert_bwd_impl alone, for routed experts whose other products are computed elsewhere (moe_quant_expert_bwd): dG and
-// dU are given, the plan is in ws.  The kernels are those of the launches above, without row tiles.
+// dU are given, the plan is in ws.
+struct DwGemms {
+  WGemm dwd, dwgu, dwd_light, dwgu_light;
+};
 template <int PATH>
-void expert_dw_impl(const BwdArgs& a, hipStream_t st) {
-  typedef Cores<PATH> C;
+static DwGemms dw_gemms(const BwdArgs& a) {
   const Plan pl = carve_plan(a.ws, a.n_groups, plan_cap(a.n_groups, a.n_rows));
   WGemm w = {};
   w.ginfo = pl.ginfo; w.n_rows = a.n_rows; w.n_groups = a.n_groups;
@@ -1064,30 +1066,37 @@ void expert_dw_impl(const BwdArgs& a, hipStream_t st) {
   v.A = a.Xin; v.lda = a.d;
   v.B[0] = a.dG; v.B[1] = a.dU; v.ldb = a.F;
   v.C[0] = a.dWg; v.C[1] = a.dWu;
-  WGemm wl_ = w, vl_ = v;
-  w.k_min = v.k_min = kLightGroupRows + 1;
-  w.k_max = v.k_max = 0x7fffffff;
-  wl_.k_min = vl_.k_min = 1;
-  wl_.k_max = vl_.k_max = kLightGroupRows;
+  DwGemms r = {w, v, w, v};
+  r.dwd.k_min = r.dwgu.k_min = kLightGroupRows + 1;
+  r.dwd.k_max = r.dwgu.k_max = 0x7fffffff;
+  r.dwd_light.k_min = r.dwgu_light.k_min = 1;
+  r.dwd_light.k_max = r.dwgu_light.k_max = kLightGroupRows;
   auto even_reps = [&](int n_cols) {
-    const int ntn = ceil_div(n_cols, C::template core_light<1>::BN);
+    const int ntn = ceil_div(n_cols, Cores<PATH>::template core_light<1>::BN);
     return ceil_div(ntn, ceil_div(ntn, kLightReps));
   };
-  wl_.n_reps = even_reps(wl_.N);
-  vl_.n_reps = even_reps(vl_.N);
+  r.dwd_light.n_reps = even_reps(w.N);
+  r.dwgu_light.n_reps = even_reps(v.N);
+  return r;
+}
+// In the kernels of the launches above, without row tiles.
+template <int PATH>
+void expert_dw_impl(const BwdArgs& a, hipStream_t st) {
+  typedef Cores<PATH> C;
   typedef RowCores<PATH, 1, true> Rows;
   typedef typename C::template core<1, false, false> W1;
   typedef typename C::template core<2, false, false> W2;
+  const DwGemms g = dw_gemms<PATH>(a);
   const RowGemm none = {};
   constexpr int kLds1 = std::max(row_lds_bytes<Rows>(), W1::LDS_BYTES), kLds2 = std::max(row_lds_bytes<Rows>(), W2::LDS_BYTES);
   if (a.Wu) {
-    launch_gemm<row_w_gemm_kernel<Rows, EPI_SWIGLU_BWD, W1, 1, true>>("gemm_bwd_dwd", w_block_count<W1>(w), W1::NT, kLds1, st, none, w, 0, 0);
-    launch_gemm<row_w_gemm_kernel<Rows, EPI_STORE, W2, 2, true>>("gemm_bwd_dwgu", w_block_count<W2>(v), W2::NT, kLds2, st, none, v, 0, 0);
+    launch_gemm<row_w_gemm_kernel<Rows, EPI_SWIGLU_BWD, W1, 1, true>>("gemm_bwd_dwd", w_block_count<W1>(g.dwd), W1::NT, kLds1, st, none, g.dwd, 0, 0);
+    launch_gemm<row_w_gemm_kernel<Rows, EPI_STORE, W2, 2, true>>("gemm_bwd_dwgu", w_block_count<W2>(g.dwgu), W2::NT, kLds2, st, none, g.dwgu, 0, 0);
   } else {
-    launch_gemm<row_w_gemm_kernel<Rows, EPI_GELU_BWD, W1, 1, true>>("gemm_bwd_dwd", w_block_count<W1>(w), W1::NT, kLds1, st, none, w, 0, 0);
-    launch_gemm<row_w_gemm_kernel<Rows, EPI_STORE, W1, 1, true>>("gemm_bwd_dwgu", w_block_count<W1>(v), W1::NT, kLds1, st, none, v, 0, 0);
+    launch_gemm<row_w_gemm_kernel<Rows, EPI_GELU_BWD, W1, 1, true>>("gemm_bwd_dwd", w_block_count<W1>(g.dwd), W1::NT, kLds1, st, none, g.dwd, 0, 0);
+    launch_gemm<row_w_gemm_kernel<Rows, EPI_STORE, W1, 1, true>>("gemm_bwd_dwgu", w_block_count<W1>(g.dwgu), W1::NT, kLds1, st, none, g.dwgu, 0, 0);
   }
-  launch_w_light<typename C::template core_light<1>>("gemm_bwd_dw_light", wl_, vl_, a.Wu ? 2 : 1, st);
+  launch_w_light<typename C::template core_light<1>>("gemm_bwd_dw_light", g.dwd_light, g.dwgu_light, a.Wu ? 2 : 1, st);
 }
 
 // ------------------------------------------------------------------------------------ router

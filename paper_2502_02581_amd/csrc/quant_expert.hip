@@ -77,13 +77,12 @@ template <int NB> using QuantShort = QuantCore<64, NB, 3>;
 // Tiles are dealt to the XCDs as in row_gemm_block: band by band of kBandRows row tiles, column by column within a band, runs of 32 (launches of
 // few rounds: of 8) consecutive tiles to an XCD.
 template <int NB, class Epi>
-__global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
-  extern __shared__ __align__(16) char smem[];
+__device__ __forceinline__ void quant_gemm_block(const QuantGemm& p, int block, char* smem) {
   constexpr int BN = 256 / NB;
   const int ntn = (p.N + BN - 1) / BN;
   const int n_mt = *p.n_tiles;
   const int total = n_mt * ntn, rounds = total >> 8, per_band = kBandRows * ntn;
-  const int xcd = blockIdx.x & 7, round = blockIdx.x >> 8, b = (blockIdx.x >> 3) & 31;
+  const int xcd = block & 7, round = block >> 8, b = (block >> 3) & 31;
   int q = round << 8;
   if (round < rounds) q += rounds > kFineRounds && round < rounds - 1 ? (xcd << 5) + b : ((b >> 3) << 6) + (xcd << 3) + (b & 7);
   else q += (b << 3) + xcd;
@@ -104,6 +103,20 @@ __global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
   if (tile_rows(t) > 128) quant_tile<QuantTall<NB>, Epi, NB>(p, t, nt, smem);
   else if (tile_rows(t) > 64) quant_tile<QuantMid<NB>, Epi, NB>(p, t, nt, smem);
   else quant_tile<QuantShort<NB>, Epi, NB>(p, t, nt, smem);
+}
+template <int NB, class Epi>
+__global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
+  extern __shared__ __align__(16) char smem[];
+  quant_gemm_block<NB, Epi>(p, blockIdx.x, smem);
+}
+// An input gradient and a weight gradient that does not depend on it (bf16) in one launch, as in row_w_gemm_kernel: the tiles of the one fill the units
+// that the last tiles of the other leave idle.
+template <class Epi, class WCore, int WNB>
+__global__ __launch_bounds__(256, 1) void quant_w_gemm_kernel(QuantGemm p, WGemm w, int first_w, int rows, int w_blocks) {
+  extern __shared__ __align__(16) char smem[];
+  const int b = (int)blockIdx.x, row = b - first_w, wb = row < 0 ? b : row - rows;
+  if (row >= 0 && row < rows) quant_gemm_block<1, Epi>(p, row, smem);
+  else if (wb < w_blocks) w_gemm_block<WCore, WNB, true>(w, wb, smem);
 }
 
 // Calls of few rows (quant_small): tiles of 64 rows, found in the offsets by the blocks themselves, which costs about a microsecond where a plan takes a
@@ -263,6 +276,15 @@ static void launch_quant(const char* label, const QuantGemm& p, int max_tiles, h
   constexpr int kLds = std::max({QuantTall<NB>::LDS_BYTES, QuantMid<NB>::LDS_BYTES, QuantShort<NB>::LDS_BYTES});
   launch_gemm<quant_gemm_kernel<NB, Epi>>(label, blocks, 256, kLds, st, p);
 }
+template <class Epi, class WCore, int WNB>
+static void launch_quant_w(const char* label, const QuantGemm& p, int max_tiles, const WGemm& w, hipStream_t st) {
+  constexpr int kLds = std::max({QuantTall<1>::LDS_BYTES, QuantMid<1>::LDS_BYTES, QuantShort<1>::LDS_BYTES, WCore::LDS_BYTES});
+  const unsigned rows = row_block_count(max_tiles, p.N, 256), w_blocks = w_block_count<WCore>(w);
+  const int first = MOE_KNOB("MOE_Q_WFIRST", 0);
+  const unsigned first_w = first ? (w_blocks + 7) / 8 * 8 : 0;
+  launch_gemm<quant_w_gemm_kernel<Epi, WCore, WNB>>(label, rows + (first ? first_w : w_blocks), 256, kLds, st, p, w, (int)first_w, (int)rows, (int)w_blocks);
+}
+
 // ------------------------------------------------------------------------------------ one product
 static int quant_tiles(int n_groups, int n_rows) { return max_row_tiles(MOE_BF16, n_groups, n_rows, INT32_MAX); }
 static size_t quant_plan_size(int n_groups, int n_rows) { return align_up(plan_bytes(n_groups, plan_cap(n_groups, n_rows) + 1), 256); }
@@ -335,8 +357,6 @@ extern "C" int moe_quant_gemm(int32_t n_groups, const int32_t* offsets, int32_t 
 // ---------------------------------------------------------------------------------------- experts
 namespace moe {
 
-extern template void expert_dw_impl<PATH_BF16>(const BwdArgs&, hipStream_t);
-extern template void expert_dw_impl<PATH_BF16_TAIL>(const BwdArgs&, hipStream_t);
 extern template void expert_dw_impl<PATH_BF16_SMALL>(const BwdArgs&, hipStream_t);
 
 // Workspace: plan; codes and exponents of H (forward) or of [dG | dU]; backward: dG and dU in bf16, for the weight gradients.
@@ -523,8 +543,6 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   p.in[0] = G; p.in[1] = U; p.out[0] = dG; p.out[1] = dU; p.ldc = F;
   p.q[0] = Q; p.qs[0] = S; p.q[1] = Q + quant_row(F); p.qs[1] = S + quant_blocks(F);
   p.ldq = mats * quant_row(F); p.lds = mats * quant_blocks(F);
-  if (gated) launch_quant<1, QuantOut<Epi8<1, EPI_SWIGLU_BWD>, 2, true>>("quant_bwd_dh", p, tiles, st);
-  else launch_quant<1, QuantOut<Epi8<1, EPI_GELU_BWD>, 1, true>>("quant_bwd_dh", p, tiles, st);
   QuantGemm q = {};
   q.tiles = pl.tiles; q.n_tiles = pl.n_tiles; q.n_rows = n_rows;
   q.N = d; q.nk = mats * (int)quant_blocks(F);
@@ -532,13 +550,31 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   q.B[0] = (const uint8_t*)W->Wgu; q.Bs[0] = (const uint8_t*)W->Wgu_s;
   q.ldb = q.lda; q.b_group = d * q.ldb; q.lbs = q.nk; q.bs_group = quant_blocks(d) * q.lbs;
   q.out[0] = dXin; q.ldc = d;
-  launch_quant<1, Epi8<1, EPI_STORE>>("quant_bwd_dx", q, tiles, st);
   BwdArgs a = {};
   a.d = d; a.F = F; a.n_groups = n_groups; a.n_rows = n_rows; a.offsets = offsets;
   a.Xin = Xin; a.Wu = gated ? W->Wgu : nullptr; a.G = G; a.U = U; a.H = H; a.dYin = dYin;
   a.dWg = dWg_c; a.dWu = dWu_c; a.dWd = dWd_c; a.ws = (char*)ws; a.dG = dG; a.dU = dU;
-  if (small_tiles(MOE_BF16, n_groups, n_rows, d, F)) expert_dw_impl<PATH_BF16_SMALL>(a, st);
-  else if (d % 64 == 0 && F % 64 == 0) expert_dw_impl<PATH_BF16>(a, st);
-  else expert_dw_impl<PATH_BF16_TAIL>(a, st);
+  typedef QuantOut<Epi8<1, EPI_SWIGLU_BWD>, 2, true> Gated;
+  typedef QuantOut<Epi8<1, EPI_GELU_BWD>, 1, true> Plain;
+  typedef Epi8<1, EPI_STORE> Store;
+  if (small_tiles(MOE_BF16, n_groups, n_rows, d, F)) {  // (two of their weight-gradient blocks fit a compute unit: launches of their own)
+    if (gated) launch_quant<1, Gated>("quant_bwd_dh", p, tiles, st);
+    else launch_quant<1, Plain>("quant_bwd_dh", p, tiles, st);
+    launch_quant<1, Store>("quant_bwd_dx", q, tiles, st);
+    expert_dw_impl<PATH_BF16_SMALL>(a, st);
+    return launch_status(who);
+  }
+  typedef Cores<PATH_BF16> C;  // (the weight gradients of sizes with a K tail run on the same cores)
+  typedef C::core<1, false, false> W1;
+  typedef C::core<2, false, false> W2;
+  const DwGemms g = dw_gemms<PATH_BF16>(a);
+  if (gated) {
+    launch_quant_w<Gated, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, st);
+    launch_quant_w<Store, W2, 2>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, st);
+  } else {
+    launch_quant_w<Plain, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, st);
+    launch_quant_w<Store, W1, 1>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, st);
+  }
+  launch_w_light<C::core_light<1>>("gemm_bwd_dw_light", g.dwd_light, g.dwgu_light, gated ? 2 : 1, st);
   return launch_status(who);
 }
