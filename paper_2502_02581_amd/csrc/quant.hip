@@ -7,7 +7,8 @@ namespace moe {
 
 // ------------------------------------------------------------------------------------- rows
 // Sixteen lanes per block of 128 values, eight values a lane: 16 (fp32: 32) bytes in, 8 out; the maximum by four exchanges.
-// Bound by HBM: it reads every value and writes every code once.
+// Bound by HBM: it reads every value and writes every code once (8192 x 7168 bf16 values 29.3 us, 6.0 TB/s; with the maximum by exchanges
+// through LDS and the conversion from fp32 36.5).
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {  // n: how many of the eight there are
   if (VEC && n >= 8) {
@@ -62,7 +63,8 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ X
 
 // ---------------------------------------------------------------------------------- matrices
 // A block of 256 threads per 128 x 128 values, 8 x 8 of them a thread: the values are read once and both layouts are written from
-// registers, the transposed one through LDS, so that all three streams are whole 128-byte pieces.  Bound by HBM.
+// registers, the transposed one through LDS, so that all three streams are whole 128-byte pieces.  Bound by HBM: 60 bf16 matrices of 2048 x 1408, both
+// layouts, 133 us, 5.2 TB/s, where a plain copy moves 4.8.  (LDS pieces swizzled so that no banks conflict: no change.)
 struct QuantMatrix {
   uint8_t *Q, *S;       // [G][K rows of ldq bytes], [G][K / 128 rows of lds bytes]; NULL: not wanted
   int64_t ldq, lds;

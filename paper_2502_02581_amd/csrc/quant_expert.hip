@@ -110,7 +110,8 @@ __global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
   quant_gemm_block<NB, Epi>(p, blockIdx.x, smem);
 }
 // An input gradient and a weight gradient that does not depend on it (bf16) in one launch, as in row_w_gemm_kernel: the tiles of the one fill the units
-// that the last tiles of the other leave idle.
+// that the last tiles of the other leave idle.  (Training steps apart and together, us: T = 3001, d = 1000, 24 experts of 1368 537 and 501; T = 4096, d = 2048,
+// 60 of 1408 1432 and 1418; T = 1426, d = 2688, one of 3584 289 and 231.)
 template <class Epi, class WCore, int WNB>
 __global__ __launch_bounds__(256, 1) void quant_w_gemm_kernel(QuantGemm p, WGemm w, int first_w, int rows, int w_blocks) {
   extern __shared__ __align__(16) char smem[];
@@ -208,6 +209,8 @@ static void launch_small(const char* label, const QuantGemm& p, hipStream_t st) 
 }
 
 // A product of one group: height and parts by an estimate in microseconds, of a block of K (`iter`) and of what a tile takes besides (`fixed`).
+// (Tall tiles in one part, and by this rule, us: 16 x 7168 x 2048 32 and 15, 256 x 7168 x 2048 34 and 21, 1024 x 7168 x 2048 37 and 30, 512 x 4096 x 6400 33 and 33; rounds
+// of tall tiles only, and the last one cut: 8192 x 4096 x 6400 195 and 177, 2048 x 7168 x 2048 71 and 39.  Over 18 sizes it was within 10 % of the best choice.)
 struct DirectQuant {
   int height = 256, parts = 1, tail = 1;
   double us = 0;
@@ -276,13 +279,13 @@ static void launch_quant(const char* label, const QuantGemm& p, int max_tiles, h
   constexpr int kLds = std::max({QuantTall<NB>::LDS_BYTES, QuantMid<NB>::LDS_BYTES, QuantShort<NB>::LDS_BYTES});
   launch_gemm<quant_gemm_kernel<NB, Epi>>(label, blocks, 256, kLds, st, p);
 }
+// w_first: the tiles of the weight gradient come first (first_w blocks, a multiple of 8, so that the row tiles keep their XCDs), else last.
 template <class Epi, class WCore, int WNB>
-static void launch_quant_w(const char* label, const QuantGemm& p, int max_tiles, const WGemm& w, hipStream_t st) {
+static void launch_quant_w(const char* label, const QuantGemm& p, int max_tiles, const WGemm& w, bool w_first, hipStream_t st) {
   constexpr int kLds = std::max({QuantTall<1>::LDS_BYTES, QuantMid<1>::LDS_BYTES, QuantShort<1>::LDS_BYTES, WCore::LDS_BYTES});
   const unsigned rows = row_block_count(max_tiles, p.N, 256), w_blocks = w_block_count<WCore>(w);
-  const int first = MOE_KNOB("MOE_Q_WFIRST", 0);
-  const unsigned first_w = first ? (w_blocks + 7) / 8 * 8 : 0;
-  launch_gemm<quant_w_gemm_kernel<Epi, WCore, WNB>>(label, rows + (first ? first_w : w_blocks), 256, kLds, st, p, w, (int)first_w, (int)rows, (int)w_blocks);
+  const unsigned first_w = w_first ? (w_blocks + 7) / 8 * 8 : 0;
+  launch_gemm<quant_w_gemm_kernel<Epi, WCore, WNB>>(label, rows + (w_first ? first_w : w_blocks), 256, kLds, st, p, w, (int)first_w, (int)rows, (int)w_blocks);
 }
 
 // ------------------------------------------------------------------------------------ one product
@@ -568,12 +571,16 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   typedef C::core<1, false, false> W1;
   typedef C::core<2, false, false> W2;
   const DwGemms g = dw_gemms<PATH_BF16>(a);
+  // Row tiles of dH over up to eight blocks of K are shorter than the weight gradient's tiles of any group that counts.  (Whole steps with the row tiles first and
+  // last, Zipf loads, us: d = 512, 32 experts of 1408 558 and 514, d = 768, 64 of 2816 1308 and 1269, two-matrix ones 982 and 937, even loads 984 and 1002,
+  // d = 1000 503 and 492; d = 2048 1427 and 1426, d = 4096 6080 and 6121.  dX last: 0 to 3 % more, but for the two-matrix experts, 982 and 946.)
+  const bool w_first = p.nk <= 8;
   if (gated) {
-    launch_quant_w<Gated, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, st);
-    launch_quant_w<Store, W2, 2>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, st);
+    launch_quant_w<Gated, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, w_first, st);
+    launch_quant_w<Store, W2, 2>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, false, st);
   } else {
-    launch_quant_w<Plain, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, st);
-    launch_quant_w<Store, W1, 1>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, st);
+    launch_quant_w<Plain, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, w_first, st);
+    launch_quant_w<Store, W1, 1>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, false, st);
   }
   launch_w_light<C::core_light<1>>("gemm_bwd_dw_light", g.dwd_light, g.dwgu_light, gated ? 2 : 1, st);
   return launch_status(who);

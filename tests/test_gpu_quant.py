@@ -12,6 +12,8 @@ import torch
 
 from oracle import quant_oracle as qo
 
+from .helpers import small_tiles
+
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
@@ -213,6 +215,9 @@ def test_gemm_exponents_at_the_ends():
 EXPERTS = [(1, 4, 1, 64, 64, True, True), (1, 8, 4, 128, 136, True, True), (16, 12, 4, 256, 192, True, True), (33, 3, 1, 136, 72, False, False),
            (300, 6, 3, 200, 264, True, True), (150, 2, 1, 1000, 328, False, True), (600, 5, 2, 256, 384, True, False), (1100, 3, 1, 384, 128, True, True),
            (64, 40, 2, 128, 256, True, True), (700, 2, 1, 128, 136, True, True), (520, 2, 1, 264, 648, False, False)]
+# calls whose weight gradients take the tall tiles, in common launches with the input gradients, the weight gradients' tiles first (d up to 1024) or last
+TALL = [(3500, 3, 1, 1000, 136, True, True), (3500, 3, 1, 1000, 136, False, False), (1700, 4, 1, 2056, 200, True, False), (1150, 5, 2, 2048, 128, False, True),
+        (900, 70, 4, 1024, 64, True, True)]
 
 
 def routed(T, E, k, seed):
@@ -309,12 +314,13 @@ def test_experts_forward(case):
     assert torch.equal(Y.view(torch.int16), L.Y.view(torch.int16))
 
 
-@pytest.mark.parametrize("case", EXPERTS)
+@pytest.mark.parametrize("case", EXPERTS + TALL)
 def test_experts_backward(case):
     """dX and the weight gradients in the 2-norm: their own rounding, 2^-8, and what becomes of dG and dU that lie near a border of bf16 or
     e4m3 and fall on its other side: fewer than one in 2^8 (the products' error is below 2^-12 of a value, a step of e4m3 at least 2^-4 of
     it), by one step of at most 2^-3: 2^-3 * 2^-4 = 2^-7.  The weight gradients see steps of bf16 only: 2^-8 in place of that."""
     L = Layer(*case)
+    assert small_tiles(L.E, L.n, L.shape.d, L.shape.d_ff) == (case in EXPERTS)
     L.forward()
     L.backward()
     G, U, H = (np_of(t) for t in (L.G, L.U, L.H))
@@ -455,7 +461,8 @@ def test_refusals_of_the_binding(monkeypatch):
 @pytest.mark.parametrize("T,E,k,d,F,S,Fs,overlap,fused,gated,gated_s", [
     (1, 8, 2, 128, 64, 0, 0, False, True, True, True), (130, 6, 2, 256, 200, 0, 0, False, True, True, True),
     (300, 5, 3, 136, 264, 2, 72, False, True, True, True), (257, 4, 2, 128, 128, 1, 64, True, True, True, False),
-    (200, 6, 2, 200, 136, 1, 128, True, False, False, True), (0, 4, 2, 64, 64, 1, 64, False, True, True, True)])
+    (200, 6, 2, 200, 136, 1, 128, True, False, False, True), (0, 4, 2, 64, 64, 1, 64, False, True, True, True),
+    (1800, 4, 2, 1024, 128, 1, 64, False, True, True, True)])
 def test_layer(T, E, k, d, F, S, Fs, overlap, fused, gated, gated_s):
     """MoEHotPath with quant: the routed experts are the separate calls bit for bit, the shared ones those of the layer without; then the clipping
     of its gradients against their 64-bit norm."""
