@@ -358,7 +358,9 @@ int moe_combine_bwd(const moe_shape_t* shape, const void* dY, const void* Yp, co
  *   A, As: rows of K values (moe_quant_rows);  B, Bs: [n_groups, N, K] (Qt, St of moe_quant_weights on [n_groups, K, N]), tight rows;
  *   C [n_rows, N] bf16, N a multiple of 8; K and N up to 2^22.  Rows outside the offsets' range are not touched.
  *   Sums are fp32.  The matrix instruction adds products of eight neighbouring values of K after aligning them to the largest, with 13 bits below it;
- *   over normally distributed values that is an error of 1.5e-5 of the result, against 2e-3 of its rounding to bf16.
+ *   over normally distributed values that is an error of 1.5e-5 of the result, against 2e-3 of its rounding to bf16.  Expert calls of n_rows * d_ff up to
+ *   2^16 compute G, U and dH from the bf16 values that the codes stand for instead, in fp32's accuracy: there one code of H, dG or dU that the error moves by a
+ *   step shows in Y and dX.  (Values of 2^128 and more are infinite in such calls, and those below 2^-126 zero.)
  *   ws >= moe_quant_gemm_workspace_bytes(n_groups, n_rows, K, N)
  *
  * moe_quant_expert_fwd / moe_quant_expert_bwd -- moe_expert_fwd / _bwd of routed experts whose products (but those of the weight gradients) run on

@@ -72,7 +72,7 @@ __device__ __forceinline__ void quant_tile(const QuantGemm& p, const RowTile& t,
 // their height).
 template <int NB> using QuantTall = QuantCore<256, NB, 2>;
 template <int NB> using QuantMid = QuantCore<128, NB, 3>;
-template <int NB> using QuantShort = QuantCore<64, NB, 3>;
+template <int NB, bool EXACT = false> using QuantShort = QuantCore<64, NB, 3, EXACT>;
 
 // Tiles are dealt to the XCDs as in row_gemm_block: band by band of kBandRows row tiles, column by column within a band, runs of 32 (launches of
 // few rounds: of 8) consecutive tiles to an XCD.
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, 1) void quant_w_gemm_kernel(QuantGemm p, WGemm
 
 // Calls of few rows (quant_small): tiles of 64 rows, found in the offsets by the blocks themselves, which costs about a microsecond where a plan takes a
 // launch of seven.
-template <int NB, class Epi>
+template <int NB, class Epi, bool EXACT>
 __global__ __launch_bounds__(256, 1) void quant_small_gemm_kernel(QuantGemm p) {
   extern __shared__ __align__(16) char smem[];
   constexpr int BN = 256 / NB, BM = 64;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256, 1) void quant_small_gemm_kernel(QuantGemm p) {
   t.rows = __builtin_amdgcn_readfirstlane(found[2]);
   if (t.rows == 0) return;
   t.row0_out = t.row0_in;
-  quant_tile<QuantShort<NB>, Epi, NB>(p, t, nt, smem);
+  quant_tile<QuantShort<NB, EXACT>, Epi, NB>(p, t, nt, smem);
 }
 
 // One group of n_rows rows: tiles of one height, in parts along K or not; those of a last round that is not full cut into 2 or 4 lower ones.
@@ -202,10 +202,15 @@ __global__ __launch_bounds__(256, 1) void quant_direct_gemm_kernel(QuantGemm p) 
 // 512 46 and 45, 1024 65 and 48, 2048 75 and 70, 4096 100 and 109; products of K = 4096, N = 6400, 4 groups, 512 rows 50 and 40, 1024 59 and 72.
 // Sums in parts, joined by another launch, gain where a call has four rows (K = 2048, N = 1408: 13.8 and 11.6 us) and lose from eight on.)
 static bool quant_small(int n_groups, int n_rows) { return n_rows <= 512 || (n_groups >= 8 && n_rows <= 1024); }
-template <int NB, class Epi>
+// Products whose outputs are quantised, of up to 2^16 values of them: computed from bf16 values, in tiles of 64 rows.  The 8-bit instruction's error, 1.5e-5, moves one
+// in 4000 of the outputs to the other side of a border between codes.  Over many that adds 1e-3 to the 1.7e-3 of the next product's rounding to bf16, but where
+// fewer than some sixteen of them are moved, the error is that of the one which weighs most (0.0056 of a training step's dX, 0.0051 of a forward pass's Y of 2 tokens;
+// from bf16 values 0.0017).  Gate and up of 64 rows, 60 experts of 2048 x 1408, which are more than that: 28 us from bf16 values, 21 on the 8-bit instruction.
+static bool quant_exact(int64_t n_rows, int cols) { return n_rows * cols <= 1 << 16; }
+template <int NB, class Epi, bool EXACT = false>
 static void launch_small(const char* label, const QuantGemm& p, hipStream_t st) {
   const int tiles = p.n_rows / 64 + std::min(p.n_groups, p.n_rows);  // at most
-  launch_gemm<quant_small_gemm_kernel<NB, Epi>>(label, (unsigned)(tiles * ceil_div(p.N, 256 / NB)), 256, QuantShort<NB>::LDS_BYTES, st, p);
+  launch_gemm<quant_small_gemm_kernel<NB, Epi, EXACT>>(label, (unsigned)(tiles * ceil_div(p.N, 256 / NB)), 256, QuantShort<NB, EXACT>::LDS_BYTES, st, p);
 }
 
 // A product of one group: height and parts by an estimate in microseconds, of a block of K (`iter`) and of what a tile takes besides (`fixed`).
@@ -462,7 +467,7 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   if (n_rows == 0) return MOE_OK;
   hipStream_t st = (hipStream_t)stream;
   const int d = shape->d, F = shape->d_ff, tiles = max_row_tiles(MOE_BF16, n_groups, n_rows, d);
-  const bool small = quant_small(n_groups, n_rows);
+  const bool exact = quant_exact(n_rows, F), small = exact || quant_small(n_groups, n_rows);
   const Plan pl = carve_plan(plan ? (void*)plan : ws, n_groups, plan_cap(n_groups, n_rows));
   if (!plan && !small) launch_plan(offsets, n_groups, 256, pl, nullptr, nullptr, st);
   uint8_t *HQ = (uint8_t*)ws + sp.plan, *HS = HQ + sp.codes;
@@ -478,7 +483,8 @@ extern "C" int moe_quant_expert_fwd(const moe_shape_t* shape, int32_t n_groups, 
   typedef Epi8<2, EPI_SWIGLU_FWD> Gated;
   typedef Epi8<1, EPI_GELU_FWD> Plain;
   auto gate_up = [&](auto nb, auto epi) {
-    if (small) launch_small<decltype(nb)::value, decltype(epi)>("quant_fwd_gate_up", p, st);
+    if (exact) launch_small<decltype(nb)::value, decltype(epi), true>("quant_fwd_gate_up", p, st);
+    else if (small) launch_small<decltype(nb)::value, decltype(epi)>("quant_fwd_gate_up", p, st);
     else launch_quant<decltype(nb)::value, decltype(epi)>("quant_fwd_gate_up", p, tiles, st);
   };
   const std::integral_constant<int, 1> one;
@@ -537,7 +543,7 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   uint8_t *Q = (uint8_t*)dU + sp.act, *S = Q + sp.codes;  // a row of [dG | dU]
   const int mats = gated ? 2 : 1;
   QuantGemm p = {};
-  p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.n_rows = n_rows;
+  p.tiles = pl.tiles; p.n_tiles = pl.n_tiles; p.offsets = offsets; p.n_rows = n_rows; p.n_groups = n_groups;
   p.N = F; p.nk = (int)quant_blocks(d);
   p.A = (const uint8_t*)dYQ; p.As = (const uint8_t*)dYS; p.lda = quant_row(d); p.las = p.nk;
   p.a_index = src_of; p.a_index_div = shape->k; p.a_src_rows = shape->T; p.c_scale = row_w;
@@ -560,9 +566,14 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   typedef QuantOut<Epi8<1, EPI_SWIGLU_BWD>, 2, true> Gated;
   typedef QuantOut<Epi8<1, EPI_GELU_BWD>, 1, true> Plain;
   typedef Epi8<1, EPI_STORE> Store;
+  const bool exact = quant_exact(n_rows, F);
+  if (exact) {
+    if (gated) launch_small<1, Gated, true>("quant_bwd_dh", p, st);
+    else launch_small<1, Plain, true>("quant_bwd_dh", p, st);
+  }
   if (small_tiles(MOE_BF16, n_groups, n_rows, d, F)) {  // (two of their weight-gradient blocks fit a compute unit: launches of their own)
-    if (gated) launch_quant<1, Gated>("quant_bwd_dh", p, tiles, st);
-    else launch_quant<1, Plain>("quant_bwd_dh", p, tiles, st);
+    if (!exact && gated) launch_quant<1, Gated>("quant_bwd_dh", p, tiles, st);
+    if (!exact && !gated) launch_quant<1, Plain>("quant_bwd_dh", p, tiles, st);
     launch_quant<1, Store>("quant_bwd_dx", q, tiles, st);
     expert_dw_impl<PATH_BF16_SMALL>(a, st);
     return launch_status(who);
@@ -575,11 +586,12 @@ extern "C" int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, 
   // last, Zipf loads, us: d = 512, 32 experts of 1408 558 and 514, d = 768, 64 of 2816 1308 and 1269, two-matrix ones 982 and 937, even loads 984 and 1002,
   // d = 1000 503 and 492; d = 2048 1427 and 1426, d = 4096 6080 and 6121.  dX last: 0 to 3 % more, but for the two-matrix experts, 982 and 946.)
   const bool w_first = p.nk <= 8;
+  const int dh_tiles = exact ? 0 : tiles;  // (computed above)
   if (gated) {
-    launch_quant_w<Gated, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, w_first, st);
+    launch_quant_w<Gated, W1, 1>("quant_bwd_dh_dwd", p, dh_tiles, g.dwd, w_first, st);
     launch_quant_w<Store, W2, 2>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, false, st);
   } else {
-    launch_quant_w<Plain, W1, 1>("quant_bwd_dh_dwd", p, tiles, g.dwd, w_first, st);
+    launch_quant_w<Plain, W1, 1>("quant_bwd_dh_dwd", p, dh_tiles, g.dwd, w_first, st);
     launch_quant_w<Store, W1, 1>("quant_bwd_dx_dwgu", q, tiles, g.dwgu, false, st);
   }
   launch_w_light<C::core_light<1>>("gemm_bwd_dw_light", g.dwd_light, g.dwgu_light, gated ? 2 : 1, st);

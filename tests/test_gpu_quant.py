@@ -214,7 +214,8 @@ def test_gemm_exponents_at_the_ends():
 # T, E, k, d, d_ff, gated, rows read in place
 EXPERTS = [(1, 4, 1, 64, 64, True, True), (1, 8, 4, 128, 136, True, True), (16, 12, 4, 256, 192, True, True), (33, 3, 1, 136, 72, False, False),
            (300, 6, 3, 200, 264, True, True), (150, 2, 1, 1000, 328, False, True), (600, 5, 2, 256, 384, True, False), (1100, 3, 1, 384, 128, True, True),
-           (64, 40, 2, 128, 256, True, True), (700, 2, 1, 128, 136, True, True), (520, 2, 1, 264, 648, False, False)]
+           (64, 40, 2, 128, 256, True, True), (700, 2, 1, 128, 136, True, True), (520, 2, 1, 264, 648, False, False),
+           (100, 12, 4, 264, 392, True, True), (200, 9, 2, 136, 200, False, True)]
 # calls whose weight gradients take the tall tiles, in common launches with the input gradients, the weight gradients' tiles first (d up to 1024) or last
 TALL = [(3500, 3, 1, 1000, 136, True, True), (3500, 3, 1, 1000, 136, False, False), (1700, 4, 1, 2056, 200, True, False), (1150, 5, 2, 2048, 128, False, True),
         (900, 70, 4, 1024, 64, True, True)]
@@ -375,6 +376,51 @@ def test_gradient_against_differences():
     h = 1e-4 / np.abs(dX).max()
     diff = (loss(L.xv + h * dX) - loss(L.xv - h * dX)) / (2 * h)
     assert abs(diff - (dX * dX).sum()) <= 3 * 2.0 ** -4 * (dX * dX).sum()
+
+
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("T,E,k,d,F", [(1, 1, 1, 256, 136), (3, 2, 1, 1000, 64), (20, 1, 1, 264, 200), (50, 1, 1, 136, 136), (90, 2, 2, 256, 256)])
+def test_few_values_are_computed_without_alignment(T, E, k, d, F, gated):
+    """What is quantised behind a product of up to 2^16 values: every row and column holds two products of 448^2 that cancel, the other ones are 1, 0 or -1.
+    All partial sums are whole numbers below 2^24, and what is left, of K products of variance 4/9, one of up to 256: exact in fp32 and in bf16.  An
+    instruction that drops what lies 13 bits below the largest of eight products loses it.  g = 32, whose sigmoid is 1 in fp32, scales dU by 32."""
+    L = Layer(T, E, k, d, F, gated, True)
+    assert L.n * F <= 1 << 16
+    g = torch.Generator().manual_seed(T + d)
+    small = lambda *s: torch.randint(-1, 2, s, generator=g).float()
+    x, dy, wg, wd = small(T, d), small(T, d), small(E, d, F), small(E, F, d)
+    for t, at, sign in ((x, 5, 1), (dy, 17, 1)):
+        t[:, at], t[:, at + 1] = 448, 448 * sign
+    wg[:, 5], wg[:, 6] = 448, -448
+    wd[:, :, 17], wd[:, :, 18] = 448, -448
+    to = lambda t: t.to(torch.bfloat16).to(DEV)
+    L.X, L.dY, L.row_w = to(x), to(dy), torch.ones(T, k, device=DEV)
+    L.weights.update(to(wg), to(wg) if gated else None, to(wd))
+    moe().moe_quant_rows(L.X, *L.xq)
+    moe().moe_quant_rows(L.dY, *L.dyq)
+    token = L.src_np // k
+    G = qo.grouped(np_of(x)[token], L.bounds, [np_of(w) for w in wg])
+    dH = qo.grouped(np_of(dy)[token], L.bounds, [np.ascontiguousarray(np_of(w).T) for w in wd])
+    assert max(np.abs(G).max(), np.abs(dH).max()) <= 256
+    L.forward()
+    assert np.array_equal(np_of(L.G), G)
+    if gated:
+        assert np.array_equal(np_of(L.U), G)
+    # the gradient of each row by itself: the weight gradient of an operand that has a one in a column of that row's own
+    L.G.fill_(32)
+    if gated:
+        L.U.zero_()
+    L.Xp = torch.zeros(L.n, d, dtype=torch.bfloat16, device=DEV)
+    L.Xp[torch.arange(L.n), torch.arange(L.n) % d] = 1
+    assert L.n <= d
+    L.backward()
+    got, scale = (L.dW[1], 32) if gated else (L.dW[0], 1)   # (gelu'(32) is 1)
+    slot = 0
+    for e in range(E):
+        a, b = L.bounds[e], L.bounds[e + 1]
+        if b > a:
+            assert np.array_equal(np_of(got[slot])[a:b], scale * dH[a:b])
+            slot += 1
 
 
 def test_experts_without_rows():
