@@ -742,6 +742,9 @@ def _grad_list(grads, out=None, written=False):
         outs = [o for o, n in zip(members[1::6], members[2::6]) if n]
         if len(set(outs)) != len(outs):
             raise MoEError("a tensor is there twice")
+        ins = {g: i for i, (g, n) in enumerate(zip(members[::6], members[2::6])) if n} if out is not None else {}
+        if any(ins.get(o, i) != i for i, (o, n) in enumerate(zip(members[1::6], members[2::6])) if n):
+            raise MoEError("an output is another gradient")
     if not members:
         return (_CGrad * 1)()
     return (_CGrad * len(grads)).from_buffer(bytearray(struct.pack(f"={len(members)}q", *members)))

@@ -142,3 +142,14 @@ def test_refusals():
         m.moe_grad_norm([(x[0], torch.ones(1, dtype=torch.int32, device=DEV))], norm, torch.empty(1 << 14, dtype=torch.uint8, device=DEV))
     with pytest.raises(m.MoEError, match="GPU"):
         m.moe_grad_norm([torch.ones(3)], norm, ws)
+
+
+def test_clip_refuses_an_output_that_is_another_gradient():
+    m = moe()
+    x, y, norm = torch.ones(8, device=DEV), torch.ones(8, device=DEV), torch.ones(1, device=DEV)
+    with pytest.raises(m.MoEError, match="another gradient"):
+        m.moe_grad_clip([x, y], norm, 0.5, [y, torch.empty_like(x)])
+    with pytest.raises(m.MoEError, match="another gradient"):
+        m.moe_grad_clip([x, y], norm, 0.5, [y, x])
+    m.moe_grad_clip([x, y], norm, 0.5, [x, torch.empty_like(y)])   # the first in place, the second not
+    assert abs(float(x[0]) - 0.5) <= 1e-6 and float(y[0]) == 1.0   # (0.5 / (1 + 1e-6))
