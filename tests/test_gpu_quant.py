@@ -607,3 +607,52 @@ def test_layer_refuses_fp32():
     m = moe()
     with pytest.raises(m.MoEError, match="bf16"):
         m.MoEHotPath(m.MoEShape(8, 64, 4, 2, 64, "f32"), quant=True)
+
+
+@pytest.mark.parametrize("case", [(60, 3, 2, 256, 136, True, False), (100, 12, 4, 264, 392, True, False), (600, 5, 2, 256, 384, False, False),
+                                  (1700, 4, 1, 2056, 200, True, False)])
+@pytest.mark.parametrize("graph", [False, True])
+def test_rows_of_no_group(case, graph):
+    """Rows ahead of the first and behind the last group, of NaN codes, exponents of 255 and NaN: their outputs stay as they were, and nothing of them
+    reaches another row or a weight gradient, whichever tiles the call takes; eager and in a graph."""
+    L = Layer(*case)
+    off = L.bounds.copy()
+    off[:] = np.clip(off, 5, L.n - 37)
+    L.off = torch.from_numpy(off).to(DEV)
+
+    def run():
+        L.forward()
+        L.backward()
+
+    outs = [L.G, L.H, L.Y, L.dX] + ([L.U] if L.gated else [])
+    grads = [t for t in L.dW if t is not None]
+    run()
+    inside = slice(5, L.n - 37)
+    n = int(L.n_active.item())
+    ref = [t[inside].clone() for t in outs] + [t[:n].clone() for t in grads]
+    for rows in (slice(0, 5), slice(L.n - 37, L.n)):
+        for t in (*L.xq, *L.dyq):
+            t[rows] = 255
+        for t in (L.Xp, L.dYp):
+            t[rows] = float("nan")
+        for t in outs:
+            t[rows] = 7
+    L.ws.fill_(255)
+    for t in grads:
+        t.fill_(7)
+    if graph:
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            run()
+    for _ in range(3 if graph else 1):
+        for t in outs:
+            t[inside] = 0 if t is L.Y or t is L.dX else t[inside]
+        g.replay() if graph else run()
+        torch.cuda.synchronize()
+        got = [t[inside] for t in outs] + [t[:n] for t in grads]
+        assert int(L.n_active.item()) == n and all(bool(torch.isfinite(t.float()).all()) for t in got)
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(got, ref))
+        for t in outs:
+            assert bool((t[:5] == 7).all()) and bool((t[L.n - 37:] == 7).all())
+        assert all(bool((t[n:] == 7).all()) for t in grads)
