@@ -84,7 +84,7 @@ __device__ __forceinline__ void static_for(F f) {
 // copied out one by one.
 // ROWS: rows of a block.  MT: rows of a tile, one per lane % MT; its columns are four for every lane of a row, lane / MT by lane / MT.
 // AHEAD: the next block's inputs are loaded under a block's arithmetic (two blocks per CU have no registers for them).
-// Epilogues with a member `quantises` (see quant_core.h) also get every finished piece of a row, by quantise<output>(piece, row, first column); where
+// Epilogues with a member `quantises` (see quant_core.h) also get the finished pieces of rows, by quantise<output, number>(pieces, first row, rows between two, first column); where
 // their STORES is false the pieces are not written themselves.
 template <class Epi, class = void> struct Quantises : std::false_type {
   static constexpr bool stores = true;
@@ -160,8 +160,7 @@ struct TileEpilogue {
       }
       if constexpr (Quantises<Epi>::value) {
         static_for<NOUT>([&](auto x) __attribute__((always_inline)) {
-#pragma unroll
-          for (int p = 0; p < NPASS; p++) epi.template quantise<decltype(x)::value>(r[decltype(x)::value][p], wm0 + i * ROWS + p * RPP + rrow, c0);
+          epi.template quantise<decltype(x)::value, NPASS>(r[decltype(x)::value], wm0 + i * ROWS + rrow, RPP, c0);
         });
       }
     };

@@ -37,21 +37,26 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ X
     uint2 codes;
     int e;
     if constexpr (VEC && sizeof(T) == 2) {
-      uint32_t v[4] = {0, 0, 0, 0};
+      uint32_t v[1][4] = {};
       if (c0 + 8 <= (uint32_t)cols) {
         const uint4 t = *reinterpret_cast<const uint4*>(x);
-        v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+        v[0][0] = t.x; v[0][1] = t.y; v[0][2] = t.z; v[0][3] = t.w;
       } else {
-        for (int i = 0; i < cols - (int)c0; i++) v[i / 2] |= (uint32_t)x[i] << (16 * (i % 2));
+        for (int i = 0; i < cols - (int)c0; i++) v[0][i / 2] |= (uint32_t)x[i] << (16 * (i % 2));
       }
-      e = quant_block_bf16(v, 0xffffffffu, codes);
+      uint2 c[1];
+      int b1[1];
+      quant_blocks_bf16(v, 0xffffffffu, c, b1);
+      codes = c[0];
+      e = b1[0];
     } else {
       float v[8];
       load8<T, VEC>(x, cols - (int)c0, v);
-      uint32_t m = 0;
+      int m[1] = {0};
 #pragma unroll
-      for (int i = 0; i < 8; i++) m = max(m, finite_bits(v[i]));
-      e = quant_exponent((uint32_t)row_max16((int)m));
+      for (int i = 0; i < 8; i++) m[0] = max(m[0], (int)finite_bits(v[i]));
+      row_max16(m);
+      e = quant_exponent((uint32_t)m[0]);
       const float f = quant_factor(e);
       const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
       codes = make_uint2(quant_codes(lo, f), quant_codes(hi, f));

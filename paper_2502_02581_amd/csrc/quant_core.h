@@ -20,20 +20,30 @@ struct QuantOut : E {
   // Rows and columns that do not exist are dropped by the descriptors' bounds: the offsets of lanes whose column is beyond the row of codes, and for exponents of
   // all but one lane of a row, start at 2 GiB (256 rows of codes take less).
   static constexpr uint32_t kDrop = 0x80000000u;
-  template <int x>
-  __device__ __forceinline__ void quantise(const u32x4_t& piece, int row, int col) const {
+  // pieces of rows row, row + step, ..
+  template <int x, int N>
+  __device__ __forceinline__ void quantise(const u32x4_t (&piece)[N], int row, int step, int col) const {
     if constexpr (x >= E::NOUT - NQ) {
       constexpr int n = x - (E::NOUT - NQ);
       // (beyond the last column there may be what other rows' NaN left)
-      const uint32_t v[4] = {piece[0], piece[1], piece[2], piece[3]};
-      uint2 c;
-      const int e = quant_block_bf16(v, col < E::n_valid ? 0xffffffffu : 0u, c);
+      uint32_t v[N][4];
+#pragma unroll
+      for (int p = 0; p < N; p++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[p][i] = piece[p][i];
+      uint2 c[N];
+      int e[N];
+      quant_blocks_bf16(v, col < E::n_valid ? 0xffffffffu : 0u, c, e);
       const uint32_t at = col < q_valid ? (uint32_t)col : kDrop;
       const uint32_t at_s = col < q_valid && (col & (kQuantBlock - 1)) == 0 ? (uint32_t)col / kQuantBlock : kDrop;
       typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
       const uint32_t last = (uint32_t)E::rows - 1;
-      __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{c.x, c.y}, make_rsrc(q[n], last * ldq + (uint32_t)q_valid), at + (uint32_t)row * ldq, 0, 0);
-      __builtin_amdgcn_raw_buffer_store_b8((uint8_t)e, make_rsrc(s[n], last * lds + (uint32_t)q_valid / kQuantBlock), at_s + (uint32_t)row * lds, 0, 0);
+#pragma unroll
+      for (int p = 0; p < N; p++) {
+        const uint32_t r = (uint32_t)(row + p * step);
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{c[p].x, c[p].y}, make_rsrc(q[n], last * ldq + (uint32_t)q_valid), at + r * ldq, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b8((uint8_t)e[p], make_rsrc(s[n], last * lds + (uint32_t)q_valid / kQuantBlock), at_s + r * lds, 0, 0);
+      }
     }
   }
 };

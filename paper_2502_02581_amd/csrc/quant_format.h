@@ -24,7 +24,7 @@ __device__ __forceinline__ uint32_t finite_bits(float x) {
 // (448 = 1.75 * 2^8), e at least -126 (2^-e is then a normal number, too); e = 0 for a block of zeros.
 __device__ __forceinline__ int quant_exponent(uint32_t maximum) {
   if (maximum == 0) return 127;
-  return max((int)(maximum >> 23) - 8 + ((maximum & 0x7fffffu) > 0x600000u), 1);
+  return max((int)((maximum + 0x1fffffu) >> 23) - 8, 1);  // (a mantissa above 0.75 carries into the exponent)
 }
 __device__ __forceinline__ float quant_factor(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }  // 2^-e
 // Four codes: nearest, ties to even, subnormal codes included; the scaled values are at most 448, so none saturates.  The conversion makes NaN codes of
@@ -33,38 +33,55 @@ __device__ __forceinline__ uint32_t quant_codes(const float (&x)[4], float f) {
   const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, w, true);
 }
-// maximum over the sixteen lanes of a row, in all of them (in-register rotations: exchanges through LDS cost 46 us of a 124 us launch whose
-// epilogue quantises two outputs)
-__device__ __forceinline__ int row_max16(int v) {
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, false));
-  return max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false));
+// maxima over the sixteen lanes of a row, in all of them (in-register rotations: exchanges through LDS cost 46 us of a 124 us launch whose
+// epilogue quantises two outputs; several at a time, because a rotation may read what was written only two instructions later)
+template <int ROTATE, int N>
+__device__ __forceinline__ void rotate_max(int (&v)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; n++) v[n] = max(v[n], __builtin_amdgcn_update_dpp(0, v[n], 0x120 + ROTATE, 0xf, 0xf, false));
 }
-// A block of 128 bf16 values, eight in each of sixteen lanes: the lane's codes and the block's exponent byte.  With 0x80 added to their magnitudes
+template <int N>
+__device__ __forceinline__ void row_max16(int (&v)[N]) {
+  rotate_max<8>(v);
+  rotate_max<4>(v);
+  rotate_max<2>(v);
+  rotate_max<1>(v);
+}
+// Blocks of 128 bf16 values, eight of each in each of sixteen lanes: the lane's codes and the blocks' exponent bytes.  With 0x80 added to their magnitudes
 // infinities and NaN are negative 16-bit numbers and lose against every finite value.  `there`: 0xffffffff, or 0 in lanes whose values are not part of
-// the block (codes of zero).
-__device__ __forceinline__ int quant_block_bf16(const uint32_t (&v)[4], uint32_t there, uint2& codes) {
+// the blocks (codes of zero).
+template <int N>
+__device__ __forceinline__ void quant_blocks_bf16(const uint32_t (&v)[N][4], uint32_t there, uint2 (&codes)[N], int (&e)[N]) {
   typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
   typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
   typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-  i16x2_t m = {0x80, 0x80};
+  i16x2_t m[N];
   const uint32_t magnitude = 0x7fff7fffu & there;
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const u16x2_t t = __builtin_bit_cast(u16x2_t, v[i] & magnitude) + u16x2_t{0x80, 0x80};
-    m = __builtin_elementwise_max(m, __builtin_bit_cast(i16x2_t, t));
-  }
-  const int e = quant_exponent((uint32_t)(row_max16(max((int)m[0], (int)m[1])) - 0x80) << 16);
-  const float scale = __uint_as_float((uint32_t)e << 23);  // 2^e: the conversion divides by it
-  i16x2_t c[2] = {};
+  for (int n = 0; n < N; n++) m[n] = i16x2_t{0x80, 0x80};
 #pragma unroll
-  for (int i = 0; i < 2; i++) {
-    c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[2 * i]), scale, false);
-    c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[2 * i + 1]), scale, true);
+  for (int i = 0; i < 4; i++)
+#pragma unroll
+    for (int n = 0; n < N; n++) {
+      const u16x2_t t = __builtin_bit_cast(u16x2_t, v[n][i] & magnitude) + u16x2_t{0x80, 0x80};
+      m[n] = __builtin_elementwise_max(m[n], __builtin_bit_cast(i16x2_t, t));
+    }
+  int a[N];
+#pragma unroll
+  for (int n = 0; n < N; n++) a[n] = max((int)m[n][0], (int)m[n][1]);
+  row_max16(a);
+#pragma unroll
+  for (int n = 0; n < N; n++) {
+    e[n] = quant_exponent((uint32_t)(a[n] - 0x80) << 16);
+    const float scale = __uint_as_float((uint32_t)e[n] << 23);  // 2^e: the conversion divides by it
+    i16x2_t c[2] = {};
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[n][2 * i]), scale, false);
+      c[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i], __builtin_bit_cast(bf16x2_t, v[n][2 * i + 1]), scale, true);
+    }
+    codes[n] = make_uint2(__builtin_bit_cast(uint32_t, c[0]) & there, __builtin_bit_cast(uint32_t, c[1]) & there);
   }
-  codes = make_uint2(__builtin_bit_cast(uint32_t, c[0]) & there, __builtin_bit_cast(uint32_t, c[1]) & there);
-  return e;
 }
 
 }  // namespace moe
