@@ -206,8 +206,8 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, what="tensor"):
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # (the handle without a Stream object around it: 0.4 us of a call on the host, 2.9 with it)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 

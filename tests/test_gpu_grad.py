@@ -153,3 +153,18 @@ def test_clip_refuses_an_output_that_is_another_gradient():
         m.moe_grad_clip([x, y], norm, 0.5, [y, x])
     m.moe_grad_clip([x, y], norm, 0.5, [x, torch.empty_like(y)])   # the first in place, the second not
     assert abs(float(x[0]) - 0.5) <= 1e-6 and float(y[0]) == 1.0   # (0.5 / (1 + 1e-6))
+
+
+def test_calls_go_to_the_current_stream():
+    from paper_2502_02581_amd.binding import _stream
+
+    side = torch.cuda.Stream()
+    assert _stream(None) == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(side):
+        assert _stream(None) == side.cuda_stream == _stream(side)
+    graph = torch.cuda.CUDAGraph()
+    x = torch.zeros(8, device=DEV)
+    with torch.cuda.graph(graph):
+        assert _stream(None) == torch.cuda.current_stream().cuda_stream
+        x.add_(1)
+    torch.cuda.synchronize()
