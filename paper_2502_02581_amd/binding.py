@@ -841,6 +841,7 @@ class MoEHotPath:
         self.aux_alpha = float(aux_alpha)
         self.overlap = bool(overlap_shared and n_shared)
         self.quant = bool(quant)
+        self._gated = None   # whether the last backward pass had gated experts: (routed, shared)
         if self.quant and shape.dtype != "bf16":
             raise MoEError("quant goes with bf16 layers")
         s, dt, dev = shape, shape.torch_dtype, self.device
@@ -1002,11 +1003,21 @@ class MoEHotPath:
             moe_route_bwd(s, self._logits, b["topk_idx"], b["dw"], b["dlogits"], stream)
             if self.aux_alpha > 0:
                 moe_aux_loss_bwd(s, self._logits, b["counts"], self.aux_alpha, 1.0, True, b["dlogits"], stream)
+        self._gated = (Wg.gated if self.quant else Wu is not None, Wsu is not None)
         return b["dX"]
 
-    def gradients(self, gated: bool = True, gated_shared: bool = True):
-        """The weight gradients of the last backward pass, as moe_grad_norm and moe_grad_clip take them."""
+    def gradients(self, gated: Optional[bool] = None, gated_shared: Optional[bool] = None):
+        """The weight gradients of the last backward pass, as moe_grad_norm and moe_grad_clip take them.  That pass says which experts were gated: two-matrix
+        ones have no dWu, and what its buffer holds is not part of the list.  Before the first pass both arguments have to say it; later ones must agree
+        with the pass."""
         b = self.b
+        known = self._gated or (None, None)
+        wanted = [w if k is None else k for w, k in zip((gated, gated_shared if self.S else False), known)]
+        if None in wanted:
+            raise MoEError("gradients: there was no backward pass yet that says whether the experts are gated")
+        if gated not in (None, wanted[0]) or (self.S and gated_shared not in (None, wanted[1])):
+            raise MoEError("gradients: gated does not agree with the experts of the last backward pass")
+        gated, gated_shared = wanted
         names = ["dWg_c"] + (["dWu_c"] if gated else []) + ["dWd_c"]
         shared = (["dWsg"] + (["dWsu"] if gated_shared else []) + ["dWsd"]) if self.S else []
         return [(b[n], b["n_active"]) for n in names] + [b[n] for n in shared]
