@@ -519,10 +519,13 @@ def _sized(t, shape, what, dtype=torch.uint8):
     return _ptr(t, dtype, what)
 
 
-def _here(t, who):
-    """Refuses tensors of another GPU than the current one, on which the call would launch."""
-    if t.device.index != torch.cuda.current_device():
-        raise MoEError(f"{who}: the tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+def _here(who, *tensors):
+    """Refuses tensors of another GPU than the current one, on which the call would launch.  (What is not on a GPU at all is refused where its
+    pointer is taken.)"""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device and t.is_cuda:
+            raise MoEError(f"{who}: a tensor is on {t.device}, the current device is cuda:{device}")
 
 
 def _pitched(t, shape, what):
@@ -560,7 +563,7 @@ def moe_quant_rows(X, Q, S, stream=None):
     ldx = max(X.stride(0), cols) if n > 1 else cols
     if n > 1 and X.stride(0) < cols:
         raise MoEError("X: rows must not overlap")
-    _here(X, "moe_quant_rows")
+    _here("moe_quant_rows", X, Q, S)
     rc = load_library().moe_quant_rows(X.data_ptr(), dt, n, cols, ldx, _sized(Q, (n, moe_quant_row_bytes(cols)), "Q"),
                                        _sized(S, (n, moe_quant_scale_bytes(cols)), "S"), _stream(stream))
     _check(rc, "moe_quant_rows")
@@ -576,7 +579,7 @@ def moe_quant_weights(W, Q, S, Qt, St, stream=None):
     b = moe_quant_scale_bytes
     args = []
     _ptr(W, None, "W")
-    _here(W, "moe_quant_weights")
+    _here("moe_quant_weights", W, Q, S, Qt, St)
     for t, shape, what in ((Q, (g, K, moe_quant_row_bytes(N)), "Q"), (S, (g, b(K), b(N)), "S"),
                            (Qt, (g, N, moe_quant_row_bytes(K)), "Qt"), (St, (g, b(N), b(K)), "St")):
         args += _pitched(t, shape, what)
@@ -594,7 +597,7 @@ def moe_quant_gemm(offsets, K: int, A, As, B, Bs, C, ws, stream=None):
         raise MoEError("C must be [n_rows, N], B [groups, N, .]")
     (n, N), g = C.shape, B.shape[0]
     kb, rb = moe_quant_scale_bytes(K), moe_quant_row_bytes(K)
-    _here(C, "moe_quant_gemm")
+    _here("moe_quant_gemm", offsets, A, As, B, Bs, C, ws)
     if offsets is not None:
         _sized(offsets, (g + 1,), "offsets", torch.int32)
     rc = load_library().moe_quant_gemm(g, _ptr(offsets, torch.int32, "offsets"), n, K, N, _sized(A, (n, rb), "A"), _sized(As, (n, kb), "As"),
@@ -662,6 +665,9 @@ class MoEQuantWeights:
         mats = 2 if self.gated else 1
         self.c = _CQuantWeights(*ptrs(self.WgT, F, d, 1, "WgT"), *ptrs(self.WuT, F, d, 1, "WuT"), *ptrs(self.WdT, d, F, 1, "WdT"),
                                 *ptrs(self.Wgu, d, F, mats, "Wgu"), *ptrs(self.Wd, F, d, 1, "Wd"), int(self.gated))
+        devices = sorted({t.get_device() for pair in (self.WgT, self.WuT, self.WdT, self.Wgu, self.Wd) if pair is not None for t in pair})
+        if len(devices) > 1:
+            raise MoEError(f"the matrices must be on one device, not on {devices}")
 
 
 def moe_quant_expert_fwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int) -> int:
@@ -672,18 +678,18 @@ def moe_quant_expert_bwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows:
     return int(load_library().moe_quant_expert_bwd_workspace_bytes(ctypes.byref(shape.c()), n_groups, n_rows))
 
 
-def _quant_args(shape, n_groups, n_rows, src_of, Q, S, W, who):
+def _quant_args(shape, n_groups, n_rows, src_of, Q, S, W, who, *others):
+    _here(who, src_of, Q, S, W.WgT[0], *others)
     if W.n_groups != n_groups or (W.shape.d, W.shape.d_ff) != (shape.d, shape.d_ff):
         raise MoEError(f"{who}: the weights are those of {W.n_groups} experts of d={W.shape.d}, d_ff={W.shape.d_ff}")
     rows = n_rows if src_of is None else shape.T
-    _here(Q, who)
     return (_sized(Q, (rows, moe_quant_row_bytes(shape.d)), "codes"), _sized(S, (rows, moe_quant_scale_bytes(shape.d)), "exponents"))
 
 
 def moe_quant_expert_fwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, XQ, XS, W: MoEQuantWeights, G, U, H, Yout, ws, plan=None, stream=None):
     """Forward pass of routed experts on block-scaled operands; G, U and H None where no backward pass follows."""
     bf = torch.bfloat16
-    q = _quant_args(shape, n_groups, n_rows, src_of, XQ, XS, W, "moe_quant_expert_fwd")
+    q = _quant_args(shape, n_groups, n_rows, src_of, XQ, XS, W, "moe_quant_expert_fwd", offsets, G, U, H, Yout, plan, ws)
     rc = load_library().moe_quant_expert_fwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, torch.int32, "offsets"), n_rows, _ptr(src_of, torch.int32, "src_of"), *q,
         ctypes.byref(W.c), _ptr(G, bf, "G"), _ptr(U, bf, "U"), _ptr(H, bf, "H"), _ptr(Yout, bf, "Yout"),
@@ -697,7 +703,8 @@ def moe_quant_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, row
     bf, i32 = torch.bfloat16, torch.int32
     if W.Wgu is None:
         raise MoEError("moe_quant_expert_bwd: these weights have no layouts of the backward pass")
-    q = _quant_args(shape, n_groups, n_rows, src_of, dYQ, dYS, W, "moe_quant_expert_bwd")
+    q = _quant_args(shape, n_groups, n_rows, src_of, dYQ, dYS, W, "moe_quant_expert_bwd", offsets, row_w, Xin, G, U, H, dYin, dXin, active_ids,
+                    n_active, dWg_c, dWu_c, dWd_c, ws)
     rc = load_library().moe_quant_expert_bwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, i32, "offsets"), n_rows, _ptr(src_of, i32, "src_of"),
         _ptr(row_w, torch.float32, "row_w"), *q, _ptr(Xin, bf, "Xin"), ctypes.byref(W.c), _ptr(G, bf, "G"),
@@ -714,6 +721,7 @@ def _grad_list(grads, out=None, written=False):
     if out is not None and len(out) != len(grads):
         raise MoEError(f"{len(grads)} gradients, {len(out)} outputs")
     members, counters = [], {}   # (a counter serves the tensors of a layer: looked at once)
+    device = torch.cuda.current_device()
     for i, x in enumerate(grads):
         n_active, slot = None, 1
         if not isinstance(x, torch.Tensor):
@@ -721,20 +729,23 @@ def _grad_list(grads, out=None, written=False):
         dt = x.dtype
         if not (dt is torch.float32 or dt is torch.bfloat16):
             raise MoEError(f"gradient {i} must be float32 or bfloat16, got {dt}")
-        if not x.is_cuda or not x.is_contiguous():
-            raise MoEError(f"gradient {i} must live on the GPU and be contiguous")
+        if x.get_device() != device or not x.is_contiguous():
+            raise MoEError(f"gradient {i} must live on the GPU and be contiguous; it is on {x.device}, the current device is cuda:{device}")
         g = o = x.data_ptr()
         n = x.numel()
         if out is not None:
             y = out[i]
-            if y.dtype is not dt or y.shape != x.shape or not y.is_cuda or not y.is_contiguous():
-                raise MoEError(f"output {i} must be a contiguous {dt} tensor on the GPU of shape {tuple(x.shape)}")
+            if y.dtype is not dt or y.shape != x.shape or y.get_device() != device or not y.is_contiguous():
+                raise MoEError(f"output {i} must be a contiguous {dt} tensor on the GPU of shape {tuple(x.shape)}; it is on {y.device}, the current "
+                               f"device is cuda:{device}")
             o = y.data_ptr()
         if n_active is not None:
             if x.dim() == 0:
                 raise MoEError(f"gradient {i} must be [slots, ...]")
             slot = n // x.shape[0] if n else 1
             if id(n_active) not in counters:
+                if n_active.get_device() != device:
+                    raise MoEError(f"n_active of gradient {i} must live on the GPU; it is on {n_active.device}, the current device is cuda:{device}")
                 counters[id(n_active)] = _ptr(n_active, torch.int32, "n_active")
             n_active = counters[id(n_active)]
         members += (g, o, n, n_active or 0, slot, MOE_F32 if dt is torch.float32 else MOE_BF16)
@@ -757,7 +768,7 @@ def moe_grad_norm_workspace_bytes() -> int:
 def moe_grad_norm(grads, norm, ws, stream=None):
     """norm [1] = the norm of all gradients taken as one vector.  An entry is a tensor, or (tensor [slots, ...], n_active): a compacted
     gradient, whose first n_active slots (a number on the GPU) count."""
-    _here(norm, "moe_grad_norm")
+    _here("moe_grad_norm", norm, ws)
     rc = load_library().moe_grad_norm(_grad_list(grads), len(grads), _ptr(norm, torch.float32, "norm"), _ptr(ws, None, "ws"),
                                       ws.numel() * ws.element_size(), _stream(stream))
     _check(rc, "moe_grad_norm")
@@ -765,7 +776,7 @@ def moe_grad_norm(grads, norm, ws, stream=None):
 
 def moe_grad_clip(grads, norm, max_norm: float, out=None, stream=None):
     """The same list times min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
-    _here(norm, "moe_grad_clip")
+    _here("moe_grad_clip", norm)
     rc = load_library().moe_grad_clip(_grad_list(grads, out, written=True), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
     _check(rc, "moe_grad_clip")
 
