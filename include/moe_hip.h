@@ -410,7 +410,8 @@ int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, const int32
  * A gradient is n values, f32 or bf16, 16-byte aligned.  With n_active (device) it is the first min(n, n_active[0] * slot) of them: the compacted weight
  * gradients of moe_expert_bwd, whose number only the GPU knows; values behind those are neither read nor written.
  * out may be g itself (then nothing is written where the factor is 1) and must not overlap any gradient or output otherwise, so no tensor may be in the
- * list twice; moe_grad_norm does not look at it, and counts what is there twice twice.  A norm that is NaN makes every value NaN.
+ * list twice; lists where one does, by the n values of each, are refused.  moe_grad_norm does not look at out, and counts what is there twice twice.
+ * A norm that is NaN makes every value NaN.
  *   grads: n entries in HOST memory, read during the call;  norm [1] f32 (device);  ws >= moe_grad_norm_workspace_bytes()
  */
 typedef struct moe_grad {

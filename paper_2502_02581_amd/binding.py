@@ -715,9 +715,9 @@ def moe_quant_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, row
 
 
 # ---- gradients: lists of tensors, or of (tensor, n_active) for compacted ones [slots, ...]
-def _grad_list(grads, out=None, written=False):
+def _grad_list(grads, out=None):
     """The C form of a list of gradients: its members as one buffer of whole numbers, which for many small tensors takes half the time of
-    structures one by one.  written: no tensor may be an output twice."""
+    structures one by one."""
     if out is not None and len(out) != len(grads):
         raise MoEError(f"{len(grads)} gradients, {len(out)} outputs")
     members, counters = [], {}   # (a counter serves the tensors of a layer: looked at once)
@@ -749,13 +749,6 @@ def _grad_list(grads, out=None, written=False):
                 counters[id(n_active)] = _ptr(n_active, torch.int32, "n_active")
             n_active = counters[id(n_active)]
         members += (g, o, n, n_active or 0, slot, MOE_F32 if dt is torch.float32 else MOE_BF16)
-    if written:
-        outs = [o for o, n in zip(members[1::6], members[2::6]) if n]
-        if len(set(outs)) != len(outs):
-            raise MoEError("a tensor is there twice")
-        ins = {g: i for i, (g, n) in enumerate(zip(members[::6], members[2::6])) if n} if out is not None else {}
-        if any(ins.get(o, i) != i for i, (o, n) in enumerate(zip(members[1::6], members[2::6])) if n):
-            raise MoEError("an output is another gradient")
     if not members:
         return (_CGrad * 1)()
     return (_CGrad * len(grads)).from_buffer(bytearray(struct.pack(f"={len(members)}q", *members)))
@@ -777,7 +770,7 @@ def moe_grad_norm(grads, norm, ws, stream=None):
 def moe_grad_clip(grads, norm, max_norm: float, out=None, stream=None):
     """The same list times min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
     _here("moe_grad_clip", norm)
-    rc = load_library().moe_grad_clip(_grad_list(grads, out, written=True), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
+    rc = load_library().moe_grad_clip(_grad_list(grads, out), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
     _check(rc, "moe_grad_clip")
 
 

@@ -4,6 +4,8 @@
 // training step has no synchronisation between its backward pass and its optimiser, and slots that no expert used are
 // neither read nor written.
 #include <algorithm>
+#include <memory>
+#include <new>
 
 #include "moe_common.h"
 
@@ -153,6 +155,46 @@ static int check_grads(const moe_grad_t* grads, int n, bool out, const char* who
   }
   return MOE_OK;
 }
+// What is written must not overlap anything else that is read or written: chunks are scaled in no order.  Tensors by address; each against the furthest end of
+// those before it (96 tensors and as many outputs: 3 us).
+static int check_outputs(const moe_grad_t* grads, int n, const char* who) {
+  struct Span {
+    uintptr_t from, to;
+    int i;
+    bool out;
+  };
+  std::unique_ptr<Span[]> spans(new (std::nothrow) Span[2 * (size_t)n]);
+  if (!spans) {
+    set_error("%s: no host memory for a list of %d gradients", who, n);
+    return MOE_EINVAL;
+  }
+  size_t m = 0;
+  for (int i = 0; i < n; i++) {
+    const moe_grad_t& g = grads[i];
+    if (g.n == 0) continue;
+    const size_t bytes = (size_t)g.n * elem_size(g.dtype);
+    spans[m++] = {(uintptr_t)g.out, (uintptr_t)g.out + bytes, i, true};
+    if (g.g != g.out) spans[m++] = {(uintptr_t)g.g, (uintptr_t)g.g + bytes, i, false};
+  }
+  std::sort(spans.get(), spans.get() + m, [](const Span& a, const Span& b) { return a.from < b.from; });
+  const Span *in = nullptr, *out = nullptr;  // those that reach furthest so far
+  for (size_t k = 0; k < m; k++) {
+    const Span& s = spans[k];
+    const Span* hit = out && s.from < out->to ? out : s.out && in && s.from < in->to ? in : nullptr;
+    if (hit && hit->out && s.out) {
+      set_error("%s: outputs %d and %d overlap (a tensor is there twice)", who, hit->i, s.i);
+      return MOE_EINVAL;
+    }
+    if (hit) {
+      const Span &o = s.out ? s : *hit, &g = s.out ? *hit : s;
+      set_error(o.i == g.i ? "%s: output %d overlaps its gradient (%d) without being it" : "%s: output %d is another gradient (%d), or overlaps it", who, o.i, g.i);
+      return MOE_EINVAL;
+    }
+    const Span*& far = s.out ? out : in;
+    if (!far || s.to > far->to) far = &s;
+  }
+  return MOE_OK;
+}
 // tensors [from, ..) of a launch; returns the first one behind it
 static int fill_list(GradList& l, const moe_grad_t* grads, int n, int from) {
   l = {};
@@ -202,7 +244,8 @@ extern "C" int moe_grad_norm(const moe_grad_t* grads, int32_t n, float* norm, vo
 
 extern "C" int moe_grad_clip(const moe_grad_t* grads, int32_t n, const float* norm, float max_norm, void* stream) {
   using namespace moe;
-  const int rc = check_grads(grads, n, true, "moe_grad_clip");
+  int rc = check_grads(grads, n, true, "moe_grad_clip");
+  if (!rc) rc = check_outputs(grads, n, "moe_grad_clip");
   if (rc) return rc;
   if (!norm || (uintptr_t)norm % 4 || !(max_norm >= 0.f)) {
     set_error("moe_grad_clip: null pointer, or max_norm not a number from 0 on");
