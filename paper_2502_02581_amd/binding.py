@@ -746,6 +746,8 @@ def _grad_list(grads, out=None):
             if id(n_active) not in counters:
                 if n_active.get_device() != device:
                     raise MoEError(f"n_active of gradient {i} must live on the GPU; it is on {n_active.device}, the current device is cuda:{device}")
+                if n_active.numel() == 0:   # (its address would be NULL: every slot)
+                    raise MoEError(f"n_active of gradient {i} is empty")
                 counters[id(n_active)] = _ptr(n_active, torch.int32, "n_active")
             n_active = counters[id(n_active)]
         members += (g, o, n, n_active or 0, slot, MOE_F32 if dt is torch.float32 else MOE_BF16)

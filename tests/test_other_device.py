@@ -114,3 +114,12 @@ def test_weights_of_another_device(lib, name):
     with pytest.raises(moe.MoEError, match="cuda:1, the current device is cuda:0"):
         call({n: on(t.clone(), int(n.startswith(("Wg", "Wu", "Wd")))) for n, t in args.items()})
     assert lib.reached == 0
+
+
+@pytest.mark.parametrize("name", ["norm", "clip"])
+def test_empty_counter(lib, name):
+    """A counter without a value has no address, which would mean that every slot counts."""
+    args, call = CALLS[name]
+    with pytest.raises(moe.MoEError, match="empty"):
+        call({n: on(i32(0) if n == "n" else t) for n, t in args.items()})
+    assert lib.reached == 0
