@@ -528,6 +528,13 @@ def _here(who, *tensors):
             raise MoEError(f"{who}: a tensor is on {t.device}, the current device is cuda:{device}")
 
 
+def _holds(who, *tensors):
+    """Refuses tensors of fewer values than the call reads or writes."""
+    for t, n, what in tensors:
+        if t is not None and t.numel() < n:
+            raise MoEError(f"{who}: {what} has {t.numel()} values, the call takes {n}")
+
+
 def _pitched(t, shape, what):
     """Pointer and bytes between rows of a [groups, rows, bytes] tensor whose rows may be pieces of longer ones."""
     if t is None:
@@ -683,6 +690,7 @@ def _quant_args(shape, n_groups, n_rows, src_of, Q, S, W, who, *others):
     if W.n_groups != n_groups or (W.shape.d, W.shape.d_ff) != (shape.d, shape.d_ff):
         raise MoEError(f"{who}: the weights are those of {W.n_groups} experts of d={W.shape.d}, d_ff={W.shape.d_ff}")
     rows = n_rows if src_of is None else shape.T
+    _holds(who, (src_of, n_rows, "src_of"))
     return (_sized(Q, (rows, moe_quant_row_bytes(shape.d)), "codes"), _sized(S, (rows, moe_quant_scale_bytes(shape.d)), "exponents"))
 
 
@@ -690,6 +698,11 @@ def moe_quant_expert_fwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, XQ,
     """Forward pass of routed experts on block-scaled operands; G, U and H None where no backward pass follows."""
     bf = torch.bfloat16
     q = _quant_args(shape, n_groups, n_rows, src_of, XQ, XS, W, "moe_quant_expert_fwd", offsets, G, U, H, Yout, plan, ws)
+    kept = n_rows * shape.d_ff
+    _holds("moe_quant_expert_fwd", (offsets, n_groups + 1, "offsets"), (G, kept, "G"), (U if W.gated else None, kept, "U"), (H, kept, "H"),
+           (Yout, n_rows * shape.d, "Yout"))
+    if plan is not None:
+        _holds("moe_quant_expert_fwd", (plan, moe_expert_plan_bytes(shape), "plan"))
     rc = load_library().moe_quant_expert_fwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, torch.int32, "offsets"), n_rows, _ptr(src_of, torch.int32, "src_of"), *q,
         ctypes.byref(W.c), _ptr(G, bf, "G"), _ptr(U, bf, "U"), _ptr(H, bf, "H"), _ptr(Yout, bf, "Yout"),
@@ -705,6 +718,10 @@ def moe_quant_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, src_of, row
         raise MoEError("moe_quant_expert_bwd: these weights have no layouts of the backward pass")
     q = _quant_args(shape, n_groups, n_rows, src_of, dYQ, dYS, W, "moe_quant_expert_bwd", offsets, row_w, Xin, G, U, H, dYin, dXin, active_ids,
                     n_active, dWg_c, dWu_c, dWd_c, ws)
+    kept, tokens, dw = n_rows * shape.d_ff, n_rows * shape.d, min(n_groups, n_rows) * shape.d * shape.d_ff   # (as many slots as can be active)
+    _holds("moe_quant_expert_bwd", (offsets, n_groups + 1, "offsets"), (row_w, n_rows, "row_w"), (Xin, tokens, "Xin"), (G, kept, "G"),
+           (U if W.gated else None, kept, "U"), (H, kept, "H"), (dYin, tokens, "dYin"), (dXin, tokens, "dXin"), (active_ids, n_groups, "active_ids"),
+           (n_active, 1, "n_active"), (dWg_c, dw, "dWg_c"), (dWu_c if W.gated else None, dw, "dWu_c"), (dWd_c, dw, "dWd_c"))
     rc = load_library().moe_quant_expert_bwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, i32, "offsets"), n_rows, _ptr(src_of, i32, "src_of"),
         _ptr(row_w, torch.float32, "row_w"), *q, _ptr(Xin, bf, "Xin"), ctypes.byref(W.c), _ptr(G, bf, "G"),

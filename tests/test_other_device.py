@@ -28,6 +28,9 @@ def on(t, at=0):
 class Library:
     reached = 0
 
+    def moe_expert_plan_bytes(self, shape):   # (asked for, not a call)
+        return 1 << 12
+
     def __getattr__(self, name):
         def call(*a):
             self.reached += 1
