@@ -12,7 +12,8 @@ not look into.  Two things it would otherwise guarantee are therefore checked on
     instruction in the two wait states before it: fragments come straight from LDS reads, whose wait the
     compiler places itself, and this makes sure that no register move is put in between;
   * no GEMM kernel keeps anything in scratch memory: accumulator tiles that end up there (an
-    epilogue too large to unroll did that once) cost a factor of four and show up nowhere else;
+    epilogue too large to unroll did that once) cost a factor of four and show up nowhere else; nor do the kernels that
+    quantise and clip, whose values go through registers only;
   * no packed fp32 arithmetic (v_pk_add_f32, v_pk_mul_f32, v_pk_fma_f32): the build switches the
     feature off (`-packed-fp32-ops`), and this makes sure the switch is still in the flags.
 
@@ -164,11 +165,12 @@ def check_mfma_sources(lines: List[str], wait_states: int = 2) -> List[str]:
     return findings
 
 
-# every kernel of the GEMM sources: row_gemm_, row_w_gemm_, wide_*_gemm_, the light weight gradients and the sums of parts
-GEMM_KERNELS = ("gemm_kernel", "w_light_kernel", "reduce_kernel")
+# every kernel of the GEMM sources: row_gemm_, row_w_gemm_, wide_*_gemm_, the light weight gradients and the sums of parts;
+# and the streams of the quantisation and of the clipping
+NO_SCRATCH = ("gemm_kernel", "w_light_kernel", "reduce_kernel", "quant_rows_kernel", "quant_matrix_kernel", "grad_")
 
 
-def check_no_scratch(lines: List[str], name_parts=GEMM_KERNELS) -> List[str]:
+def check_no_scratch(lines: List[str], name_parts=NO_SCRATCH) -> List[str]:
     findings = []
     kernel = None
     for raw in lines:

@@ -7,23 +7,17 @@ namespace moe {
 
 // ------------------------------------------------------------------------------------- rows
 // Sixteen lanes per block of 128 values, eight values a lane: 16 (fp32: 32) bytes in, 8 out; the maximum by four exchanges.
-// Bound by HBM: it reads every value and writes every code once (8192 x 7168 bf16 values 29.3 us, 6.0 TB/s; with the maximum by exchanges
-// through LDS and the conversion from fp32 36.5).
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {  // n: how many of the eight there are
-  if (VEC && n >= 8) {
-    if constexpr (sizeof(T) == 2) {
-      Vec16<T>::load(p, v);
-    } else {
-      float a[4], b[4];
-      Vec16<T>::load(p, a);
-      Vec16<T>::load(p + 4, b);
-#pragma unroll
-      for (int i = 0; i < 4; i++) { v[i] = a[i]; v[4 + i] = b[i]; }
-    }
+// Bound by HBM: it reads every value and writes every code once.  8192 x 7168 values, back to back on buffers that no cache holds: bf16 34.1 us, 5.2 TB/s, of which
+// the kernel is 29.3 (with the maximum by exchanges through LDS and the conversion from fp32 36.5); fp32 51.0, 5.8 TB/s (61.3 with the whole and the cut
+// pieces of a row loaded by one loop, which kept two of a lane's values in scratch memory).
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    Vec16<T>::load(p, v);
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < n ? Elem<T>::load(p + i) : 0.f;
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   }
 }
 
@@ -50,8 +44,14 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ X
       codes = c[0];
       e = b1[0];
     } else {
-      float v[8];
-      load8<T, VEC>(x, cols - (int)c0, v);
+      float v[8] = {};
+      if (VEC && c0 + 8 <= (uint32_t)cols) {
+        load8(x, v);
+      } else {
+        const int n = cols - (int)c0;  // how many of the eight there are
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = i < n ? Elem<T>::load(x + i) : 0.f;
+      }
       int m[1] = {0};
 #pragma unroll
       for (int i = 0; i < 8; i++) m[0] = max(m[0], (int)finite_bits(v[i]));
@@ -69,7 +69,8 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ X
 // ---------------------------------------------------------------------------------- matrices
 // A block of 256 threads per 128 x 128 values, 8 x 8 of them a thread: the values are read once and both layouts are written from
 // registers, the transposed one through LDS, so that all three streams are whole 128-byte pieces.  Bound by HBM: 60 bf16 matrices of 2048 x 1408, both
-// layouts, 133 us, 5.2 TB/s, where a plain copy moves 4.8.  (LDS pieces swizzled so that no banks conflict: no change.)
+// layouts, 135 us, 5.1 TB/s, where a plain copy moves 4.8, fp32 ones 189 us, 5.5; 24 bf16 ones of 1000 x 1368, which end in cut blocks and a partial round, 34 us,
+// 3.8 TB/s.  (LDS pieces swizzled so that no banks conflict: no change.)
 struct QuantMatrix {
   uint8_t *Q, *S;       // [G][K rows of ldq bytes], [G][K / 128 rows of lds bytes]; NULL: not wanted
   int64_t ldq, lds;
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__
   for (int i = 0; i < 8; i++) {
     // (K and N are multiples of 8: a thread's values are all there or all missing)
     if (k0 < K && n0 < N) {
-      load8<T, true>(W + (g * K + k0 + i) * N + n0, 8, v[i]);
+      load8(W + (g * K + k0 + i) * N + n0, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; j++) v[i][j] = 0.f;
