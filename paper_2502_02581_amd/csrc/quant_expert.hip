@@ -81,28 +81,21 @@ __device__ __forceinline__ void quant_gemm_block(const QuantGemm& p, int block, 
   constexpr int BN = 256 / NB;
   const int ntn = (p.N + BN - 1) / BN;
   const int n_mt = *p.n_tiles;
-  const int total = n_mt * ntn, rounds = total >> 8, per_band = kBandRows * ntn;
-  const int xcd = block & 7, round = block >> 8, b = (block >> 3) & 31;
-  int q = round << 8;
-  if (round < rounds) q += rounds > kFineRounds && round < rounds - 1 ? (xcd << 5) + b : ((b >> 3) << 6) + (xcd << 3) + (b & 7);
-  else q += (b << 3) + xcd;
+  const int total = n_mt * ntn, q = dealt_tile(block, total);
   if (q >= total) return;
   // Launches of four rounds and more take bands two from the front, one from the back, until a third of them have come from the back: short tiles, bound
   // by streaming their matrices, beside tall ones.  (The last band, which may have fewer rows, stays the last.  Longest first and so, us: gate/up of
   // 16384 rows, d = 2048, 60 experts of 1408, Zipf loads, 202 and 184, of 32768 264 and 252, down 137 and 136; 16384 rows, d = 7168, 128 experts of 2048 870
   // and 876, down 472 and 457; launches of two to three rounds lose, gate/up of 9003 rows, d = 1000, 24 experts of 1368, 74 and 83, dH 75 and 93.)
-  const int at = q / per_band, r = q - at * per_band, bands = n_mt / kBandRows, from_back = rounds >= 4 ? bands / 3 : 0, mixed = 3 * from_back;
-  const int band = at >= bands ? at : at >= mixed ? at - from_back : at % 3 == 2 ? bands - 1 - at / 3 : at / 3 * 2 + at % 3;
-  const int high = min(kBandRows, n_mt - band * kBandRows);
-  const int mt = band * kBandRows + r % high, nt = r / high;
-  RowTile t = p.tiles[mt];
+  const TilePlace at = band_tile(q, n_mt, ntn, total >> 8 >= 4 ? n_mt / kBandRows / 3 : 0);
+  RowTile t = p.tiles[at.mt];
   t.group = __builtin_amdgcn_readfirstlane(t.group);
   t.row0_in = __builtin_amdgcn_readfirstlane(t.row0_in);
   t.rows = __builtin_amdgcn_readfirstlane(t.rows);
   t.row0_out = __builtin_amdgcn_readfirstlane(t.row0_out);
-  if (tile_rows(t) > 128) quant_tile<QuantTall<NB>, Epi, NB>(p, t, nt, smem);
-  else if (tile_rows(t) > 64) quant_tile<QuantMid<NB>, Epi, NB>(p, t, nt, smem);
-  else quant_tile<QuantShort<NB>, Epi, NB>(p, t, nt, smem);
+  if (tile_rows(t) > 128) quant_tile<QuantTall<NB>, Epi, NB>(p, t, at.nt, smem);
+  else if (tile_rows(t) > 64) quant_tile<QuantMid<NB>, Epi, NB>(p, t, at.nt, smem);
+  else quant_tile<QuantShort<NB>, Epi, NB>(p, t, at.nt, smem);
 }
 template <int NB, class Epi>
 __global__ __launch_bounds__(256, 1) void quant_gemm_kernel(QuantGemm p) {
@@ -173,28 +166,19 @@ __global__ __launch_bounds__(256, 1) void quant_direct_gemm_kernel(QuantGemm p) 
   extern __shared__ __align__(16) char smem[];
   const int ntn = (p.N + 255) / 256, n_mt = (p.n_rows + p.height - 1) / p.height;
   const int part = PART ? blockIdx.x / p.part_blocks : 0, block = PART ? blockIdx.x - part * p.part_blocks : blockIdx.x;
-  const int total = n_mt * ntn, rounds = total >> 8, full = rounds << 8, per_band = kBandRows * ntn;
-  // (the order of the tiles: see quant_gemm_kernel)
-  const int xcd = block & 7, round = block >> 8, b = (block >> 3) & 31;
-  int q = block, piece = 0, pieces = 1;
-  if (block < full) {
-    q = (round << 8) + (rounds > kFineRounds && round < rounds - 1 ? (xcd << 5) + b : ((b >> 3) << 6) + (xcd << 3) + (b & 7));
-  } else {
-    pieces = p.tail;
-    q = full + (block - full) / pieces;
-    piece = (block - full) % pieces;
-  }
-  if (q >= total) return;
-  const int band = q / per_band, r = q - band * per_band, high = min(kBandRows, n_mt - band * kBandRows);
-  const int nt = r / high, height = p.height / pieces;
+  const int total = n_mt * ntn;
+  const CutTile cut = cut_tile(block, total, PART ? 1 : p.tail);
+  if (cut.q >= total) return;
+  const TilePlace at = band_tile(cut.q, n_mt, ntn, 0);
+  const int height = p.height / cut.pieces;
   RowTile t;
   t.group = 0;
-  t.row0_in = t.row0_out = (band * kBandRows + r % high) * p.height + piece * height;
+  t.row0_in = t.row0_out = at.mt * p.height + cut.piece * height;
   t.rows = min(height, p.n_rows - t.row0_in);
   if (t.rows <= 0) return;
-  if (t.rows > 128) quant_tile<QuantTall<1>, Epi, 1, PART>(p, t, nt, smem, part);
-  else if (t.rows > 64) quant_tile<QuantMid<1>, Epi, 1, PART>(p, t, nt, smem, part);
-  else quant_tile<QuantShort<1>, Epi, 1, PART>(p, t, nt, smem, part);
+  if (t.rows > 128) quant_tile<QuantTall<1>, Epi, 1, PART>(p, t, at.nt, smem, part);
+  else if (t.rows > 64) quant_tile<QuantMid<1>, Epi, 1, PART>(p, t, at.nt, smem, part);
+  else quant_tile<QuantShort<1>, Epi, 1, PART>(p, t, at.nt, smem, part);
 }
 
 // Calls of up to 512 rows, of up to 1024 over eight groups or more: above, a group's tiles read its matrix too often.  (Forward passes with a plan and so, us:
@@ -264,7 +248,7 @@ static void launch_direct(const char* label, QuantGemm p, float* part, hipStream
   p.k_part = ceil_div(p.nk, c.parts);
   p.part = part;
   const int tiles = ceil_div(p.n_rows, c.height) * ceil_div(p.N, 256);
-  p.part_blocks = (tiles / 256 + (tiles % 256 > 0 && c.tail == 1)) * 256 + (c.tail > 1 ? tiles % 256 * c.tail : 0);
+  p.part_blocks = cut_tile_blocks(tiles, c.tail);
   constexpr int kLds = std::max({QuantTall<1>::LDS_BYTES, QuantMid<1>::LDS_BYTES, QuantShort<1>::LDS_BYTES});
   if (c.parts == 1) {
     launch_gemm<quant_direct_gemm_kernel<Epi8<1, EPI_STORE>, false>>(label, (unsigned)p.part_blocks, 256, kLds, st, p);
