@@ -68,8 +68,8 @@ struct QuantTile {
 // Every fragment is read from LDS once, and no register holds two blocks' values of the same fragment.  MFMAs are inline assembly with a memory
 // clobber, so that the order is the one written here (see MfmaDmaCore, whose loads, LDS layout and epilogue these are).
 //
-// What bounds it: the matrix pipe at the clock it leaves itself.  A block of K of a 256 x 256 tile (64 MFMAs a wave, 2048 cycles) takes 1.4 to 1.65 us by box; without loads
-// and LDS reads 1.26, i.e. the shader clock falls to 1.6 GHz; without the loads 1.40; with loads that all hit L2 1.58 (of 1.70).  A tile costs
+// What bounds it: the matrix pipe at the clock it leaves itself.  A block of K of a 256 x 256 tile (64 MFMAs a wave, 2048 cycles) takes 1.4 to 1.7 us by box.  Where it took
+// 1.70: with loads that all hit L2 1.58, without the loads 1.40, without LDS reads too 1.26, i.e. the shader clock falls to 1.6 GHz.  A tile costs
 // 7 us besides (first loads, epilogue).  Products of 8192 x 4096 x 6400 175 us (2.45 PFLOP/s), of 16384 x 8192 x 8192 779 us (2.82); the
 // register-resident loop of this instruction sustains 3.5 to 4.4 by operands, the vendor library (one scale a tensor) takes 235 us for the former and reaches
 // 2.70 on 8192 x 8192 x 8192, where this core reaches 2.65.

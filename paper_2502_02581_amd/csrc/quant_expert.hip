@@ -187,9 +187,10 @@ __global__ __launch_bounds__(256, 1) void quant_direct_gemm_kernel(QuantGemm p) 
 // Sums in parts, joined by another launch, gain where a call has four rows (K = 2048, N = 1408: 13.8 and 11.6 us) and lose from eight on.)
 static bool quant_small(int n_groups, int n_rows) { return n_rows <= 512 || (n_groups >= 8 && n_rows <= 1024); }
 // Products whose outputs are quantised, of up to 2^16 values of them: computed from bf16 values, in tiles of 64 rows.  The 8-bit instruction's error, 1.5e-5, moves one
-// in 4000 of the outputs to the other side of a border between codes.  Over many that adds 1e-3 to the 1.7e-3 of the next product's rounding to bf16, but where
-// fewer than some sixteen of them are moved, the error is that of the one which weighs most (0.0056 of a training step's dX, 0.0051 of a forward pass's Y of 2 tokens;
-// from bf16 values 0.0017; 1800 random calls of 2^16 to 2^20 values on the 8-bit instruction at most 0.0038).  Gate and up of 64 rows, 60 experts of
+// in 600 of the outputs of silu(G) U to the other side of a border between codes, one in 1000 of gelu(G): small ones above all, by their share of the sum of squares one
+// in 5000 to 15000.  Over many that adds 1e-3 to the 1.7e-3 of the next product's rounding to bf16, but where few of them carry weight, the error is that of the one which
+// carries most (0.0056 of a training step's dX, 0.0051 of a forward pass's Y of 2 tokens; from bf16 values 0.0017; 1800 random calls of 2^16 to 2^20 values on the 8-bit
+// instruction at most 0.0038).  The line is one for the tensor: a row of d_ff values of which one is moved may be off by more (see moe_hip.h).  Gate and up of 64 rows, 60 experts of
 // 2048 x 1408, which are more than that: 28 us from bf16 values, 21 on the 8-bit instruction.
 static bool quant_exact(int64_t n_rows, int cols) { return n_rows * cols <= 1 << 16; }
 template <int NB, class Epi, bool EXACT = false>

@@ -33,8 +33,8 @@ __device__ __forceinline__ uint32_t quant_codes(const float (&x)[4], float f) {
   const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, w, true);
 }
-// maxima over the sixteen lanes of a row, in all of them (in-register rotations: exchanges through LDS cost 46 us of a 124 us launch whose
-// epilogue quantises two outputs; several at a time, because a rotation may read what was written only two instructions later)
+// maxima over the sixteen lanes of a row, in all of them (in-register rotations: a launch of 124 us took 170 with exchanges through LDS once its
+// epilogue quantised its two outputs, 145 with these; several at a time, because a rotation may read what was written only two instructions later)
 template <int ROTATE, int N>
 __device__ __forceinline__ void rotate_max(int (&v)[N]) {
 #pragma unroll
