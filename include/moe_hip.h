@@ -376,7 +376,8 @@ int moe_combine_bwd(const moe_shape_t* shape, const void* dY, const void* Yp, co
  *     dG, dU as in moe_expert_bwd, from the bf16 G, U, and rounded to bf16;  dXin = quant(dG) Wg[e]^T + quant(dU) Wu[e]^T;
  *     dWg = Xin^T dG, dWu = Xin^T dU, dWd = H^T dYin: bf16 products, as in moe_expert_bwd (a gradient that is summed over thousands of steps
  *     is not worth 4 bits), compacted as there; Xin, dYin [n_rows, d] are in grouped order.
- *   The gradients are those of the same pass with each quantised tensor's gradient passed on as it is.
+ *   dXin is the gradient of that forward pass with each quantised tensor's gradient passed on as it is; the weight gradients are taken with Xin, H and dYin
+ *   themselves in the place of the values that their codes stand for.
  *   weights: what moe_quant_weights makes of Wg, Wu [n_groups, d, d_ff], Wd [n_groups, d_ff, d]; the passes use their own layouts:
  *     forward:  WgT, WuT [n_groups, d_ff, rows of d], WdT [n_groups, d, rows of d_ff]
  *     backward: Wd [n_groups, d_ff, rows of d];  Wgu [n_groups, d, a row of Wg and then the same row of Wu], both padded to whole blocks, and
@@ -413,7 +414,8 @@ int moe_quant_expert_bwd(const moe_shape_t* shape, int32_t n_groups, const int32
  * gradients of moe_expert_bwd, whose number only the GPU knows; values behind those are neither read nor written.
  * out may be g itself (then nothing is written where the factor is 1) and must not overlap any gradient or output otherwise, so no tensor may be in the
  * list twice; lists where one does, by the n values of each, are refused.  moe_grad_norm does not look at out, and counts what is there twice twice.
- * A norm that is NaN makes every value NaN.
+ * A norm that is NaN makes every value NaN.  The sum of squares cannot overflow, its root rounded to f32 can: a norm of 2^128 or more is infinite, the factor
+ * then 0, and finite values become zero, infinite ones NaN.
  *   grads: n entries in HOST memory, read during the call;  norm [1] f32 (device);  ws >= moe_grad_norm_workspace_bytes()
  */
 typedef struct moe_grad {

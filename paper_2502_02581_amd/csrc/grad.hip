@@ -12,7 +12,7 @@
 namespace moe {
 
 // Both passes are bound by HBM: two layers of 60 experts, d = 2048, d_ff = 1408, 2.06 GB of gradients: norm 371 us (5.6 TB/s read), clipping 778 us (5.3 TB/s
-// read and written).  Many small tensors cost a launch each way and nothing else: 32 of 8 KB to 1 MB, 9 + 7 + 12 us.
+// read and written).  Many small tensors cost a launch each way and nothing else: 32 of 4 KB to 1 MB, 9 + 7 + 12 us.
 //
 // Tensors are cut into chunks of kChunk values, numbered through all tensors of a launch; blocks take them in turn.
 constexpr int kChunk = 16384, kGradThreads = 256, kGradBlocks = 2048, kGradsPerLaunch = 48;
@@ -43,7 +43,7 @@ __device__ __forceinline__ Chunk find_chunk(const GradList& l, uint32_t c) {
   return {lo, from, min(from + kChunk, n)};
 }
 
-// Squares are summed in 64 bits: no overflow or underflow for any finite gradient, and an error that is far below the result's rounding
+// Squares are summed in 64 bits: the sum has no overflow or underflow for any finite gradient (its root may be beyond fp32's range), and an error that is far below the result's rounding
 // whatever the number of values.  A lane has eight loads of 16 bytes in flight and four sums; its partial sum, the block's and those of the blocks are added in a
 // fixed order, so two calls give the same bits.
 template <typename T>

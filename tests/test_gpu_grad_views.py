@@ -1,4 +1,4 @@
-"""Clipping of gradients that are pieces of one buffer."""
+"""Clipping of gradients that are pieces of one buffer, and of a norm that fp32 does not hold."""
 import pytest
 import torch
 
@@ -34,3 +34,26 @@ def test_pieces_of_one_buffer():
     assert torch.equal(a, want) and torch.equal(b, want)
     m.moe_grad_clip(pieces, norm, limit)
     assert torch.equal(whole, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_beyond_fp32(dtype):
+    """Below 2^128 the norm is a number and the factor scales by it; from there on it is infinite and clips to zero, infinities to NaN."""
+    import paper_2502_02581_amd as m
+
+    norm, ws = torch.zeros(1, device=DEV), torch.empty(m.moe_grad_norm_workspace_bytes(), dtype=torch.uint8, device=DEV)
+    big = 2.0 ** 127
+    x, out = torch.tensor([big, big, -big], dtype=dtype, device=DEV), torch.ones(3, dtype=dtype, device=DEV)
+    m.moe_grad_norm([x], norm, ws)
+    assert abs(float(norm) / (big * 3 ** 0.5) - 1) <= 2.0 ** -23
+    m.moe_grad_clip([x], norm, 1.0, [out])
+    assert float((out.double().abs() - 3 ** -0.5).abs().max()) <= 3 ** -0.5 * (torch.finfo(dtype).eps / 2 + 2.0 ** -21)
+    x = torch.tensor([big, big, -big, big, 1.0], dtype=dtype, device=DEV)
+    out = torch.ones(5, dtype=dtype, device=DEV)
+    m.moe_grad_norm([x], norm, ws)
+    assert float(norm) == float("inf")   # 2^128 and a little more
+    m.moe_grad_clip([x], norm, 1.0, [out])
+    assert bool((out == 0).all())
+    x[1] = float("inf")
+    m.moe_grad_clip([x], norm, 1.0, [out])
+    assert bool(torch.isnan(out[1])) and bool((out[[0, 2, 3, 4]] == 0).all())
