@@ -197,143 +197,143 @@ struct QuantCore {
       vos = srow < t.map.rows ? (uint32_t)t.map(srow) * (uint32_t)las : kNowhere;
     } else {
 #pragma unroll
-        for (int j = 0; j < A_NI; j++) voa[j] = (uint32_t)(row + 32 * j) * (uint32_t)lda + col;
-        vos = srow < t.map.rows ? (uint32_t)srow * (uint32_t)las : kNowhere;
+      for (int j = 0; j < A_NI; j++) voa[j] = (uint32_t)(row + 32 * j) * (uint32_t)lda + col;
+      vos = srow < t.map.rows ? (uint32_t)srow * (uint32_t)las : kNowhere;
+    }
+#pragma unroll
+    for (int j = 0; j < B_NI; j++) vob[j] = (uint32_t)(row + 32 * j) * (uint32_t)ldb + col;
+    const uint32_t zero = 0;
+    Cursor c;
+    const uint32_t k_bytes = (uint32_t)nk * BK;
+    c.a = desc(t.a, t.a_bytes);
+    c.as = desc(t.as, t.as_bytes);
+#pragma unroll
+    for (int x = 0; x < NB; x++) {
+      c.b[x] = desc(t.b[x], (uint32_t)(t.n_valid - 1) * (uint32_t)ldb + k_bytes);
+      // columns of this wave that do not exist have no exponents either
+      c.bs[x] = desc(t.bs[x] + (NB == 1 ? (wn0 / kQuantBlock) * lbs : 0), wn0 < t.n_valid ? (uint32_t)nk : 0u);
+    }
+    c.left = nk;
+#pragma unroll
+    for (int x = 0; x < NB; x++) asm volatile("" : "+s"(c.b[x]), "+s"(c.bs[x]) : : "memory");
+    asm volatile("s_nop 4" : "+s"(c.a), "+s"(c.as) : : "memory");
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    // LDS addresses of a slot's pieces of this wave (16-byte loads, words of A's exponents, of B's)
+    const uint32_t p16 = lds0 + (uint32_t)wave * 1024u, pa = lds0 + SA_AT + (uint32_t)((wave * 64) & (BM - 1)) * 4u, pb = lds0 + SB_AT + (uint32_t)wave * (NB * 256u);
+    // load number n of an iteration: A, then B, then the exponents; `at`: the slot's offset
+    auto each_load = [&](auto n_c, uint32_t at, auto&& f) __attribute__((always_inline)) {
+      constexpr int n = decltype(n_c)::value;
+      if constexpr (n < A_NI) f(std::integral_constant<int, n * 4096>(), std::false_type(), c.a, p16 + at, voa[n]);
+      else if constexpr (n < A_NI + NB * B_NI) {
+        constexpr int x = (n - A_NI) / B_NI, j = (n - A_NI) % B_NI;
+        f(std::integral_constant<int, A_BYTES + x * B_BYTES + j * 4096>(), std::false_type(), c.b[x], p16 + at, vob[j]);
+      } else if constexpr (n == A_NI + NB * B_NI) f(std::integral_constant<int, 0>(), std::true_type(), c.as, pa + at, vos);
+      else {
+        constexpr int x = n - (A_NI + NB * B_NI + 1);
+        f(std::integral_constant<int, x * 256>(), std::true_type(), c.bs[x], pb + at, zero);
       }
+    };
+    auto issue = [&](auto n_c, uint32_t at) __attribute__((always_inline)) {
+      each_load(n_c, at, [&](auto plus, auto word, const rsrc_t& r, uint32_t base, uint32_t vo) __attribute__((always_inline)) {
+        load<decltype(plus)::value, decltype(word)::value>(r, base, vo);
+      });
+    };
+    for (int s = 0; s < SLOTS; s++) {
+      static_for<L>([&](auto n) __attribute__((always_inline)) { issue(n, (uint32_t)(s * SLOT_BYTES)); });
+      next(c);
+    }
 #pragma unroll
-      for (int j = 0; j < B_NI; j++) vob[j] = (uint32_t)(row + 32 * j) * (uint32_t)ldb + col;
-      const uint32_t zero = 0;
-      Cursor c;
-      const uint32_t k_bytes = (uint32_t)nk * BK;
-      c.a = desc(t.a, t.a_bytes);
-      c.as = desc(t.as, t.as_bytes);
+    for (int x = 0; x < NB; x++)
 #pragma unroll
-      for (int x = 0; x < NB; x++) {
-        c.b[x] = desc(t.b[x], (uint32_t)(t.n_valid - 1) * (uint32_t)ldb + k_bytes);
-        // columns of this wave that do not exist have no exponents either
-        c.bs[x] = desc(t.bs[x] + (NB == 1 ? (wn0 / kQuantBlock) * lbs : 0), wn0 < t.n_valid ? (uint32_t)nk : 0u);
-      }
-      c.left = nk;
+      for (int i = 0; i < TM; i++)
 #pragma unroll
-      for (int x = 0; x < NB; x++) asm volatile("" : "+s"(c.b[x]), "+s"(c.bs[x]) : : "memory");
-      asm volatile("s_nop 4" : "+s"(c.a), "+s"(c.as) : : "memory");
-      const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-      // LDS addresses of a slot's pieces of this wave (16-byte loads, words of A's exponents, of B's)
-      const uint32_t p16 = lds0 + (uint32_t)wave * 1024u, pa = lds0 + SA_AT + (uint32_t)((wave * 64) & (BM - 1)) * 4u, pb = lds0 + SB_AT + (uint32_t)wave * (NB * 256u);
-      // load number n of an iteration: A, then B, then the exponents; `at`: the slot's offset
-      auto each_load = [&](auto n_c, uint32_t at, auto&& f) __attribute__((always_inline)) {
-        constexpr int n = decltype(n_c)::value;
-        if constexpr (n < A_NI) f(std::integral_constant<int, n * 4096>(), std::false_type(), c.a, p16 + at, voa[n]);
-        else if constexpr (n < A_NI + NB * B_NI) {
-          constexpr int x = (n - A_NI) / B_NI, j = (n - A_NI) % B_NI;
-          f(std::integral_constant<int, A_BYTES + x * B_BYTES + j * 4096>(), std::false_type(), c.b[x], p16 + at, vob[j]);
-        } else if constexpr (n == A_NI + NB * B_NI) f(std::integral_constant<int, 0>(), std::true_type(), c.as, pa + at, vos);
-        else {
-          constexpr int x = n - (A_NI + NB * B_NI + 1);
-          f(std::integral_constant<int, x * 256>(), std::true_type(), c.bs[x], pb + at, zero);
-        }
-      };
-      auto issue = [&](auto n_c, uint32_t at) __attribute__((always_inline)) {
-        each_load(n_c, at, [&](auto plus, auto word, const rsrc_t& r, uint32_t base, uint32_t vo) __attribute__((always_inline)) {
-          load<decltype(plus)::value, decltype(word)::value>(r, base, vo);
-        });
-      };
-      for (int s = 0; s < SLOTS; s++) {
-        static_for<L>([&](auto n) __attribute__((always_inline)) { issue(n, (uint32_t)(s * SLOT_BYTES)); });
-        next(c);
-      }
+        for (int j = 0; j < TN; j++) acc[x][i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // (pinned: see MfmaDmaCore)
 #pragma unroll
-      for (int x = 0; x < NB; x++)
+    for (int x = 0; x < NB; x++)
 #pragma unroll
-        for (int i = 0; i < TM; i++)
+      for (int i = 0; i < TM; i++)
 #pragma unroll
-          for (int j = 0; j < TN; j++) acc[x][i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      // (pinned: see MfmaDmaCore)
-#pragma unroll
-      for (int x = 0; x < NB; x++)
-#pragma unroll
-        for (int i = 0; i < TM; i++)
-#pragma unroll
-          for (int j = 0; j < TN; j++) asm volatile("" : "+a"(acc[x][i][j])::"memory");
-      asm volatile("s_nop 7" ::: "memory");
+        for (int j = 0; j < TN; j++) asm volatile("" : "+a"(acc[x][i][j])::"memory");
+    asm volatile("s_nop 7" ::: "memory");
 
-      // ---- fragments: lane l holds 32 codes of row l % 16: the 16-byte pieces l / 16 and 4 + l / 16 (any order of K that both operands share will do)
-      const int fr = lane & 15, h = lane >> 4;
-      // (EXACT: where only the first of the WM strips of rows has any, its waves share K with the others)
-      const bool share = EXACT && WM > 1 && t.map.rows <= BM / WM;
-      const int am0 = share ? 0 : wm0;
-      uint32_t ao[2], bo[2];
+    // ---- fragments: lane l holds 32 codes of row l % 16: the 16-byte pieces l / 16 and 4 + l / 16 (any order of K that both operands share will do)
+    const int fr = lane & 15, h = lane >> 4;
+    // (EXACT: where only the first of the WM strips of rows has any, its waves share K with the others)
+    const bool share = EXACT && WM > 1 && t.map.rows <= BM / WM;
+    const int am0 = share ? 0 : wm0;
+    uint32_t ao[2], bo[2];
 #pragma unroll
-      for (int q = 0; q < 2; q++) {
-        ao[q] = lds0 + (uint32_t)((am0 + fr) * BK + (((4 * q + h) ^ swizzle(am0 + fr)) << 4));
-        bo[q] = lds0 + A_BYTES + (uint32_t)((wn0 + fr) * BK + (((4 * q + h) ^ swizzle(wn0 + fr)) << 4));
-      }
-      const uint32_t sao = lds0 + SA_AT + (uint32_t)(am0 + fr) * 4u, sbo = pb + (uint32_t)lane * 4u;
-      frag_t fa[TM], fl[HB], fh[HB];
-      int sa[TM], sl, sh;
-      auto frag = [&](const uint32_t (&o)[2], uint32_t at, uint32_t plus) __attribute__((always_inline)) {
-        const u32x4_t p = lds<u32x4_t>(o[0] + at + plus), q = lds<u32x4_t>(o[1] + at + plus);
-        return __builtin_bit_cast(frag_t, __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7));
+    for (int q = 0; q < 2; q++) {
+      ao[q] = lds0 + (uint32_t)((am0 + fr) * BK + (((4 * q + h) ^ swizzle(am0 + fr)) << 4));
+      bo[q] = lds0 + A_BYTES + (uint32_t)((wn0 + fr) * BK + (((4 * q + h) ^ swizzle(wn0 + fr)) << 4));
+    }
+    const uint32_t sao = lds0 + SA_AT + (uint32_t)(am0 + fr) * 4u, sbo = pb + (uint32_t)lane * 4u;
+    frag_t fa[TM], fl[HB], fh[HB];
+    int sa[TM], sl, sh;
+    auto frag = [&](const uint32_t (&o)[2], uint32_t at, uint32_t plus) __attribute__((always_inline)) {
+      const u32x4_t p = lds<u32x4_t>(o[0] + at + plus), q = lds<u32x4_t>(o[1] + at + plus);
+      return __builtin_bit_cast(frag_t, __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto read_a = [&](auto i_c, uint32_t at) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_c)::value;
+      sa[i] = lds<int32_t>(sao + at + i * 64);
+      fa[i] = frag(ao, at, i * 16 * BK);
+    };
+    auto read_lo = [&](auto j_c, uint32_t at) __attribute__((always_inline)) {
+      constexpr int j = decltype(j_c)::value;
+      if constexpr (j == 0) sl = lds<int32_t>(sbo + at);
+      fl[j] = frag(bo, at, j * 16 * BK);
+    };
+    auto read_hi = [&](auto j_c, uint32_t at) __attribute__((always_inline)) {
+      constexpr int j = decltype(j_c)::value;
+      if constexpr (j == 0) sh = lds<int32_t>(sbo + at + (NB - 1) * 256);
+      fh[j] = frag(bo, at, NB == 2 ? B_BYTES + j * 16 * BK : (HB + j) * 16 * BK);
+    };
+    auto landed = [&](auto n) __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(n)::value) : "memory");
+      __syncthreads();
+    };
+    uint32_t cur = 0;
+    if constexpr (EXACT) {
+      // the bf16 values of a quarter of a fragment: an operand of v_mfma_f32_16x16x32_bf16
+      auto values = [](const frag_t& f, auto q_c, int byte) __attribute__((always_inline)) {
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+        constexpr int q = decltype(q_c)::value;
+        const float scale = __uint_as_float((uint32_t)byte << 23);
+        const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q], scale, false),
+                       b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q], scale, true),
+                       c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q + 1], scale, false),
+                       d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q + 1], scale, true);
+        bf16x8_t v = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+        asm volatile("s_nop 1" : "+v"(v));  // two wait states between the conversions and the matrix instructions
+        return v;
       };
-      auto read_a = [&](auto i_c, uint32_t at) __attribute__((always_inline)) {
-        constexpr int i = decltype(i_c)::value;
-        sa[i] = lds<int32_t>(sao + at + i * 64);
-        fa[i] = frag(ao, at, i * 16 * BK);
-      };
-      auto read_lo = [&](auto j_c, uint32_t at) __attribute__((always_inline)) {
-        constexpr int j = decltype(j_c)::value;
-        if constexpr (j == 0) sl = lds<int32_t>(sbo + at);
-        fl[j] = frag(bo, at, j * 16 * BK);
-      };
-      auto read_hi = [&](auto j_c, uint32_t at) __attribute__((always_inline)) {
-        constexpr int j = decltype(j_c)::value;
-        if constexpr (j == 0) sh = lds<int32_t>(sbo + at + (NB - 1) * 256);
-        fh[j] = frag(bo, at, NB == 2 ? B_BYTES + j * 16 * BK : (HB + j) * 16 * BK);
-      };
-      auto landed = [&](auto n) __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(n)::value) : "memory");
-        __syncthreads();
-      };
-      uint32_t cur = 0;
-      if constexpr (EXACT) {
-        // the bf16 values of a quarter of a fragment: an operand of v_mfma_f32_16x16x32_bf16
-        auto values = [](const frag_t& f, auto q_c, int byte) __attribute__((always_inline)) {
-          typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-          constexpr int q = decltype(q_c)::value;
-          const float scale = __uint_as_float((uint32_t)byte << 23);
-          const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q], scale, false),
-                         b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q], scale, true),
-                         c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q + 1], scale, false),
-                         d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * q + 1], scale, true);
-          bf16x8_t v = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-          asm volatile("s_nop 1" : "+v"(v));  // two wait states between the conversions and the matrix instructions
-          return v;
-        };
-        for (int it = 0; it < nk; it++) {
-          landed(std::integral_constant<int, (SLOTS - 1) * L>());
-          static_for<TM>([&](auto i) __attribute__((always_inline)) { read_a(i, cur); });
-          static_for<HB>([&](auto j) __attribute__((always_inline)) { read_lo(j, cur); });
-          static_for<HB>([&](auto j) __attribute__((always_inline)) { read_hi(j, cur); });
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          __syncthreads();  // every wave has read the slot: the loads of it + SLOTS may overwrite it
-          static_for<L>([&](auto n) __attribute__((always_inline)) { issue(n, cur); });
-          next(c);
-          static_for<4>([&](auto q_c) __attribute__((always_inline)) {
-            if (share && decltype(q_c)::value / (4 / WM) != wave / WN) return;
-            bf16x8_t va[TM];
-            static_for<TM>([&](auto i) __attribute__((always_inline)) { va[decltype(i)::value] = values(fa[decltype(i)::value], q_c, sa[decltype(i)::value]); });
-            static_for<2 * HB>([&](auto t_c) __attribute__((always_inline)) {
-              constexpr int t = decltype(t_c)::value, j = t % HB;
-              const bf16x8_t vb = values(t < HB ? fl[j] : fh[j], q_c, t < HB ? sl : sh);
-              static_for<TM>([&](auto i_c) __attribute__((always_inline)) {
-                constexpr int i = decltype(i_c)::value;
-                mfma_values(t < HB ? acc[0][i][j] : NB == 2 ? acc[NB - 1][i][j] : acc[0][i][TN - HB + j], vb, va[i]);
-              });
+      for (int it = 0; it < nk; it++) {
+        landed(std::integral_constant<int, (SLOTS - 1) * L>());
+        static_for<TM>([&](auto i) __attribute__((always_inline)) { read_a(i, cur); });
+        static_for<HB>([&](auto j) __attribute__((always_inline)) { read_lo(j, cur); });
+        static_for<HB>([&](auto j) __attribute__((always_inline)) { read_hi(j, cur); });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __syncthreads();  // every wave has read the slot: the loads of it + SLOTS may overwrite it
+        static_for<L>([&](auto n) __attribute__((always_inline)) { issue(n, cur); });
+        next(c);
+        static_for<4>([&](auto q_c) __attribute__((always_inline)) {
+          if (share && decltype(q_c)::value / (4 / WM) != wave / WN) return;
+          bf16x8_t va[TM];
+          static_for<TM>([&](auto i) __attribute__((always_inline)) { va[decltype(i)::value] = values(fa[decltype(i)::value], q_c, sa[decltype(i)::value]); });
+          static_for<2 * HB>([&](auto t_c) __attribute__((always_inline)) {
+            constexpr int t = decltype(t_c)::value, j = t % HB;
+            const bf16x8_t vb = values(t < HB ? fl[j] : fh[j], q_c, t < HB ? sl : sh);
+            static_for<TM>([&](auto i_c) __attribute__((always_inline)) {
+              constexpr int i = decltype(i_c)::value;
+              mfma_values(t < HB ? acc[0][i][j] : NB == 2 ? acc[NB - 1][i][j] : acc[0][i][TN - HB + j], vb, va[i]);
             });
           });
-          cur = cur == (SLOTS - 1) * SLOT_BYTES ? 0u : cur + SLOT_BYTES;
-        }
-      } else {
+        });
+        cur = cur == (SLOTS - 1) * SLOT_BYTES ? 0u : cur + SLOT_BYTES;
+      }
+    } else {
       landed(std::integral_constant<int, (SLOTS - 1) * L>());
       static_for<HB>([&](auto j) __attribute__((always_inline)) { read_lo(j, 0); });
       static_for<TM - 1>([&](auto i) __attribute__((always_inline)) { read_a(i, 0); });
