@@ -1,4 +1,4 @@
-"""Clipping of gradients that are pieces of one buffer, and of a norm that fp32 does not hold."""
+"""Clipping of gradients that are pieces of one buffer, of a norm that fp32 does not hold, and of more values than 32 bits count."""
 import pytest
 import torch
 
@@ -57,3 +57,28 @@ def test_norm_beyond_fp32(dtype):
     x[1] = float("inf")
     m.moe_grad_clip([x], norm, 1.0, [out])
     assert bool(torch.isnan(out[1])) and bool((out[[0, 2, 3, 4]] == 0).all())
+
+
+def test_more_values_than_32_bits_count():
+    import paper_2502_02581_amd as m
+
+    torch.cuda.empty_cache()
+    n = (1 << 32) + 24
+    if torch.cuda.mem_get_info()[0] < 32 << 30:
+        pytest.skip("32 GiB of device memory")
+    x = torch.ones(4, n // 4, dtype=torch.bfloat16, device=DEV)   # slots of 2^30 + 6 values, three of which count
+    used = torch.tensor([3], dtype=torch.int32, device=DEV)
+    norm, ws = torch.zeros(1, device=DEV), torch.empty(m.moe_grad_norm_workspace_bytes(), dtype=torch.uint8, device=DEV)
+    for grads, values in (([x], n), ([(x, used)], n // 4 * 3)):
+        x.fill_(1)
+        x.view(-1)[-1] = 2
+        m.moe_grad_norm(grads, norm, ws)
+        want = (values + (3 if values == n else 0)) ** 0.5
+        assert abs(float(norm) - want) <= 2.0 ** -23 * want
+        m.moe_grad_clip(grads, norm, 0.5 * float(norm))
+        flat = x.view(-1)
+        for i in (0, 1 << 31, (1 << 32) - 8, values - 2):
+            assert float(flat[min(i, values - 2)]) == 0.5
+        assert bool((flat[n // 4 * 3:n // 4 * 3 + 100] == (0.5 if values == n else 1)).all()) and float(flat[-1]) == (1 if values == n else 2)
+    del x
+    torch.cuda.empty_cache()
