@@ -8,7 +8,7 @@ namespace moe {
 // ------------------------------------------------------------------------------------- rows
 // Sixteen lanes per block of 128 values, eight values a lane: 16 (fp32: 32) bytes in, 8 out; the maximum by four exchanges.
 // Bound by HBM: it reads every value and writes every code once.  8192 x 7168 values, back to back on buffers that no cache holds: bf16 34.1 us, 5.2 TB/s, of which
-// the kernel is 29.3 (with the maximum by exchanges through LDS and the conversion from fp32 36.5); fp32 51.0, 5.8 TB/s (61.3 with the whole and the cut
+// the kernel is 28.2 (with the maximum by exchanges through LDS and the conversion from fp32 36.5); fp32 51.0, 5.8 TB/s (kernel 47.2; 61.3 with the whole and the cut
 // pieces of a row loaded by one loop, which kept two of a lane's values in scratch memory).
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
