@@ -853,7 +853,7 @@ class MoEHotPath:
     With quant (bf16 layers) the routed experts run on block-scaled operands: forward() and backward() take a MoEQuantWeights in the place of
     Wg, and None for Wu and Wd.  Tokens and their gradients are quantised once, in their own order, and read in place.  Shared experts stay in
     bf16 and have no launches in common with the routed ones: their calls follow those, or, with overlap_shared, go to the second stream beside them (the
-    training step above with quant 1.83 ms, with overlap_shared 1.76, in bf16 on this machine 2.04).
+    training step above with quant 1.83 ms, with overlap_shared 1.76, in bf16 measured beside them 2.04).
     """
 
     def __init__(self, shape: MoEShape, n_shared: int = 0, d_ff_shared: int = 0, device="cuda:0",

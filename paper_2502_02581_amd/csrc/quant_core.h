@@ -69,9 +69,9 @@ struct QuantTile {
 // clobber, so that the order is the one written here (see MfmaDmaCore, whose loads, LDS layout and epilogue these are).
 //
 // What bounds it: matrix instructions that share their cycles with loads and LDS reads, at a clock that power holds down.  In the launch of 8192 x 4096 x 6400 the pipe is busy in
-// 61 % of a unit's cycles at 1.8 GHz, in the K loop in 69 %; waits for LDS are 0.6 % of a wave's time.  A block of K of a 256 x 256 tile (64 MFMAs a wave, 2048 cycles) takes 1.4 to 1.7 us by box.  Where it took
+// 61 % of a unit's cycles at 1.8 GHz, in the K loop in 69 %; waits for LDS are 0.6 % of a wave's time.  A block of K of a 256 x 256 tile (64 MFMAs a wave, 2048 cycles) takes 1.4 to 1.7 us by card.  Where it took
 // 1.70: with loads that all hit L2 1.58, without the loads 1.40, without LDS reads too 1.26, i.e. 2048 cycles at 1.6 GHz.  A tile costs
-// 7 us besides (first loads, epilogue).  Products of 8192 x 4096 x 6400 172 to 179 us by box (2.40 to 2.50 PFLOP/s), of 16384 x 8192 x 8192 779 us (2.82); the
+// 7 us besides (first loads, epilogue).  Products of 8192 x 4096 x 6400 172 to 179 us by card (2.40 to 2.50 PFLOP/s), of 16384 x 8192 x 8192 779 us (2.82); the
 // register-resident loop of this instruction sustains 3.5 to 4.4 by operands, the vendor library (one scale a tensor) takes 235 us for the former and reaches
 // 2.70 on 8192 x 8192 x 8192, where this core reaches 2.65.
 // EXACT: the products are computed from the bf16 values that the codes stand for (a code times a power of two is one, but for the ends of bf16's range), whose

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from .test_gpu_quant import Layer
+from .test_gpu_quant import Layer, moe
 
 pytestmark = pytest.mark.gpu
 # calls of few values, on small tiles with a plan, in common launches with the weight gradients first and last; gated or not; rows in place or grouped
@@ -116,3 +116,39 @@ def test_rows_of_no_group_stay_and_all_others_are_written(case, graph):
         for t in outs:
             assert bool((t[:5] == 7 + i).all()) and bool((t[L.n - 37:] == 7 + i).all())
         assert all(bool((t[n:] == 7 + i).all()) for t in grads)
+
+
+def test_two_passes_at_once():
+    """Two layers and a clipping on three streams, each on its own workspace, give the bits that they give alone."""
+    m = moe()
+    layers = [Layer(700, 5, 2, 256, 384, True, True), Layer(1700, 4, 1, 2056, 200, True, False)]
+    for L in layers:
+        L.forward()
+        L.backward()
+    grads = [torch.randn(100003, device=layers[0].X.device), torch.randn(1 << 20, device=layers[0].X.device).to(torch.bfloat16)]
+    out = [torch.empty_like(t) for t in grads]
+    norm, ws = torch.zeros(1, device=grads[0].device), torch.empty(m.moe_grad_norm_workspace_bytes(), dtype=torch.uint8, device=grads[0].device)
+
+    def clip(stream=None):
+        m.moe_grad_norm(grads, norm, ws, stream)
+        m.moe_grad_clip(grads, norm, 1.0, out, stream)
+
+    clip()
+    torch.cuda.synchronize()
+    bits, ref = [Bits(L) for L in layers], [norm.clone(), *[t.clone() for t in out]]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for i in range(4):
+        for b in bits:
+            b.clear(i)
+        for t in (norm, *out):
+            t.fill_(-1)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for L, s in zip(layers, streams):
+                L.forward(stream=s)
+                L.backward(stream=s)
+            clip(streams[2])
+        torch.cuda.synchronize()
+        for b in bits:
+            b.check(i)
+        assert all(torch.equal(a, r) for a, r in zip((norm, *out), ref))
