@@ -431,6 +431,70 @@ int moe_grad_norm(const moe_grad_t* grads, int32_t n, float* norm, void* ws, siz
 int moe_grad_clip(const moe_grad_t* grads, int32_t n, const float* norm, float max_norm, void* stream);
 
 /*
+ * What stands around the experts in a pre-norm block, x + drop(MoE(norm(x))).  Tensors of rows [n_rows, cols] have a row stride ld in values, at least cols (any value
+ * where there is one row), and need no alignment beyond that of a value.  Outputs may be inputs of the same call where that is said; otherwise tensors must not overlap.
+ *
+ * moe_dropout -- out = R + (kept ? X / (1 - p) : 0); R == NULL: no added term.  With X = the gradient of out and R == NULL it is its own adjoint.
+ *   The mask is not stored: value (row, col) is kept if its 16 bits are not below round(65536 p).  They are half-word col mod 8 (the low half of a word first) of
+ *   Philox4x32-10 of the counter (col / 8 + 65536 site, row, low word of step, high word of step) and the key (low word of seed, high word of seed).  p is thus a
+ *   multiple of 2^-16, and what is kept is scaled by 65536 / (65536 - round(65536 p)).  Dropped values add nothing, infinities and NaN neither.
+ *   rng [2] (device, 8-byte aligned): seed and step, read when the kernel runs; a captured graph draws other masks at every replay if a node of it, or the program
+ *   between replays, advances the step.  The forward and the backward pass must find the same values there.  Calls of one step that must not share a mask have sites of their own.
+ *   X, R, out in dtype (f32 or bf16), cols up to 2^18; out may be X or R (same address and stride).  p = 0 (less than 2^-17) adds only; rng may then be NULL.
+ *
+ * moe_norm_fwd -- Z = R + drop(X), rounded to dtype (without R and drop, Z = X: Z is then NULL);
+ *   MOE_NORM_LAYER: mean = sum Z / d, v = sum (Z - mean)^2 / d;   MOE_NORM_RMS: mean = 0, v = sum Z^2 / d;
+ *   rstd = 1 / sqrt(v + eps);   Y = (Z - mean) rstd w + b
+ *   w, b [d] in wdtype; NULL: ones, zeros.  mean, rstd [n_rows] f32 out, kept for the backward pass; either may be NULL (RMS has no mean).  1 <= d <= 16384.
+ *   Sums are fp32, the mean's own rounding error is taken out of Z - mean (in both passes), and Y is rounded once.  Z may be X or R, Y may be X.
+ * moe_norm_bwd -- g = dY w;  h = (Z - mean) rstd;  dZtotal = dZ + rstd (g - mean(g) [layer] - h mean(g h));
+ *   dR = dZtotal;  dX = drop'(dZtotal) (with drop: the mask of the forward pass; dX is then required and dR may be NULL);
+ *   dw = sum over rows of dY h,  db = sum over rows of dY  (wdtype; either may be NULL; with n_rows == 0 they are written as zeros)
+ *   dZ: the gradient that reaches Z by another way, the residual stream's; NULL: none.  dR may be dY or dZ, and so may dX, but not both the same.
+ *   ws >= moe_norm_bwd_workspace_bytes(norm) where dw or db is wanted (sums of the blocks, added in a fixed order: no atomics)
+ */
+enum { MOE_NORM_LAYER = 0, MOE_NORM_RMS = 1 };
+typedef struct moe_norm {
+  int32_t n_rows, d;
+  int32_t dtype, wdtype;  /* MOE_F32 or MOE_BF16 */
+  int32_t kind;
+  float eps;
+} moe_norm_t;
+typedef struct moe_drop {
+  float p;              /* 0 <= p < 1 - 2^-17 */
+  uint32_t site;        /* 0..65535 */
+  const uint64_t* rng;  /* device: seed, step */
+} moe_drop_t;
+int moe_dropout(const void* X, int64_t ldx, const void* R, int64_t ldr, int32_t dtype, int32_t n_rows, int32_t cols, const moe_drop_t* drop, void* out,
+                int64_t ldo, void* stream);
+size_t moe_norm_bwd_workspace_bytes(const moe_norm_t* norm);
+int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, const void* R, int64_t ldr, const moe_drop_t* drop, const void* w, const void* b,
+                 void* Z, int64_t ldz, void* Y, int64_t ldy, float* mean, float* rstd, void* stream);
+int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy, const void* Z, int64_t ldz, const void* w, const float* mean, const float* rstd,
+                 const void* dZ, int64_t lddz, const moe_drop_t* drop, void* dR, int64_t lddr, void* dX, int64_t lddx, void* dw, void* db, void* ws,
+                 size_t ws_bytes, void* stream);
+
+/*
+ * moe_seq_loss / moe_seq_loss_bwd -- the balance loss over each sequence instead of the batch (moe_aux_loss), the loads per sequence, and the router's z loss.
+ *   Sequence s owns the T_s = seq_len[s] tokens from seq_start[s] on (seq_len NULL: up to seq_start[s + 1]; seq_start then has n_seqs + 1 entries).  Sequences are in
+ *   ascending order and do not overlap (a length beyond the next start or T counts as up to there); they may be empty, and tokens between or behind them (padding) belong
+ *   to none: their logits and topk_idx are not looked at.  seq_start == NULL: one sequence of all T tokens.  S' = sequences with tokens, T' = their tokens.
+ *   counts[s, e] = how often topk_idx names e in sequence s;  f = counts / (k T_s);  P[s, e] = mean of p_te over its tokens, p_t the gate's scores as shares of one
+ *   (as in moe_aux_loss);  0 for empty sequences
+ *   loss[0] = alpha / S' sum_s E sum_e f_se P_se;    loss[1] = beta / T' sum_t lse_t^2, lse_t = log sum_e exp(logits_te)   (0 without tokens)
+ *   Backward, the loads held constant: dlogits of dloss (loss[0] + loss[1]); rows of no sequence get zeros, or nothing when accumulate != 0.
+ *   Rows whose logits are all -inf (sigmoid: whose scores are all 0 in fp32) have shares and lse 0; other rows may hold -inf.  topk_idx outside 0..E-1 is not counted.
+ *   logits, dlogits [T, E] f32; topk_idx [T, k]; seq_start, seq_len i32 (device); counts [n_seqs, E] i32 out; P [n_seqs, E] f32 out; loss [2] f32 out;
+ *   coef [n_seqs + 1] f32 out: alpha E / (S' k T_s^2) for every sequence, 2 beta / T': what the backward pass takes from the forward pass, besides counts.
+ *   shape gives T, E, k and gate.  ws >= moe_seq_loss_workspace_bytes(shape, n_seqs).  All sums in a fixed order: two calls give the same bits.
+ */
+size_t moe_seq_loss_workspace_bytes(const moe_shape_t* shape, int32_t n_seqs);
+int moe_seq_loss(const moe_shape_t* shape, const float* logits, const int32_t* topk_idx, int32_t n_seqs, const int32_t* seq_start, const int32_t* seq_len,
+                 float alpha, float beta, int32_t* counts, float* P, float* loss, float* coef, void* ws, size_t ws_bytes, void* stream);
+int moe_seq_loss_bwd(const moe_shape_t* shape, const float* logits, int32_t n_seqs, const int32_t* seq_start, const int32_t* seq_len, const int32_t* counts,
+                     const float* coef, float dloss, int32_t accumulate, float* dlogits, void* stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the hot path; off by default).
  * moe_profile_enable(1) clears earlier records and makes every later kernel launch of this
  * library be bracketed by two HIP events on the launch's own stream; moe_profile_enable(0)

@@ -15,6 +15,7 @@ _lib = None
 
 MOE_F32, MOE_BF16 = 0, 1
 MOE_GATE_SOFTMAX, MOE_GATE_SIGMOID = 0, 1
+MOE_NORM_LAYER, MOE_NORM_RMS = 0, 1
 EXPORTS = ["moe_abi_version", "moe_last_error", "moe_route_bwd", "moe_router_fwd", "moe_router_bwd",
            "moe_router_fwd_workspace_bytes", "moe_router_bwd_workspace_bytes", "moe_dispatch_workspace_bytes", "moe_expert_fwd_workspace_bytes",
            "moe_expert_bwd_workspace_bytes", "moe_route", "moe_dispatch", "moe_expert_fwd", "moe_expert_bwd",
@@ -26,7 +27,9 @@ EXPORTS = ["moe_abi_version", "moe_last_error", "moe_route_bwd", "moe_router_fwd
            "moe_experts_bwd", "moe_expert_plan_bytes", "moe_route_dispatch_plan",
            "moe_quant_row_bytes", "moe_quant_scale_bytes", "moe_quant_rows", "moe_quant_weights", "moe_quant_gemm_workspace_bytes",
            "moe_quant_gemm", "moe_quant_expert_fwd_workspace_bytes", "moe_quant_expert_bwd_workspace_bytes", "moe_quant_expert_fwd",
-           "moe_quant_expert_bwd", "moe_grad_norm_workspace_bytes", "moe_grad_norm", "moe_grad_clip"]
+           "moe_quant_expert_bwd", "moe_grad_norm_workspace_bytes", "moe_grad_norm", "moe_grad_clip",
+           "moe_dropout", "moe_norm_bwd_workspace_bytes", "moe_norm_fwd", "moe_norm_bwd",
+           "moe_seq_loss_workspace_bytes", "moe_seq_loss", "moe_seq_loss_bwd"]
 
 
 class MoEError(RuntimeError):
@@ -54,6 +57,14 @@ class _CGrad(ctypes.Structure):   # moe_grad_t
                 ("slot", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
+class _CNorm(ctypes.Structure):   # moe_norm_t
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_rows", "d", "dtype", "wdtype", "kind")] + [("eps", ctypes.c_float)]
+
+
+class _CDrop(ctypes.Structure):   # moe_drop_t
+    _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("rng", ctypes.c_void_p)]
+
+
 @dataclasses.dataclass(frozen=True)
 class MoEShape:
     T: int
@@ -76,6 +87,47 @@ class MoEShape:
     @property
     def torch_dtype(self) -> torch.dtype:
         return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+
+@dataclasses.dataclass(frozen=True)
+class MoENorm:
+    """Rows and kind of a norm (moe_norm_t)."""
+    n_rows: int
+    d: int
+    kind: str = "layer"      # "layer" | "rms"
+    eps: float = 1e-5
+    dtype: str = "bf16"      # rows: "f32" | "bf16"
+    wdtype: str = ""         # weights and their gradients; "": as the rows
+
+    def __post_init__(self):
+        for value, known in ((self.kind, ("layer", "rms")), (self.dtype, ("f32", "bf16")), (self.wdtype, ("", "f32", "bf16"))):
+            if value not in known:
+                raise MoEError(f"MoENorm: {value!r} is none of {known}")
+        code = {"f32": MOE_F32, "bf16": MOE_BF16}
+        wdtype = self.wdtype or self.dtype
+        types = {"f32": torch.float32, "bf16": torch.bfloat16}
+        # (made once: the members never change)
+        object.__setattr__(self, "c", _CNorm(self.n_rows, self.d, code[self.dtype], code[wdtype],
+                                             MOE_NORM_LAYER if self.kind == "layer" else MOE_NORM_RMS, self.eps))
+        object.__setattr__(self, "ref", ctypes.byref(self.c))
+        object.__setattr__(self, "torch_dtype", types[self.dtype])
+        object.__setattr__(self, "weight_dtype", types[wdtype])
+
+
+class MoEDropout:
+    """A dropout of probability p (moe_drop_t).  rng: int64 [2] on the GPU, seed and step, which the kernels read when they run: the program advances the step
+    (rng[1] += 1) once the backward pass has run.  Calls of one step that must not share a mask have sites of their own."""
+
+    def __init__(self, p: float, rng: Optional[torch.Tensor], site: int = 0):
+        if not 0 <= site < 1 << 16:
+            raise MoEError(f"dropout site {site} (0 to 65535)")
+        if rng is not None:
+            if rng.shape != (2,):
+                raise MoEError(f"the dropout's rng must have shape (2,), got {tuple(rng.shape)}")
+            _ptr(rng, torch.int64, "the dropout's rng")
+        self.p, self.rng, self.site = float(p), rng, int(site)
+        self.c = _CDrop(self.p, self.site, rng.data_ptr() if rng is not None else None)
+        self.ref = ctypes.byref(self.c)
 
 
 def lib_path() -> str:
@@ -177,6 +229,21 @@ def load_library():
     lib.moe_grad_norm.argtypes = [grads, i32, vp, vp, sz, vp]
     lib.moe_grad_clip.restype = ctypes.c_int
     lib.moe_grad_clip.argtypes = [grads, i32, vp, ctypes.c_float, vp]
+    nrm, drp = ctypes.POINTER(_CNorm), ctypes.POINTER(_CDrop)
+    lib.moe_dropout.restype = ctypes.c_int
+    lib.moe_dropout.argtypes = [vp, i64, vp, i64, i32, i32, i32, drp, vp, i64, vp]
+    lib.moe_norm_bwd_workspace_bytes.restype = sz
+    lib.moe_norm_bwd_workspace_bytes.argtypes = [nrm]
+    lib.moe_norm_fwd.restype = ctypes.c_int
+    lib.moe_norm_fwd.argtypes = [nrm, vp, i64, vp, i64, drp, vp, vp, vp, i64, vp, i64, vp, vp, vp]
+    lib.moe_norm_bwd.restype = ctypes.c_int
+    lib.moe_norm_bwd.argtypes = [nrm, vp, i64, vp, i64, vp, vp, vp, vp, i64, drp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.moe_seq_loss_workspace_bytes.restype = sz
+    lib.moe_seq_loss_workspace_bytes.argtypes = [shp, i32]
+    lib.moe_seq_loss.restype = ctypes.c_int
+    lib.moe_seq_loss.argtypes = [shp, vp, vp, i32, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp, vp, vp, sz, vp]
+    lib.moe_seq_loss_bwd.restype = ctypes.c_int
+    lib.moe_seq_loss_bwd.argtypes = [shp, vp, i32, vp, vp, vp, vp, ctypes.c_float, i32, vp, vp]
     lib.moe_combine.restype = ctypes.c_int
     lib.moe_combine.argtypes = [shp, vp, vp, vp, vp, vp, vp]
     lib.moe_combine_bwd.restype = ctypes.c_int
@@ -791,6 +858,117 @@ def moe_grad_clip(grads, norm, max_norm: float, out=None, stream=None):
     _here("moe_grad_clip", norm)
     rc = load_library().moe_grad_clip(_grad_list(grads, out), len(grads), _ptr(norm, torch.float32, "norm"), float(max_norm), _stream(stream))
     _check(rc, "moe_grad_clip")
+
+
+# ---- what stands around the experts: dropout, norms, the sequences' balance loss
+def _rows(t, n, d, dtype, device, what):
+    """Pointer and row stride of a tensor of rows [n, d]; its rows may be pieces of longer ones."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.get_device() != device or t.shape != (n, d):
+        raise MoEError(f"{what} must be a {dtype} tensor of shape {(n, d)} on cuda:{device}, the current device; got {t.dtype}, {tuple(t.shape)}, {t.device}")
+    ld, one = t.stride()
+    if (one != 1 and d > 1) or (ld < d and n > 1):
+        raise MoEError(f"{what}: the values of a row must be adjacent, and rows must not overlap")
+    return t.data_ptr(), ld if n > 1 else d
+
+
+def _vector(t, n, dtype, device, what):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        raise MoEError(f"{what} must be a contiguous {dtype} tensor of {n} values on cuda:{device}, the current device; got {t.dtype}, {tuple(t.shape)}, {t.device}")
+    return t.data_ptr()
+
+
+def _drop(drop, device, who):
+    if drop is None:
+        return None
+    if drop.rng is not None and drop.rng.get_device() != device:
+        raise MoEError(f"{who}: the dropout's rng is on {drop.rng.device}, the current device is cuda:{device}")
+    return drop.ref
+
+
+def _workspace(ws, device, who):
+    if ws is None:
+        return None, 0
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise MoEError(f"{who}: ws must be contiguous and on cuda:{device}, the current device; it is on {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def moe_dropout(X, drop: MoEDropout, out, R=None, stream=None):
+    """out = R + dropout of X [n_rows, cols] (f32 or bf16; rows may be strided); with R None and X the gradient of out, the gradient of X."""
+    code = _value_dtype(X, "X")
+    if X.dim() != 2:
+        raise MoEError("X must be [n_rows, cols]")
+    dt, (n, d), device = X.dtype, X.shape, torch.cuda.current_device()
+    rc = load_library().moe_dropout(*_rows(X, n, d, dt, device, "X"), *_rows(R, n, d, dt, device, "R"), code, n, d, _drop(drop, device, "moe_dropout"),
+                                    *_rows(out, n, d, dt, device, "out"), _stream(stream))
+    if rc:
+        _check(rc, "moe_dropout")
+
+
+def moe_norm_bwd_workspace_bytes(norm: MoENorm) -> int:
+    return int(load_library().moe_norm_bwd_workspace_bytes(norm.ref))
+
+
+def moe_norm_fwd(norm: MoENorm, X, w, b, Y, mean=None, rstd=None, R=None, drop: Optional[MoEDropout] = None, Z=None, stream=None):
+    """Y = norm(Z) w + b, Z = R + drop(X) (without R and drop: X, and no Z).  mean and rstd [n_rows]: kept for moe_norm_bwd."""
+    n, d, dt, wt, device = norm.n_rows, norm.d, norm.torch_dtype, norm.weight_dtype, torch.cuda.current_device()
+    f32 = torch.float32
+    rc = load_library().moe_norm_fwd(norm.ref, *_rows(X, n, d, dt, device, "X"), *_rows(R, n, d, dt, device, "R"), _drop(drop, device, "moe_norm_fwd"),
+                                     _vector(w, d, wt, device, "w"), _vector(b, d, wt, device, "b"), *_rows(Z, n, d, dt, device, "Z"),
+                                     *_rows(Y, n, d, dt, device, "Y"), _vector(mean, n, f32, device, "mean"), _vector(rstd, n, f32, device, "rstd"),
+                                     _stream(stream))
+    if rc:
+        _check(rc, "moe_norm_fwd")
+
+
+def moe_norm_bwd(norm: MoENorm, dY, Z, w, mean, rstd, dR, dw, db, ws, dZ=None, drop: Optional[MoEDropout] = None, dX=None, stream=None):
+    """dR = dZ + the norm's gradient at Z; with drop, dX = the dropout's of that; dw, db: the weights' (either may be None; both None: no ws)."""
+    n, d, dt, wt, device = norm.n_rows, norm.d, norm.torch_dtype, norm.weight_dtype, torch.cuda.current_device()
+    f32 = torch.float32
+    rc = load_library().moe_norm_bwd(norm.ref, *_rows(dY, n, d, dt, device, "dY"), *_rows(Z, n, d, dt, device, "Z"), _vector(w, d, wt, device, "w"),
+                                     _vector(mean, n, f32, device, "mean"), _vector(rstd, n, f32, device, "rstd"), *_rows(dZ, n, d, dt, device, "dZ"),
+                                     _drop(drop, device, "moe_norm_bwd"), *_rows(dR, n, d, dt, device, "dR"), *_rows(dX, n, d, dt, device, "dX"),
+                                     _vector(dw, d, wt, device, "dw"), _vector(db, d, wt, device, "db"), *_workspace(ws, device, "moe_norm_bwd"),
+                                     _stream(stream))
+    if rc:
+        _check(rc, "moe_norm_bwd")
+
+
+def moe_seq_loss_workspace_bytes(shape: MoEShape, n_seqs: int) -> int:
+    return int(load_library().moe_seq_loss_workspace_bytes(ctypes.byref(shape.c()), n_seqs))
+
+
+def _seqs(seq_start, seq_len, n, device):
+    i32 = torch.int32
+    return (_vector(seq_start, n + (seq_len is None), i32, device, "seq_start"), _vector(seq_len, n, i32, device, "seq_len"))
+
+
+def moe_seq_loss(shape: MoEShape, logits, topk_idx, seq_start, seq_len, alpha, beta, counts, P, loss, coef, ws, stream=None):
+    """Balance loss of every sequence (weight alpha) and z loss (beta): loss [2], counts and P [n_seqs, E], coef [n_seqs + 1] for the backward pass.  seq_start and
+    seq_len [n_seqs]; seq_len None: seq_start [n_seqs + 1]; both None: one sequence of all tokens."""
+    T, E, device = shape.T, shape.E, torch.cuda.current_device()
+    n, i32, f32 = counts.shape[0], torch.int32, torch.float32
+    rc = load_library().moe_seq_loss(ctypes.byref(shape.c()), _vector(logits, T * E, f32, device, "logits"), _vector(topk_idx, T * shape.k, i32, device, "topk_idx"),
+                                     n, *_seqs(seq_start, seq_len, n, device), alpha, beta, _vector(counts, n * E, i32, device, "counts"),
+                                     _vector(P, n * E, f32, device, "P"), _vector(loss, 2, f32, device, "loss"), _vector(coef, n + 1, f32, device, "coef"),
+                                     *_workspace(ws, device, "moe_seq_loss"), _stream(stream))
+    if rc:
+        _check(rc, "moe_seq_loss")
+
+
+def moe_seq_loss_bwd(shape: MoEShape, logits, seq_start, seq_len, counts, coef, dloss, accumulate, dlogits, stream=None):
+    """dlogits (+)= the gradient of dloss (loss[0] + loss[1]), the loads held constant; rows of no sequence get zeros (accumulate: are left as they are)."""
+    T, E, device = shape.T, shape.E, torch.cuda.current_device()
+    n, i32, f32 = counts.shape[0], torch.int32, torch.float32
+    rc = load_library().moe_seq_loss_bwd(ctypes.byref(shape.c()), _vector(logits, T * E, f32, device, "logits"), n, *_seqs(seq_start, seq_len, n, device),
+                                         _vector(counts, n * E, i32, device, "counts"), _vector(coef, n + 1, f32, device, "coef"), dloss,
+                                         bool(accumulate), _vector(dlogits, T * E, f32, device, "dlogits"), _stream(stream))
+    if rc:
+        _check(rc, "moe_seq_loss_bwd")
 
 
 def moe_copy_probe(src: torch.Tensor, dst: torch.Tensor):
