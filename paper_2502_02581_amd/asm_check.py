@@ -167,7 +167,7 @@ def check_mfma_sources(lines: List[str], wait_states: int = 2) -> List[str]:
 
 # every kernel of the GEMM sources: row_gemm_, row_w_gemm_, wide_*_gemm_, the light weight gradients and the sums of parts;
 # and the streams of the quantisation and of the clipping
-NO_SCRATCH = ("gemm_kernel", "w_light_kernel", "reduce_kernel", "quant_rows_kernel", "quant_matrix_kernel", "grad_", "dropout_kernel", "seq_")
+NO_SCRATCH = ("gemm_kernel", "w_light_kernel", "reduce_kernel", "quant_rows_kernel", "quant_matrix_kernel", "grad_", "norm_", "dropout_kernel", "seq_")
 
 
 def check_no_scratch(lines: List[str], name_parts=NO_SCRATCH) -> List[str]:

@@ -45,13 +45,18 @@ __device__ __forceinline__ void load_weights(const void* w, int wf32, int col, i
   }
 }
 
-// The mean's rounding error would be that of every value of the row: delta, the mean of z - m, puts it right, so that rows far from zero (mean 1e4, deviation 1, fp32)
-// lose nothing but what their own values have lost.
+// Rows far from zero: the rounding error of the mean would be that of every value of the row.  delta, the mean of z - m, puts it right, so that they lose nothing but
+// what their own values have lost (mean 1e4, deviation 1, fp32).  Where the mean is below the deviation its error is below the deviation's, and delta would bring in the
+// roundings of z - m, which have one sign for all z of a binade; there it is left out.
 enum { kPlain = 0, kAdd = 1, kDrop = 2 };
 
-// WIDE: a block is a team; otherwise each of its wavefronts is one.
-template <typename T, int V, bool WIDE, int MODE>
-__global__ __launch_bounds__(V == 1 ? 1024 : V == 2 ? 512 : 512) void norm_fwd_kernel(NormFwd a) {
+// TEAM: who works on a row.  A wavefront of the block's four; the block; or (rows of more than 8192 values) a block of up to sixteen wavefronts, whose lanes have too few
+// registers to hold the next row as well, or, in the backward pass, this one.
+enum { kWaveTeam = 0, kBlockTeam = 1, kLongTeam = 2 };
+
+template <typename T, int V, int TEAM, int MODE>
+__global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_fwd_kernel(NormFwd a) {
+  constexpr bool WIDE = TEAM != kWaveTeam;
   __shared__ RowSums<2> sums;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
   const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? gridDim.x : gridDim.x * n_waves;
@@ -69,30 +74,41 @@ __global__ __launch_bounds__(V == 1 ? 1024 : V == 2 ? 512 : 512) void norm_fwd_k
     load_weights(a.b, a.wf32, col, valid[v], 0.f, b[v]);
   }
   const float inv_d = 1.f / (float)a.d;
+  Piece<T> x[V], r[V];  // the next row: its loads are under way while the one before is worked on
+  auto load = [&](int row) {
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const int col = 8 * (first + v * step);
+      load_piece(x[v], X + row * a.ldx + col, valid[v]);
+      if (MODE != kPlain) {
+        r[v].clear();
+        if (R) load_piece(r[v], R + row * a.ldr + col, valid[v]);
+      }
+    }
+  };
+  if (TEAM != kLongTeam && team < a.n_rows) load(team);
   for (int row = team; row < a.n_rows; row += n_teams) {
+    if (TEAM == kLongTeam) load(row);
     float z[V][8];
 #pragma unroll
     for (int v = 0; v < V; v++) {
       const int c = first + v * step;
-      Piece<T> x, r;
-      load_piece(x, X + row * a.ldx + 8 * c, valid[v]);
+      x[v].values(z[v]);
       if (MODE != kPlain) {
-        r.clear();
-        if (R) load_piece(r, R + row * a.ldr + 8 * c, valid[v]);
         float add[8];
-        x.values(z[v]);
-        r.values(add);
+        r[v].values(add);
         if (MODE == kDrop) {
           drop_piece(a.drop, key, c, row, z[v], add);
         } else {
 #pragma unroll
           for (int j = 0; j < 8; j++) z[v][j] += add[j];
         }
-        x.set(z[v]);  // the norm is of the values that are kept
-        store_piece(x, Z + row * a.ldz + 8 * c, valid[v]);
+        x[v].set(z[v]);  // the norm is of the values that are kept
+        store_piece(x[v], Z + row * a.ldz + 8 * c, valid[v]);
+        x[v].values(z[v]);
       }
-      x.values(z[v]);
     }
+    if (TEAM != kLongTeam && row + n_teams < a.n_rows) load(row + n_teams);
     float m = 0.f, delta = 0.f, var;
     if (a.layer) {
       float s[1] = {0.f};
@@ -120,9 +136,11 @@ __global__ __launch_bounds__(V == 1 ? 1024 : V == 2 ? 512 : 512) void norm_fwd_k
         t[0] = lanes_sum(t[0]);
         t[1] = lanes_sum(t[1]);
       }
-      delta = t[0] * inv_d;
-      var = fmaxf(t[1] / (float)a.d - delta * delta, 0.f);
-      if (!(t[1] == t[1])) var = t[1];  // (the maximum would lose a NaN)
+      var = t[1] / (float)a.d;
+      if (m * m > var) {
+        delta = t[0] * inv_d;
+        var -= delta * delta;
+      }
     } else {
       float t[1] = {0.f};
 #pragma unroll
@@ -149,8 +167,9 @@ __global__ __launch_bounds__(V == 1 ? 1024 : V == 2 ? 512 : 512) void norm_fwd_k
   }
 }
 
-template <typename T, int V, bool WIDE, bool DROP>
-__global__ __launch_bounds__(V == 1 ? 1024 : 512) void norm_bwd_kernel(NormBwd a) {
+template <typename T, int V, int TEAM, bool DROP>
+__global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : 1024) void norm_bwd_kernel(NormBwd a) {
+  constexpr bool WIDE = TEAM != kWaveTeam;
   __shared__ RowSums<3> sums;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
   const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? gridDim.x : gridDim.x * n_waves;
@@ -169,30 +188,85 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 512) void norm_bwd_kernel(NormBwd a
     for (int j = 0; j < 8; j++) dw[v][j] = db[v][j] = 0.f;
   }
   const float inv_d = 1.f / (float)a.d;
-  for (int row = team; row < a.n_rows; row += n_teams) {
-    Piece<T> y[V], z[V], in[V];
+  struct Loads {
+    Piece<T> y, z, in;
+  };
+  auto load = [&](Loads& p, int row, int v, bool all) {
+    const int col = 8 * (first + v * step);
+    load_piece(p.y, dY + row * a.lddy + col, valid[v]);
+    load_piece(p.z, Z + row * a.ldz + col, valid[v]);
+    if (all && dZ) load_piece(p.in, dZ + row * a.lddz + col, valid[v]);
+    else p.in.clear();
+  };
+  float s[3];  // sums of g, of g (z - m) and, for the mean's rounding error as in the forward pass, of z - m
+  float m = 0.f, rstd = 0.f;
+  auto add = [&](const Loads& p, int v) {
+    float dy[8], x[8];
+    p.y.values(dy);
+    p.z.values(x);
 #pragma unroll
-    for (int v = 0; v < V; v++) {
-      const int col = 8 * (first + v * step);
-      load_piece(y[v], dY + row * a.lddy + col, valid[v]);
-      load_piece(z[v], Z + row * a.ldz + col, valid[v]);
-      if (dZ) load_piece(in[v], dZ + row * a.lddz + col, valid[v]);
-      else in[v].clear();
+    for (int j = 0; j < 8; j++) {
+      const float g = dy[j] * w[v][j], c = x[j] - m;
+      s[0] += g;
+      s[1] = fmaf(g, c, s[1]);
+      s[2] += j < valid[v] ? c : 0.f;
     }
-    const float m = a.layer ? a.mean[row] : 0.f, rstd = a.rstd[row];
-    // sums of g, of g (z - m) and, for the mean's rounding error as in the forward pass, of z - m
-    float s[3] = {0.f, 0.f, 0.f};
+  };
+  float delta, s1, s2;
+  auto finish = [&](const Loads& p, int row, int v) {
+    const int c = first + v * step;
+    float dy[8], x[8], o[8];
+    p.y.values(dy);
+    p.z.values(x);
+    p.in.values(o);
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      const float h = ((x[j] - m) - delta) * rstd;
+      o[j] = fmaf(rstd, dy[j] * w[v][j] - s1 - h * s2, o[j]);
+      dw[v][j] = fmaf(dy[j], h, dw[v][j]);
+      db[v][j] += dy[j];
+    }
+    Piece<T> out;
+    if (dR) {
+      out.set(o);
+      store_piece(out, dR + row * a.lddr + 8 * c, valid[v]);
+    }
+    if (DROP) {
+      const float zero[8] = {};
+      drop_piece(a.drop, key, c, row, o, zero);
+      out.set(o);
+      store_piece(out, dX + row * a.lddx + 8 * c, valid[v]);
+    }
+  };
+  Loads next[V];  // the next row: its loads are under way while the one before is worked on
+  float next_m = 0.f, next_rstd = 0.f;
+  auto load_row = [&](int row) {
+    if (TEAM != kLongTeam) {
+#pragma unroll
+      for (int v = 0; v < V; v++) load(next[v], row, v, true);
+    }
+    next_m = a.layer ? a.mean[row] : 0.f;
+    next_rstd = a.rstd[row];
+  };
+  if (team < a.n_rows) load_row(team);
+  for (int row = team; row < a.n_rows; row += n_teams) {
+    Loads now[V];
+    m = next_m;
+    rstd = next_rstd;
+    if (TEAM != kLongTeam) {
+#pragma unroll
+      for (int v = 0; v < V; v++) now[v] = next[v];
+    }
+    if (row + n_teams < a.n_rows) load_row(row + n_teams);
+    s[0] = s[1] = s[2] = 0.f;
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      float dy[8], x[8];
-      y[v].values(dy);
-      z[v].values(x);
-#pragma unroll
-      for (int j = 0; j < 8; j++) {
-        const float g = dy[j] * w[v][j], c = x[j] - m;
-        s[0] += g;
-        s[1] = fmaf(g, c, s[1]);
-        s[2] += j < valid[v] ? c : 0.f;
+      if (TEAM == kLongTeam) {
+        Loads p;
+        load(p, row, v, false);
+        add(p, v);
+      } else {
+        add(now[v], v);
       }
     }
     if (WIDE) {
@@ -201,35 +275,19 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 512) void norm_bwd_kernel(NormBwd a
 #pragma unroll
       for (int i = 0; i < 3; i++) s[i] = lanes_sum(s[i]);
     }
-    const float delta = a.layer ? s[2] * inv_d : 0.f, centre = m + delta;
-    const float s1 = a.layer ? s[0] * inv_d : 0.f, s2 = (s[1] - delta * s[0]) * rstd * inv_d;
+    delta = fabsf(m) * rstd > 1.f ? s[2] * inv_d : 0.f;  // (no mean, no delta)
+    s1 = a.layer ? s[0] * inv_d : 0.f;
+    s2 = (s[1] - delta * s[0]) * rstd * inv_d;
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      const int c = first + v * step;
-      float dy[8], x[8], o[8];
-      y[v].values(dy);
-      z[v].values(x);
-      in[v].values(o);
-#pragma unroll
-      for (int j = 0; j < 8; j++) {
-        const float h = ((x[j] - m) - delta) * rstd;
-        o[j] = fmaf(rstd, dy[j] * w[v][j] - s1 - h * s2, o[j]);
-        dw[v][j] = fmaf(dy[j], h, dw[v][j]);
-        db[v][j] += dy[j];
-      }
-      Piece<T> out;
-      if (dR) {
-        out.set(o);
-        store_piece(out, dR + row * a.lddr + 8 * c, valid[v]);
-      }
-      if (DROP) {
-        const float zero[8] = {};
-        drop_piece(a.drop, key, c, row, o, zero);
-        out.set(o);
-        store_piece(out, dX + row * a.lddx + 8 * c, valid[v]);
+      if (TEAM == kLongTeam) {
+        Loads p;
+        load(p, row, v, true);
+        finish(p, row, v);
+      } else {
+        finish(now[v], row, v);
       }
     }
-    (void)centre;
   }
   if (!a.partial) return;
   if (WIDE) {
@@ -267,43 +325,56 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 512) void norm_bwd_kernel(NormBwd a
   }
 }
 
-// dw (blockIdx.y = 0) and db (1) from the blocks' sums: 32 columns x 8 runs, in a fixed order
-__global__ __launch_bounds__(256) void norm_weights_kernel(const float* partial, int blocks, int d, int wf32, void* dw, void* db) {
-  __shared__ float part[8][32];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;
+// dw (blockIdx.y = 0) and db (1) from the blocks' sums: 32 columns x 32 runs, in a fixed order
+__global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial, int blocks, int d, int wf32, void* dw, void* db) {
+  __shared__ float part[16][32];
   void* out = blockIdx.y ? db : dw;
   if (!out) return;
+  const int lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (col < d) {
     const float* p = partial + (size_t)blockIdx.y * d + col;
-#pragma unroll 8
-    for (int q = run; q < blocks; q += 8) s += p[(size_t)q * 2 * d];
+#pragma unroll 16
+    for (int q = threadIdx.x >> 5; q < blocks; q += 32) s += p[(size_t)q * 2 * d];
   }
-  part[run][threadIdx.x & 31] = s;
+  s = add_rows32(s);
+  if ((threadIdx.x & 63) < 32) part[threadIdx.x >> 6][lane] = s;
   __syncthreads();
-  if (run == 0 && col < d) {
+  if (threadIdx.x < 32 && col < d) {
     float t = 0.f;
 #pragma unroll
-    for (int r = 0; r < 8; r++) t += part[r][threadIdx.x & 31];
+    for (int r = 0; r < 16; r++) t += part[r][lane];
     if (wf32) ((float*)out)[col] = t;
     else Elem<bf16_t>::store((bf16_t*)out + col, t);
   }
 }
 
-// pieces of a lane, wavefronts of a row
+// Pieces of a lane, wavefronts of a row, blocks.  Measured (T rows of d, bf16 unless it says otherwise):
+//  - rows of up to 1024 values take a wavefront (16384 x 768 backward: 18.5 us, with a block of two wavefronts 20.2), four a block;
+//  - longer ones a block whose lanes hold one piece, in the forward pass of long rows two, where there are many (8192 x 7168: 44.0 us for 49.6, 8192 x 2048: 20.4 for 18.5,
+//    500 x 4096: 5.9 for 5.1): half as many wavefronts take part in a row's two barriers;
+//  - 16 wavefronts a unit, each with the next row's loads under way, reach the copy's rate.  The backward pass takes fewer blocks where they would get less than four
+//    rows (six, for teams of a wavefront): their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks 9.7 + 3.4 us, 1024 11.0 + 5.0, 256 12.2 + 4.1).
 struct NormPlan {
-  int V, waves, blocks;  // waves == 1: four teams in a block
+  int V, team, waves, blocks;
 };
 static NormPlan norm_plan(const moe_norm_t* n, bool backward) {
-  const int pieces = (n->d + 7) / 8;
+  const int pieces = (n->d + 7) / 8, rows = n->n_rows;
+  const auto at_most = [](int x, int most) { return x < most ? x : most; };
   NormPlan p;
-  if (pieces <= 64) p = {1, 1, 0};
-  else if (pieces <= 128) p = {2, 1, 0};
-  else if (pieces <= 1024) p = {2, (pieces + 127) / 128, 0};
-  else p = {4, (pieces + 255) / 256, 0};
-  const int rows = p.waves == 1 ? (n->n_rows + 3) / 4 : n->n_rows;
-  const int most = backward ? 512 : 2048;
-  p.blocks = rows < most ? rows : most;
+  if (pieces <= 128) {
+    p = {pieces <= 64 ? 1 : 2, kWaveTeam, 4, at_most((rows + 3) / 4, 2048)};
+    if (backward) p.blocks = at_most((rows + 3) / 4, at_most(rows / 6 + 64, 768));
+    return p;
+  }
+  const bool two = pieces > 1024 || (!backward && pieces > 256 && rows > 1024);
+  p.V = two ? 2 : 1;
+  p.team = pieces > 1024 ? kLongTeam : kBlockTeam;
+  p.waves = (pieces + 64 * p.V - 1) / (64 * p.V);
+  p.blocks = 4096 / p.waves / 256 * 256;  // 256 units, the same number of blocks each
+  if (p.blocks > 2048) p.blocks = 2048;
+  if (backward) p.blocks = at_most(p.blocks, rows / 4 + 64);
+  p.blocks = at_most(p.blocks, rows);
   return p;
 }
 
@@ -363,24 +434,26 @@ extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, 
   const NormPlan p = norm_plan(norm, false);
   const NormFwd a = {X, R, w, b, Z, Y, mean, rstd, ldx, ldr, ldz, ldy, n, d, norm->kind == MOE_NORM_LAYER, norm->wdtype == MOE_F32, norm->eps, dr};
   hipStream_t st = (hipStream_t)stream;
-  const dim3 grid(p.blocks), block(p.waves == 1 ? 256 : 64 * p.waves);
+  const dim3 grid(p.blocks), block(64 * p.waves);
   ProfScope prof("norm_fwd_kernel", st);
-#define MOE_NORM_FWD(T, V, WIDE)                                                                           \
-  do {                                                                                                     \
-    if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, V, WIDE, kPlain>), grid, block, 0, st, a);             \
-    else if (dr.threshold == 0) hipLaunchKernelGGL((norm_fwd_kernel<T, V, WIDE, kAdd>), grid, block, 0, st, a); \
-    else hipLaunchKernelGGL((norm_fwd_kernel<T, V, WIDE, kDrop>), grid, block, 0, st, a);                   \
+#define MOE_NORM_FWD_BY_PLAN(T)                                              \
+  do {                                                                       \
+    if (p.team == kLongTeam) MOE_NORM_FWD(T, 2, kLongTeam);                  \
+    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_FWD(T, 2, kBlockTeam); \
+    else if (p.team == kBlockTeam) MOE_NORM_FWD(T, 1, kBlockTeam);           \
+    else if (p.V == 2) MOE_NORM_FWD(T, 2, kWaveTeam);                        \
+    else MOE_NORM_FWD(T, 1, kWaveTeam);                                      \
   } while (0)
-#define MOE_NORM_BY_PLAN(CALL, T)                                   \
-  do {                                                              \
-    if (p.waves == 1 && p.V == 1) CALL(T, 1, false);                \
-    else if (p.waves == 1) CALL(T, 2, false);                       \
-    else if (p.V == 2) CALL(T, 2, true);                            \
-    else CALL(T, 4, true);                                          \
+#define MOE_NORM_FWD(T, V, TEAM)                                                                                \
+  do {                                                                                                          \
+    if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kPlain>), grid, block, 0, st, a);                  \
+    else if (dr.threshold == 0) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kAdd>), grid, block, 0, st, a); \
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kDrop>), grid, block, 0, st, a);                        \
   } while (0)
-  if (norm->dtype == MOE_F32) MOE_NORM_BY_PLAN(MOE_NORM_FWD, float);
-  else MOE_NORM_BY_PLAN(MOE_NORM_FWD, bf16_t);
+  if (norm->dtype == MOE_F32) MOE_NORM_FWD_BY_PLAN(float);
+  else MOE_NORM_FWD_BY_PLAN(bf16_t);
 #undef MOE_NORM_FWD
+#undef MOE_NORM_FWD_BY_PLAN
   return launch_status(who);
 }
 
@@ -421,20 +494,28 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
   if (n > 0) {
     const NormBwd a = {dY, Z, w, dZ, mean, rstd, dR, dX, weights ? (float*)ws : nullptr, lddy, ldz, lddz, lddr, lddx, n, d,
                        norm->kind == MOE_NORM_LAYER, norm->wdtype == MOE_F32, dr};
-    const dim3 grid(p.blocks), block(p.waves == 1 ? 256 : 64 * p.waves);
+    const dim3 grid(p.blocks), block(64 * p.waves);
     ProfScope prof("norm_bwd_kernel", st);
-#define MOE_NORM_BWD(T, V, WIDE)                                                                          \
+#define MOE_NORM_BWD(T, V, TEAM)                                                                          \
   do {                                                                                                    \
-    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, V, WIDE, true>), grid, block, 0, st, a);              \
-    else hipLaunchKernelGGL((norm_bwd_kernel<T, V, WIDE, false>), grid, block, 0, st, a);                  \
+    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, true>), grid, block, 0, st, a);              \
+    else hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, false>), grid, block, 0, st, a);                  \
   } while (0)
-    if (norm->dtype == MOE_F32) MOE_NORM_BY_PLAN(MOE_NORM_BWD, float);
-    else MOE_NORM_BY_PLAN(MOE_NORM_BWD, bf16_t);
+#define MOE_NORM_BWD_BY_PLAN(T)                                   \
+  do {                                                            \
+    if (p.team == kLongTeam) MOE_NORM_BWD(T, 2, kLongTeam);       \
+    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, 1, kBlockTeam); \
+    else if (p.V == 2) MOE_NORM_BWD(T, 2, kWaveTeam);             \
+    else MOE_NORM_BWD(T, 1, kWaveTeam);                           \
+  } while (0)
+    if (norm->dtype == MOE_F32) MOE_NORM_BWD_BY_PLAN(float);
+    else MOE_NORM_BWD_BY_PLAN(bf16_t);
+#undef MOE_NORM_BWD_BY_PLAN
 #undef MOE_NORM_BWD
   }
   if (weights) {
     ProfScope prof("norm_weights_kernel", st);
-    hipLaunchKernelGGL(norm_weights_kernel, dim3((d + 31) / 32, 2), dim3(256), 0, st, (const float*)ws, n > 0 ? p.blocks : 0, d, (int)(norm->wdtype == MOE_F32),
+    hipLaunchKernelGGL(norm_weights_kernel, dim3((d + 31) / 32, 2), dim3(1024), 0, st, (const float*)ws, n > 0 ? p.blocks : 0, d, (int)(norm->wdtype == MOE_F32),
                        dw, db);
   }
   return n > 0 || weights ? launch_status(who) : MOE_OK;

@@ -77,24 +77,31 @@ __device__ __forceinline__ void store_piece(const Piece<T>& x, T* p, int valid) 
 }
 
 // ---- sums.  Every lane adds in the same order as its partner, so all lanes end with the same bits.
-__device__ __forceinline__ float add_dpp(float x, const int ctrl) {
-  switch (ctrl) {  // (the control word has to be a constant)
-    case 0: return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xB1, 0xf, 0xf, true));   // lane ^ 1
-    case 1: return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4E, 0xf, 0xf, true));   // lane ^ 2
-    case 2: return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xf, 0xf, true));  // the other four of eight
-    default: return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, 0xf, 0xf, true)); // the other eight of sixteen
-  }
+template <int CONTROL, typename T> __device__ __forceinline__ T dpp(T x) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float add_lanes1(float x) { return x + dpp<0xB1>(x); }   // lane ^ 1
+__device__ __forceinline__ float add_lanes2(float x) { return x + dpp<0x4E>(x); }   // lane ^ 2
+__device__ __forceinline__ float add_lanes4(float x) { return x + dpp<0x141>(x); }  // the other four of eight, mirrored
+__device__ __forceinline__ float add_lanes8(float x) { return x + dpp<0x140>(x); }  // the other eight of sixteen, mirrored
+// lanes of sixteen whose numbers differ by 4, 8 or 12 (rotations by 8 and 4)
+template <typename T> __device__ __forceinline__ T add_quads(T x) {
+  x += dpp<0x128>(x);
+  return x + dpp<0x124>(x);
 }
 // over each sixteen neighbouring lanes
-__device__ __forceinline__ float row16_sum(float x) { return add_dpp(add_dpp(add_dpp(add_dpp(x, 0), 1), 2), 3); }
-// over the wavefront, without LDS (wave_sum's exchanges go through it)
-__device__ __forceinline__ float lanes_sum(float x) {
-  x = row16_sum(x);
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+__device__ __forceinline__ float row16_sum(float x) { return add_lanes8(add_lanes4(add_lanes2(add_lanes1(x)))); }
+// lane ^ 16, lane ^ 32
+template <typename T> __device__ __forceinline__ T add_rows16(T x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  return __builtin_bit_cast(T, (uint32_t)a[0]) + __builtin_bit_cast(T, (uint32_t)a[1]);
 }
+template <typename T> __device__ __forceinline__ T add_rows32(T x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  return __builtin_bit_cast(T, (uint32_t)a[0]) + __builtin_bit_cast(T, (uint32_t)a[1]);
+}
+// over the wavefront, without LDS (wave_sum's exchanges go through it)
+__device__ __forceinline__ float lanes_sum(float x) { return add_rows32(add_rows16(row16_sum(x))); }
 // N sums over the n_waves (up to 16) wavefronts of a block: one barrier.  `part` holds two sets that calls use in turn: who writes a set again has passed the
 // barrier of the call between, which nobody reaches before reading that set.
 template <int N>
