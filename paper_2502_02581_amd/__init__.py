@@ -14,7 +14,7 @@ from .binding import (MoEShape, MoEHotPath, lib_path, load_library, moe_abi_vers
                       MoEQuantWeights, moe_quant_row_bytes, moe_quant_scale_bytes, moe_quant_rows, moe_quant_weights,
                       moe_quant_gemm, moe_quant_gemm_workspace_bytes, moe_quant_expert_fwd, moe_quant_expert_bwd,
                       moe_quant_expert_fwd_workspace_bytes, moe_quant_expert_bwd_workspace_bytes, moe_grad_norm,
-                      moe_grad_norm_workspace_bytes, moe_grad_clip, MoENorm, MoEDropout, moe_dropout, moe_norm_fwd, moe_norm_bwd,
+                      moe_grad_norm_workspace_bytes, moe_grad_clip, MoEBlockWeights, MoENorm, MoEDropout, moe_dropout, moe_norm_fwd, moe_norm_bwd,
                       moe_norm_bwd_workspace_bytes, moe_seq_loss, moe_seq_loss_bwd, moe_seq_loss_workspace_bytes)
 
 __all__ = ["MoEShape", "MoEHotPath", "MoEError", "lib_path", "load_library", "moe_abi_version", "moe_last_error",
@@ -26,5 +26,5 @@ __all__ = ["MoEShape", "MoEHotPath", "MoEError", "lib_path", "load_library", "mo
            "MoEQuantWeights", "moe_quant_row_bytes", "moe_quant_scale_bytes", "moe_quant_rows", "moe_quant_weights",
            "moe_quant_gemm", "moe_quant_gemm_workspace_bytes", "moe_quant_expert_fwd", "moe_quant_expert_bwd",
            "moe_quant_expert_fwd_workspace_bytes", "moe_quant_expert_bwd_workspace_bytes", "moe_grad_norm",
-           "moe_grad_norm_workspace_bytes", "moe_grad_clip", "MoENorm", "MoEDropout", "moe_dropout", "moe_norm_fwd", "moe_norm_bwd",
+           "moe_grad_norm_workspace_bytes", "moe_grad_clip", "MoEBlockWeights", "MoENorm", "MoEDropout", "moe_dropout", "moe_norm_fwd", "moe_norm_bwd",
            "moe_norm_bwd_workspace_bytes", "moe_seq_loss", "moe_seq_loss_bwd", "moe_seq_loss_workspace_bytes"]

@@ -1007,6 +1007,14 @@ def moe_profile_report() -> Dict[str, tuple]:
     return out
 
 
+@dataclasses.dataclass
+class MoEBlockWeights:
+    """The weights of a block around its experts: the norm's [d] (norm_b may be None, and norm_w) and the router's Wr [d, E]."""
+    norm_w: Optional[torch.Tensor]
+    norm_b: Optional[torch.Tensor]
+    Wr: torch.Tensor
+
+
 class MoEHotPath:
     """Owns the device buffers of one layer and chains the C calls of a training step.
 
@@ -1032,10 +1040,23 @@ class MoEHotPath:
     Wg, and None for Wu and Wd.  Tokens and their gradients are quantised once, in their own order, and read in place.  Shared experts stay in
     bf16 and have no launches in common with the routed ones: their calls follow those, or, with overlap_shared, go to the second stream beside them (the
     training step above with quant 1.83 ms, with overlap_shared 1.76, in bf16 measured beside them 2.04).
+
+    With norm ("layer" or "rms") the layer is the whole pre-norm block, out = X + drop(MoE(norm(X))): forward() takes a MoEBlockWeights in the place of the logits, which
+    come from the router's linear map of the normed rows, and returns b["Out"]; backward() takes the gradient of that and returns the one of X, b["dZ"], with those of the
+    weights in b["dWr"], b["dnorm_w"], b["dnorm_b"].  Given residual, forward() adds X, the output of the sublayer before, to it first: Z = residual + drop(X),
+    out = Z + drop(MoE(norm(Z))); b["dZ"] is then the gradient of residual, and of X without dropout (with it, b["dBranch"]).  dropout: the probability; rng: int64 [2] on the
+    GPU, seed and step, of which the program advances the step after every backward pass (rng[1] += 1), in a captured graph, too; the block's two masks have the sites
+    site and site + 1.  norm_dtype: the norm weights' type ("f32" or "bf16"; the layer's).
+
+    With seq_alpha or z_beta, forward() also evaluates the balance loss of every sequence and the router's z loss (moe_seq_loss) into b["seq_loss"] [2], with b["seq_counts"],
+    b["seq_P"] [n_seqs, E], and backward() adds their gradient to dlogits.  seqs = (seq_start, seq_len) says which tokens are whose; without it all are one
+    sequence's.  Tokens of no sequence (padding) pass through the experts like any other and have no part in these losses.
     """
 
     def __init__(self, shape: MoEShape, n_shared: int = 0, d_ff_shared: int = 0, device="cuda:0",
-                 overlap_shared: bool = False, aux_alpha: float = 0.0, gather: bool = False, fused: bool = True, quant: bool = False):
+                 overlap_shared: bool = False, aux_alpha: float = 0.0, gather: bool = False, fused: bool = True, quant: bool = False,
+                 norm: Optional[str] = None, eps: float = 1e-5, norm_dtype: str = "", dropout: float = 0.0, rng: Optional[torch.Tensor] = None,
+                 site: int = 0, seq_alpha: float = 0.0, z_beta: float = 0.0, n_seqs: int = 1):
         self.shape, self.S, self.Fs, self.device = shape, n_shared, d_ff_shared, torch.device(device)
         self.gather = bool(gather)  # routed experts read X and dY through src_of (moe_expert_*_gather)
         # gate, dispatch and auxiliary loss through moe_route_dispatch / moe_route_aux_bwd (fewer launches)
@@ -1063,13 +1084,14 @@ class MoEHotPath:
             "dWg_c": torch.empty(s.E, s.d, s.d_ff, **f), "dWu_c": torch.empty(s.E, s.d, s.d_ff, **f),
             "dWd_c": torch.empty(s.E, s.d_ff, s.d, **f),
         }
+        around = self._around(norm, eps, norm_dtype, dropout, rng, site, seq_alpha, z_beta, n_seqs)
         self.ws_routed = max(moe_expert_fwd_workspace_bytes(s, s.E, A, False), moe_expert_bwd_workspace_bytes(s, s.E, A, False))
         if self.quant:
             rows = lambda: (torch.empty(s.T, moe_quant_row_bytes(s.d), dtype=torch.uint8, device=dev),
                             torch.empty(s.T, moe_quant_scale_bytes(s.d), dtype=torch.uint8, device=dev))
             (self.b["XQ"], self.b["XS"]), (self.b["dYQ"], self.b["dYS"]) = rows(), rows()
             self.ws_routed = max(self.ws_routed, moe_quant_expert_fwd_workspace_bytes(s, s.E, A), moe_quant_expert_bwd_workspace_bytes(s, s.E, A))
-        ws = max(moe_dispatch_workspace_bytes(s), moe_route_dispatch_workspace_bytes(s), self.ws_routed)
+        ws = max(moe_dispatch_workspace_bytes(s), moe_route_dispatch_workspace_bytes(s), self.ws_routed, around)
         if self.aux_alpha > 0:
             self.b.update({"aux_P": torch.empty(s.E, dtype=torch.float32, device=dev),
                            "aux_loss": torch.empty(1, dtype=torch.float32, device=dev)})
@@ -1099,6 +1121,54 @@ class MoEHotPath:
         self.plan_ids, self.plan_n_active = torch.empty_like(self.b["active_ids"]), torch.empty_like(self.b["n_active"])
         self.plan = torch.empty(moe_expert_plan_bytes(s), dtype=torch.uint8, device=dev)
 
+    def _around(self, norm, eps, norm_dtype, dropout, rng, site, seq_alpha, z_beta, n_seqs):
+        """The buffers of what stands around the experts; the bytes of workspace that it takes."""
+        s, b, dev = self.shape, self.b, self.device
+        f, f32 = dict(dtype=s.torch_dtype, device=dev), dict(dtype=torch.float32, device=dev)
+        ws = 0
+        self.norm, self.seq_alpha, self.z_beta = None, float(seq_alpha), float(z_beta)
+        self._block, self._seqs, self._added = None, (None, None), False
+        if self.seq_alpha or self.z_beta:
+            b.update({"seq_counts": torch.empty(n_seqs, s.E, dtype=torch.int32, device=dev), "seq_P": torch.empty(n_seqs, s.E, **f32),
+                      "seq_loss": torch.empty(2, **f32), "seq_coef": torch.empty(n_seqs + 1, **f32)})
+            ws = moe_seq_loss_workspace_bytes(s, n_seqs)
+        if norm is None:
+            if dropout:
+                raise MoEError("dropout goes with norm")
+            return ws
+        self.norm = MoENorm(s.T, s.d, norm, eps, s.dtype, norm_dtype)
+        self.dropout = float(dropout)
+        if self.dropout and rng is None:
+            raise MoEError("dropout takes rng, its seed and step on the GPU")
+        self.drop_in, self.drop_out = (MoEDropout(self.dropout, rng, site + i) for i in (0, 1))
+        b.update({n: torch.empty(s.T, s.d, **f) for n in ("Xn", "Z", "Out", "dZ") + (("dYd", "dBranch") if self.dropout else ())})
+        b.update({"logits": torch.empty(s.T, s.E, **f32), "mean": torch.empty(s.T, **f32), "rstd": torch.empty(s.T, **f32), "dWr": torch.empty(s.d, s.E, **f)})
+        b.update({n: torch.empty(s.d, dtype=self.norm.weight_dtype, device=dev) for n in ("dnorm_w", "dnorm_b")})
+        return max(ws, moe_router_fwd_workspace_bytes(s), moe_router_bwd_workspace_bytes(s), moe_norm_bwd_workspace_bytes(self.norm))
+
+    def _enter(self, block, X, residual, stream):
+        """The block's norm and router: the logits and rows that the experts take, and the residual stream."""
+        b = self.b
+        if not isinstance(block, MoEBlockWeights):
+            raise MoEError("a layer with norm takes a MoEBlockWeights in the place of the logits")
+        mean = b["mean"] if self.norm.kind == "layer" else None
+        self._block, self._added = block, residual is not None
+        Z = b["Z"] if self._added else X
+        moe_norm_fwd(self.norm, X, block.norm_w, block.norm_b, b["Xn"], mean, b["rstd"], R=residual, drop=self.drop_in if self._added and self.dropout else None,
+                     Z=b["Z"] if self._added else None, stream=stream)
+        moe_router_fwd(self.shape, b["Xn"], block.Wr, b["logits"], self.ws, stream)
+        return b["logits"], b["Xn"], Z
+
+    def _leave(self, dOut, X, stream):
+        """The gradients of router and norm, and of the residual stream."""
+        s, b, block = self.shape, self.b, self._block
+        moe_router_bwd(s, b["Xn"], block.Wr, b["dlogits"], b["dWr"], b["dX"], True, self.ws, stream)
+        masked = self._added and self.dropout
+        moe_norm_bwd(self.norm, b["dX"], b["Z"] if self._added else X, block.norm_w, b["mean"] if self.norm.kind == "layer" else None, b["rstd"], b["dZ"],
+                     None if block.norm_w is None else b["dnorm_w"], None if block.norm_b is None else b["dnorm_b"], self.ws, dZ=dOut,
+                     drop=self.drop_in if masked else None, dX=b["dBranch"] if masked else None, stream=stream)
+        return b["dZ"]
+
     def _ws_pieces(self):
         """The workspace of the routed and that of the shared experts (keywords of an expert set)."""
         return {"ws": self.ws[:self.ws_routed], "ws_bytes": self.ws_routed}, \
@@ -1123,10 +1193,14 @@ class MoEHotPath:
         if self.quant != isinstance(Wg, MoEQuantWeights) or (self.quant and (Wu is not None or Wd is not None)):
             raise MoEError("a layer with quant takes a MoEQuantWeights in the place of Wg, None for Wu and Wd; any other layer the matrices")
 
-    def forward(self, logits, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None):
+    def forward(self, logits, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None, residual=None, seqs=None):
         s, b = self.shape, self.b
         A = s.T * s.k
         self._check_weights(Wg, Wu, Wd)
+        if self.norm:
+            logits, X, Z = self._enter(logits, X, residual, stream)
+        elif residual is not None or isinstance(logits, MoEBlockWeights):
+            raise MoEError("residual and MoEBlockWeights go with norm")
         main = self._fork(Wu, Wsu, stream)
         stream = _stream(stream)
         self._logits = logits  # the gate's backward reads them again
@@ -1162,12 +1236,25 @@ class MoEHotPath:
             if main:
                 self._join(main)
         moe_combine(s, b["Yp"], b["row_of"], b["topk_w"], b["Ysh"] if self.S else None, b["Y"], stream)
-        return b["Y"]
+        if self.seq_alpha or self.z_beta:
+            self._seqs = seqs or (None, None)
+            moe_seq_loss(s, logits, b["topk_idx"], *self._seqs, self.seq_alpha, self.z_beta, b["seq_counts"], b["seq_P"], b["seq_loss"], b["seq_coef"], self.ws, stream)
+        if not self.norm:
+            return b["Y"]
+        moe_dropout(b["Y"], self.drop_out, b["Out"], R=Z, stream=stream)
+        return b["Out"]
 
     def backward(self, dY, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None):
         s, b = self.shape, self.b
         A = s.T * s.k
         self._check_weights(Wg, Wu, Wd)
+        if self.norm:
+            if self._block is None:
+                raise MoEError("backward: there was no forward pass yet")
+            dOut, Z, X = dY, X, b["Xn"]
+            if self.dropout:
+                dY = b["dYd"]
+                moe_dropout(dOut, self.drop_out, dY, stream=stream)
         main = self._fork(Wu, Wsu, stream)
         stream = _stream(stream)
         ws, ws_shared = self._ws_pieces()
@@ -1205,8 +1292,10 @@ class MoEHotPath:
             moe_route_bwd(s, self._logits, b["topk_idx"], b["dw"], b["dlogits"], stream)
             if self.aux_alpha > 0:
                 moe_aux_loss_bwd(s, self._logits, b["counts"], self.aux_alpha, 1.0, True, b["dlogits"], stream)
+        if self.seq_alpha or self.z_beta:
+            moe_seq_loss_bwd(s, self._logits, *self._seqs, b["seq_counts"], b["seq_coef"], 1.0, True, b["dlogits"], stream)
         self._gated = (Wg.gated if self.quant else Wu is not None, Wsu is not None)
-        return b["dX"]
+        return self._leave(dOut, Z, stream) if self.norm else b["dX"]
 
     def gradients(self, gated: Optional[bool] = None, gated_shared: Optional[bool] = None):
         """The weight gradients of the last backward pass, as moe_grad_norm and moe_grad_clip take them.  That pass says which experts were gated: two-matrix
@@ -1222,4 +1311,7 @@ class MoEHotPath:
         gated, gated_shared = wanted
         names = ["dWg_c"] + (["dWu_c"] if gated else []) + ["dWd_c"]
         shared = (["dWsg"] + (["dWsu"] if gated_shared else []) + ["dWsd"]) if self.S else []
-        return [(b[n], b["n_active"]) for n in names] + [b[n] for n in shared]
+        around = []
+        if self.norm and self._block is not None:
+            around = ["dWr"] + (["dnorm_w"] if self._block.norm_w is not None else []) + (["dnorm_b"] if self._block.norm_b is not None else [])
+        return [(b[n], b["n_active"]) for n in names] + [b[n] for n in shared + around]
