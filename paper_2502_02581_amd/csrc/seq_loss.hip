@@ -15,15 +15,16 @@
 namespace moe {
 
 constexpr int kSeqBlocks = 1024, kSeqGroups = kSeqBlocks / 32;  // blocks of the second launch at most
+constexpr int kSeqTotals = 16;  // blocks that count sequences and tokens, at most
 struct SeqInfo {  // start of the workspace
-  int32_t filled, tokens;  // S', T'
+  int2 totals[kSeqTotals];  // S' and T', in parts
   uint32_t done[1 + kSeqGroups][16];  // blocks of the second launch that have ended, by groups of 32, and groups that have (a line of the cache each)
   float2 part[kSeqBlocks];            // their sums of the two losses
 };
 struct SeqArgs {
   const float* logits;
   const int32_t *topk, *start, *len;
-  int T, E, k, gate, S, chunk, chunks;
+  int T, E, k, gate, S, chunk, chunks, parts;
   float* psum;       // [chunks + S][E, in fours] sums of shares
   uint16_t* pcount;  // the same of choices
   float* pz;         // [chunks + S] sums of lse^2
@@ -87,6 +88,16 @@ template <int L> __device__ __forceinline__ float group_sum(float x) {
   if (L >= 16) x = add_lanes8(x);
   if (L >= 32) x = add_rows16(x);
   if (L >= 64) x = add_rows32(x);
+  return x;
+}
+// the same place of all groups
+template <int L> __device__ __forceinline__ float across_groups(float x) {
+  if (L <= 1) x = add_lanes1(x);
+  if (L <= 2) x = add_lanes2(x);
+  if (L <= 4) x = add_quads(x);
+  if (L == 8) x += dpp<0x128>(x);  // a rotation of sixteen by eight
+  if (L <= 16) x = add_rows16(x);
+  if (L <= 32) x = add_rows32(x);
   return x;
 }
 template <int L> __device__ __forceinline__ float group_max(float x) {
@@ -178,72 +189,48 @@ __device__ __forceinline__ void gate_row(const Row<Q>& x, int l, int E, bool sof
       share.v[q][j] = fmaf(fmaf(-p, s, score.v[q][j]), inv, p);
     }
 }
-// The first row's load goes out before the search for the chunk's sequences, the next row's before this one is used.  (Four rows at once are no faster: there are other
-// wavefronts; a chunk of fewer rows is, where tokens are few: 256 tokens of 8 experts 4.9 -> 2.9 us.)
-template <int L, int Q>
-__global__ __launch_bounds__(256) void seq_sums_kernel(SeqArgs a, int want_z, float alpha_E, float* coef) {
-  extern __shared__ int32_t hist_all[];  // [4][Ep]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (blockIdx.x == gridDim.x - 1) {  // the last block: how many sequences have tokens, how many tokens there are, and the sequences' factors
-    int filled = 0, tokens = 0;
-    for (int s = threadIdx.x; s < a.S; s += 256) {
-      const int2 r = seq_range(a.start, a.len, a.S, a.T, s);
-      filled += r.y > r.x;
-      tokens += r.y - r.x;
-    }
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-      filled += __shfl_xor(filled, m, kWave);
-      tokens += __shfl_xor(tokens, m, kWave);
-    }
-    __shared__ int part[2][4];
-    if (lane == 0) {
-      part[0][wave] = filled;
-      part[1][wave] = tokens;
-    }
-    __syncthreads();
-    filled = part[0][0] + part[0][1] + part[0][2] + part[0][3];
-    if (threadIdx.x == 0) {
-      a.info->filled = filled;
-      a.info->tokens = part[1][0] + part[1][1] + part[1][2] + part[1][3];
-    }
-    if (threadIdx.x <= kSeqGroups) a.info->done[threadIdx.x][0] = 0;
-    for (int s = threadIdx.x; s < a.S; s += 256) {
-      const int2 r = seq_range(a.start, a.len, a.S, a.T, s);
-      const float n = (float)(r.y - r.x);
-      coef[s] = r.y > r.x ? alpha_E / (float)filled / (float)a.k / n / n : 0.f;
-    }
-    return;
-  }
-  const int c = blockIdx.x * 4 + wave;
-  if (c >= a.chunks) return;
-  constexpr int G = 64 / L;
-  const int group = lane / L, l = lane % L, Ep = (a.E + 3) & ~3;
+// The pieces of chunk c, by a team of W wavefronts, all of which see the same sequences.  lds: the team's, (1 + W) E words, E in fours; W > 1: the team is
+// the block.
+// The first tokens' loads go out before the search for the chunk's sequences, the next ones' before these are used.  (Four rows of a lane at once are no faster: there are
+// other wavefronts; a chunk of fewer rows is, where tokens are few: 256 tokens of 8 experts 4.9 -> 2.9 us.)  Teams of four, because what the second launch has to read is a
+// piece a chunk, and its few blocks read slowly (8192 tokens of 256 experts: 9.1 us behind chunks of a wavefront).
+template <int L, int Q, int W>
+__device__ __forceinline__ void chunk_sums(const SeqArgs& a, int c, int wave, int32_t* lds, bool want_z) {
+  constexpr int G = 64 / L, GW = G * W;
+  __shared__ float zsum[W];
+  const int lane = threadIdx.x & 63, thread = W > 1 ? (int)threadIdx.x : lane;
+  const int group = (W > 1 ? wave * G : 0) + lane / L, l = lane % L, Ep = (a.E + 3) & ~3;
   const int t0 = c * a.chunk, t1 = min(t0 + a.chunk, a.T);
   const bool softmax = a.gate == MOE_GATE_SOFTMAX;
+  int32_t* hist = lds;
+  float* sums = reinterpret_cast<float*>(lds + Ep) + (W > 1 ? wave * Ep : 0);
   Row<Q> x, share, acc;
   float lse, z2 = 0.f;
-  int ids;            // the first 64 choices of the next tokens
-  int at = t0;        // first of the G tokens whose shares are at hand
+  int ids;      // the first choices of the next tokens
+  int id = -1;  // of these
+  int at = t0;  // first of the GW tokens whose shares are at hand
   auto load = [&](int t) {
     load_logits<L, Q>(a.logits + (size_t)(t + group) * a.E, l, a.E, t + group < t1, x);
-    const int64_t i = (int64_t)t * a.k + lane;
+    const int64_t i = (int64_t)t * a.k + thread;
     ids = i < (int64_t)t1 * a.k ? a.topk[i] : -1;
   };
-  int id = -1;
   auto use = [&]() {
     Row<Q> soft, score;
     gate_row<L, Q>(x, l, a.E, softmax, want_z, soft, score, share, lse);
     id = ids;
-    if (at + G < t1) load(at + G);
+    if (at + GW < t1) load(at + GW);
+  };
+  auto together = [&]() {
+    if (W > 1) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   load(t0);
-  int32_t* hist = hist_all + wave * Ep;
-  for (int e = lane; e < Ep; e += 64) hist[e] = 0;
+  for (int e = thread; e < Ep; e += 64 * W) hist[e] = 0;
   SeqWalk walk;
   walk.begin(a, t0, t1);
   use();
   int s, from, to;
+  together();
   while (walk.next(a, t0, t1, s, from, to)) {
 #pragma unroll
     for (int q = 0; q < Q; q++)
@@ -252,10 +239,10 @@ __global__ __launch_bounds__(256) void seq_sums_kernel(SeqArgs a, int want_z, fl
     z2 = 0.f;
     for (;;) {
       // how often each expert was chosen: whole numbers, so the order of the additions plays no part
-      const int64_t lo = (int64_t)max(from, at) * a.k, hi = (int64_t)min(to, at + G) * a.k;
-      int64_t i = (int64_t)at * a.k + lane;
+      const int64_t lo = (int64_t)max(from, at) * a.k, hi = (int64_t)min(to, at + GW) * a.k;
+      int64_t i = (int64_t)at * a.k + thread;
       if (i >= lo && i < hi && (unsigned)id < (unsigned)a.E) atomicAdd(&hist[id], 1);
-      for (i += 64; i < hi; i += 64)
+      for (i += 64 * W; i < hi; i += 64 * W)
         if (i >= lo) {
           const int e = a.topk[i];
           if ((unsigned)e < (unsigned)a.E) atomicAdd(&hist[e], 1);
@@ -268,163 +255,328 @@ __global__ __launch_bounds__(256) void seq_sums_kernel(SeqArgs a, int want_z, fl
 #pragma unroll
           for (int j = 0; j < 4; j++) acc.v[q][j] += share.v[q][j];
       }
-      if (to <= at + G) break;
-      at += G;
+      if (to <= at + GW) break;
+      at += GW;
       use();
     }
+    z2 = across_groups<L>(z2);
 #pragma unroll
-    for (int m = L; m < 64; m <<= 1) {
-      z2 += __shfl_xor(z2, m, kWave);
+    for (int q = 0; q < Q; q++)
 #pragma unroll
-      for (int q = 0; q < Q; q++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) acc.v[q][j] += __shfl_xor(acc.v[q][j], m, kWave);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      for (int j = 0; j < 4; j++) acc.v[q][j] = across_groups<L>(acc.v[q][j]);
     const size_t piece = (size_t)c + s;
-    if (lane == 0) a.pz[piece] = z2;
-    if (group == 0) {
+    if (W > 1) {
+      if (lane < L) {
 #pragma unroll
-      for (int q = 0; q < Q; q++) {
-        const int e = 4 * (l + L * q);
-        if (e >= Ep) continue;
-        *reinterpret_cast<float4*>(a.psum + piece * Ep + e) = make_float4(acc.v[q][0], acc.v[q][1], acc.v[q][2], acc.v[q][3]);
-        const int4 n = *reinterpret_cast<const int4*>(hist + e);
-        *reinterpret_cast<uint2*>(a.pcount + piece * Ep + e) = make_uint2((uint32_t)n.x | (uint32_t)n.y << 16, (uint32_t)n.z | (uint32_t)n.w << 16);
-        *reinterpret_cast<int4*>(hist + e) = make_int4(0, 0, 0, 0);
+        for (int q = 0; q < Q; q++)
+          if (4 * (l + L * q) < Ep)
+            *reinterpret_cast<float4*>(sums + 4 * (l + L * q)) = make_float4(acc.v[q][0], acc.v[q][1], acc.v[q][2], acc.v[q][3]);
+        if (lane == 0) zsum[wave] = z2;
+      }
+      together();
+      // the team's sums, wavefront after wavefront
+      for (int e = 4 * thread; e < Ep; e += 256 * W) {
+        const float* all = reinterpret_cast<const float*>(lds + Ep) + e;
+        float4 v = *reinterpret_cast<const float4*>(all);
+#pragma unroll
+        for (int w = 1; w < W; w++) {
+          const float4 o = *reinterpret_cast<const float4*>(all + w * Ep);
+          v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        }
+        *reinterpret_cast<float4*>(a.psum + piece * Ep + e) = v;
+      }
+      if (thread == 0) {
+        float z = zsum[0];
+#pragma unroll
+        for (int w = 1; w < W; w++) z += zsum[w];
+        a.pz[piece] = z;
+      }
+    } else {
+      together();
+      if (lane == 0) a.pz[piece] = z2;
+      if (lane < L) {
+#pragma unroll
+        for (int q = 0; q < Q; q++)
+          if (4 * (l + L * q) < Ep)
+            *reinterpret_cast<float4*>(a.psum + piece * Ep + 4 * (l + L * q)) = make_float4(acc.v[q][0], acc.v[q][1], acc.v[q][2], acc.v[q][3]);
       }
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int e = 4 * thread; e < Ep; e += 256 * W) {
+      const int4 n = *reinterpret_cast<const int4*>(hist + e);
+      *reinterpret_cast<uint2*>(a.pcount + piece * Ep + e) = make_uint2((uint32_t)n.x | (uint32_t)n.y << 16, (uint32_t)n.z | (uint32_t)n.w << 16);
+      *reinterpret_cast<int4*>(hist + e) = make_int4(0, 0, 0, 0);
+    }
+    together();
   }
 }
+// How many of the sequences of part `part` of `parts` have tokens, and how many tokens they have (x, y), by a block of W wavefronts; one barrier.
+template <int W>
+__device__ __forceinline__ int2 seq_totals(const SeqArgs& a, int part, int parts) {
+  __shared__ int2 of_wave[W];
+  int filled = 0, tokens = 0;
+#pragma unroll 8
+  for (int s = part * 64 * W + (int)threadIdx.x; s < a.S; s += parts * 64 * W) {
+    const int2 r = seq_range(a.start, a.len, a.S, a.T, s);
+    filled += r.y > r.x;
+    tokens += r.y - r.x;
+  }
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) {
+    filled += __shfl_xor(filled, m, kWave);
+    tokens += __shfl_xor(tokens, m, kWave);
+  }
+  if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = make_int2(filled, tokens);
+  __syncthreads();
+  filled = tokens = 0;
+#pragma unroll
+  for (int w = 0; w < W; w++) {
+    filled += of_wave[w].x;
+    tokens += of_wave[w].y;
+  }
+  return make_int2(filled, tokens);
+}
 
-// P and counts of every sequence, and the losses.  A job is 16 experts of a sequence: four lanes side by side, and as many pieces at once as the team, a wavefront or
-// (WIDE) a block, has fours.
+// P and counts of every sequence, and the losses.  A job is 16 experts of a sequence: four lanes side by side.
 struct SeqFinish {
   SeqArgs a;
   float alpha, beta;
   int32_t* counts;
   float *P, *loss, *coef;
 };
-template <int WAVES>
-__global__ __launch_bounds__(256) void seq_finish_kernel(SeqFinish f) {
-  const SeqArgs& a = f.a;
-  constexpr bool WIDE = WAVES > 1;
-  constexpr int kWaves = WIDE ? WAVES : 4, kRuns = 16 * WAVES;
-  __shared__ float4 psum[WIDE ? WAVES : 1][4];
-  __shared__ int4 pcount[WIDE ? WAVES : 1][4];
-  __shared__ float wsum[2][2][kWaves];
-  __shared__ int last;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tiles = (a.E + 15) / 16, Ep = (a.E + 3) & ~3;
-  const int run = (WIDE ? threadIdx.x : lane) >> 2;
-  const int teams = WIDE ? gridDim.x : gridDim.x * 4;
-  float balance = 0.f, z2 = 0.f;
-  for (int64_t job = WIDE ? blockIdx.x : blockIdx.x * 4 + wave; job < (int64_t)a.S * tiles; job += teams) {
-    const int s = (int)(job / tiles), tile = (int)(job - (int64_t)s * tiles), e = tile * 16 + 4 * (lane & 3);
+struct Job {
+  int s, e, n;     // sequence, the lane's first expert, tokens
+  int64_t p0, p1;  // pieces
+  float sum[4];
+  int count[4];
+  __device__ __forceinline__ Job(const SeqArgs& a, int64_t job, int64_t jobs, int lane) {
+    const int tiles = (a.E + 15) / 16;
+    const bool there = job < jobs;
+    s = there ? (int)(job / tiles) : 0;
+    e = there ? (int)(job - (int64_t)s * tiles) * 16 + 4 * (lane & 3) : 1 << 30;
     const int2 r = seq_range(a.start, a.len, a.S, a.T, s);
-    const int n = r.y - r.x;
-    const int64_t p0 = n ? (int64_t)(r.x / a.chunk) + s : 0, p1 = n ? (int64_t)((r.y - 1) / a.chunk) + s + 1 : 0;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    int count[4] = {0, 0, 0, 0};
-    if (e < Ep) {
-#pragma unroll 8
-      for (int64_t p = p0 + run; p < p1; p += kRuns) {
-        const float4 v = *reinterpret_cast<const float4*>(a.psum + p * Ep + e);
-        const uint2 m = *reinterpret_cast<const uint2*>(a.pcount + p * Ep + e);
-        sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
-        count[0] += m.x & 0xffff; count[1] += m.x >> 16; count[2] += m.y & 0xffff; count[3] += m.y >> 16;
+    n = r.y - r.x;
+    p0 = there && n ? (int64_t)(r.x / a.chunk) + s : 0;
+    p1 = there && n ? (int64_t)((r.y - 1) / a.chunk) + s + 1 : 0;
+#pragma unroll
+    for (int j = 0; j < 4; j++) sum[j] = 0.f, count[j] = 0;
+  }
+  // pieces first, first + step, ..: U of a lane in flight
+  template <int U>
+  __device__ __forceinline__ void add(const SeqArgs& a, int64_t first, int step) {
+    const int Ep = (a.E + 3) & ~3;
+    if (e >= Ep) return;
+    for (int64_t p = first; p < p1; p += U * step) {
+      float4 v[U];
+      uint2 m[U];
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int64_t at = (p + u * step < p1 ? p + u * step : p) * Ep + e;
+        v[u] = *reinterpret_cast<const float4*>(a.psum + at);
+        m[u] = *reinterpret_cast<const uint2*>(a.pcount + at);
+      }
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        if (p + u * step >= p1) break;
+        sum[0] += v[u].x; sum[1] += v[u].y; sum[2] += v[u].z; sum[3] += v[u].w;
+        count[0] += m[u].x & 0xffff; count[1] += m[u].x >> 16; count[2] += m[u].y & 0xffff; count[3] += m[u].y >> 16;
       }
     }
-    if (tile == 0 && f.beta != 0.f)
-      for (int64_t p = p0 + (WIDE ? threadIdx.x : lane); p < p1; p += 64 * WAVES) z2 += a.pz[p];
+  }
+  // over the lanes whose numbers differ by a multiple of four
+  __device__ __forceinline__ void over_lanes() {
 #pragma unroll
-    for (int j = 0; j < 4; j++) {  // lanes whose numbers differ by a multiple of four
+    for (int j = 0; j < 4; j++) {
       sum[j] = add_rows32(add_rows16(add_quads(sum[j])));
       count[j] = add_rows32(add_rows16(add_quads(count[j])));
     }
-    if (WIDE) {
-      if (lane < 4) {
-        psum[wave][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-        pcount[wave][lane] = make_int4(count[0], count[1], count[2], count[3]);
-      }
-      __syncthreads();
-      if (threadIdx.x < 4) {
+  }
+  // writes P, counts and the sequence's factor; the lane's part of sum_e count * P / tokens
+  __device__ __forceinline__ float write(const SeqFinish& f, int filled) const {
+    float b = 0.f;
+    if (e == 0) f.coef[s] = n ? f.alpha * (float)f.a.E / (float)filled / (float)f.a.k / (float)n / (float)n : 0.f;
 #pragma unroll
-        for (int w = 1; w < WAVES; w++) {
-          const float4 v = psum[w][lane];
-          const int4 m = pcount[w][lane];
-          sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
-          count[0] += m.x; count[1] += m.y; count[2] += m.z; count[3] += m.w;
-        }
+    for (int j = 0; j < 4; j++)
+      if (e + j < f.a.E) {
+        const float share = n ? sum[j] / (float)n : 0.f;
+        f.P[(size_t)s * f.a.E + e + j] = share;
+        f.counts[(size_t)s * f.a.E + e + j] = count[j];
+        b = fmaf(share, (float)count[j], b);
       }
-      __syncthreads();
+    return n ? b / (float)n : 0.f;
+  }
+};
+// The thread's sums over the jobs of wavefront `first` of `step`: of count * P / tokens, and of lse^2.  A job is a wavefront's, or (SHORT) four lanes', but for those of
+// many pieces, which then follow one after the other.
+template <bool SHORT>
+__device__ __forceinline__ float2 finish_jobs(const SeqFinish& f, int filled, int64_t first, int64_t step) {
+  const SeqArgs& a = f.a;
+  const int lane = threadIdx.x & 63;
+  const int64_t jobs = (int64_t)a.S * ((a.E + 15) / 16);
+  float balance = 0.f, z2 = 0.f;
+  auto by_all = [&](int64_t job) {
+    Job all(a, job, jobs, lane);
+    all.add<4>(a, all.p0 + (lane >> 2), 16);
+    if (all.e < 16 && f.beta != 0.f)
+      for (int64_t p = all.p0 + lane; p < all.p1; p += 64) z2 += a.pz[p];
+    all.over_lanes();
+    if (lane < 4) balance += all.write(f, filled);
+  };
+  if (!SHORT) {
+    for (int64_t job = first; job < jobs; job += step) by_all(job);
+    return make_float2(balance, z2);
+  }
+  for (int64_t w = first; w * 16 < jobs; w += step) {
+    Job mine(a, w * 16 + (lane >> 2), jobs, lane);
+    const bool many = mine.p1 - mine.p0 > 16;
+    if (!many) {
+      mine.add<4>(a, mine.p0, 1);
+      if (mine.e == 0 && f.beta != 0.f)
+        for (int64_t p = mine.p0; p < mine.p1; p++) z2 += a.pz[p];
+      if (mine.e < a.E) balance += mine.write(f, filled);
     }
-    if ((WIDE ? (int)threadIdx.x : lane) < 4) {
-      const float per = n ? 1.f / (float)n : 0.f;
-      float b = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; j++)
-        if (e + j < a.E) {
-          const float share = n ? sum[j] / (float)n : 0.f;
-          f.P[(size_t)s * a.E + e + j] = share;
-          f.counts[(size_t)s * a.E + e + j] = count[j];
-          b = fmaf(share, (float)count[j], b);
-        }
-      balance = fmaf(b, per, balance);
+    uint64_t left = __ballot(many && (lane & 3) == 0);
+    while (left) {
+      const int q = (__ffsll((unsigned long long)left) - 1) >> 2;
+      left &= left - 1;
+      by_all(w * 16 + q);
     }
   }
+  return make_float2(balance, z2);
+}
+// The same for sequences of many pieces each: a job is a block's, of four wavefronts.
+__device__ __forceinline__ float2 finish_long_jobs(const SeqFinish& f, int filled) {
+  __shared__ float4 psum[4][4];
+  __shared__ int4 pcount[4][4];
+  const SeqArgs& a = f.a;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t jobs = (int64_t)a.S * ((a.E + 15) / 16);
+  float balance = 0.f, z2 = 0.f;
+  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+    Job all(a, job, jobs, lane);
+    all.add<8>(a, all.p0 + (threadIdx.x >> 2), 64);
+    if (all.e < 16 && f.beta != 0.f)
+      for (int64_t p = all.p0 + threadIdx.x; p < all.p1; p += 256) z2 += a.pz[p];
+    all.over_lanes();
+    if (lane < 4) {
+      psum[wave][lane] = make_float4(all.sum[0], all.sum[1], all.sum[2], all.sum[3]);
+      pcount[wave][lane] = make_int4(all.count[0], all.count[1], all.count[2], all.count[3]);
+    }
+    __syncthreads();
+    if (threadIdx.x < 4) {
+#pragma unroll
+      for (int w = 1; w < 4; w++) {
+        const float4 v = psum[w][lane];
+        const int4 m = pcount[w][lane];
+        all.sum[0] += v.x; all.sum[1] += v.y; all.sum[2] += v.z; all.sum[3] += v.w;
+        all.count[0] += m.x; all.count[1] += m.y; all.count[2] += m.z; all.count[3] += m.w;
+      }
+      balance += all.write(f, filled);
+    }
+    __syncthreads();
+  }
+  return make_float2(balance, z2);
+}
+// the sum over a block of W wavefronts; one barrier
+template <int W>
+__device__ __forceinline__ double2 finish_sum(float2 v, float2 (&part)[W]) {
+  v.x = lanes_sum(v.x);
+  v.y = lanes_sum(v.y);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double2 t = {0., 0.};
+#pragma unroll
+  for (int w = 0; w < W; w++) {
+    t.x += part[w].x;
+    t.y += part[w].y;
+  }
+  return t;
+}
+__device__ __forceinline__ void write_losses(const SeqFinish& f, int filled, int tokens, double2 t) {
+  const double per_token = tokens > 0 ? (double)f.beta / tokens : 0.;
+  f.loss[0] = filled > 0 ? (float)((double)f.alpha * f.a.E / ((double)filled * f.a.k) * t.x) : 0.f;
+  f.loss[1] = (float)(per_token * t.y);
+  f.coef[f.a.S] = (float)(2. * per_token);
+}
+
+template <int L, int Q, int W>
+__global__ __launch_bounds__(256) void seq_sums_kernel(SeqArgs a, int want_z) {
+  extern __shared__ int32_t lds[];  // [W > 1 ? 1 + W : 4][E, in fours]
+  const int part = (int)blockIdx.x - ((int)gridDim.x - a.parts);
+  if (part >= 0) {  // the last blocks: what all sequences share
+    const int2 t = seq_totals<4>(a, part, a.parts);
+    if (threadIdx.x == 0) a.info->totals[part] = t;
+    if (part == 0 && threadIdx.x <= kSeqGroups) a.info->done[threadIdx.x][0] = 0;
+    return;
+  }
+  const int wave = threadIdx.x >> 6;
+  if (W > 1) {
+    chunk_sums<L, Q, 4>(a, blockIdx.x, wave, lds, want_z);
+  } else {
+    const int c = blockIdx.x * 4 + wave;
+    if (c < a.chunks) chunk_sums<L, Q, 1>(a, c, wave, lds + wave * ((a.E + 3) & ~3), want_z);
+  }
+}
+
+enum { kShort = 0, kOrdinary = 1, kLong = 2 };  // pieces of a sequence
+template <int LENGTH>
+__global__ __launch_bounds__(256) void seq_finish_kernel(SeqFinish f) {
+  const SeqArgs& a = f.a;
+  __shared__ float2 part[2][4];
+  __shared__ int last;
+  int2 totals = {0, 0};
+  for (int p = 0; p < a.parts; p++) {
+    totals.x += a.info->totals[p].x;
+    totals.y += a.info->totals[p].y;
+  }
+  const float2 mine = LENGTH == kLong ? finish_long_jobs(f, totals.x)
+                                      : finish_jobs<LENGTH == kShort>(f, totals.x, (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), (int64_t)gridDim.x * 4);
   // The block's sums, then, in the block that ends last, those of all blocks.  Sums and counters go past the caches that other dies do not see (atomics of the agent's scope), and
   // a counter only after the sums have arrived (the wait): releasing and acquiring would write back and drop whole caches for these 8 bytes.  (Counters by groups: a
   // thousand additions to one place take 15 us.)
-  auto block_sum = [&](int turn, float b, float z) {
-    b = lanes_sum(b);
-    z = lanes_sum(z);
-    if (lane == 0) {
-      wsum[turn][0][wave] = b;
-      wsum[turn][1][wave] = z;
-    }
-    __syncthreads();
-    double2 t = {0., 0.};
-#pragma unroll
-    for (int w = 0; w < kWaves; w++) {
-      t.x += wsum[turn][0][w];
-      t.y += wsum[turn][1][w];
-    }
-    return t;
-  };
-  double2 t = block_sum(0, balance, z2);
+  double2 t = finish_sum<4>(mine, part[0]);
   if (gridDim.x > 1) {
     if (threadIdx.x == 0) {
       __hip_atomic_store(&a.info->part[blockIdx.x].x, (float)t.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __hip_atomic_store(&a.info->part[blockIdx.x].y, (float)t.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __builtin_amdgcn_s_waitcnt(0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       const uint32_t groups = (gridDim.x + 31) / 32, group = blockIdx.x % groups, members = (gridDim.x - group + groups - 1) / groups;
       last = __hip_atomic_fetch_add(&a.info->done[1 + group][0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == members - 1 &&
              __hip_atomic_fetch_add(&a.info->done[0][0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
     }
     __syncthreads();
     if (!last) return;
-    float b = 0.f, z = 0.f;
+    float2 v = {0.f, 0.f};
 #pragma unroll 4
-    for (int q = threadIdx.x; q < (int)gridDim.x; q += 64 * kWaves) {
-      b += __hip_atomic_load(&a.info->part[q].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      z += __hip_atomic_load(&a.info->part[q].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int q = threadIdx.x; q < (int)gridDim.x; q += 256) {
+      v.x += __hip_atomic_load(&a.info->part[q].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      v.y += __hip_atomic_load(&a.info->part[q].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    t = block_sum(1, b, z);
+    t = finish_sum<4>(v, part[1]);
   }
-  if (threadIdx.x == 0) {
-    const int filled = a.info->filled, tokens = a.info->tokens;
-    const double per_token = tokens > 0 ? (double)f.beta / tokens : 0.;
-    f.loss[0] = filled > 0 ? (float)((double)f.alpha * a.E / ((double)filled * a.k) * t.x) : 0.f;
-    f.loss[1] = (float)(per_token * t.y);
-    f.coef[a.S] = (float)(2. * per_token);
-  }
+  if (threadIdx.x == 0) write_losses(f, totals.x, totals.y, t);
 }
 
+// Both steps in one block, for calls that are over before a second launch would begin.
+template <int L, int Q>
+__global__ __launch_bounds__(1024) void seq_small_kernel(SeqFinish f) {
+  extern __shared__ int32_t lds[];  // [16][E, in fours]
+  __shared__ float2 part[16];
+  const SeqArgs& a = f.a;
+  const int wave = threadIdx.x >> 6;
+  for (int c = wave; c < a.chunks; c += 16) chunk_sums<L, Q, 1>(a, c, wave, lds + wave * ((a.E + 3) & ~3), f.beta != 0.f);
+  const int2 t = seq_totals<16>(a, 0, 1);
+  __syncthreads();  // the pieces are there
+  const bool few = a.S * ((a.E + 15) / 16) <= 16;  // jobs
+  const double2 sums = finish_sum<16>(few ? finish_jobs<false>(f, t.x, wave, 16) : finish_jobs<true>(f, t.x, wave, 16), part);
+  if (threadIdx.x == 0) write_losses(f, t.x, t.y, sums);
+}
+
+// A wavefront writes down whose each of its tokens is, then goes through them, each lane's group with a token of its own; the loads of the next step's logits, and of its
+// sequences' counts where they are others, are under way meanwhile.  (Sequence by sequence, the counts' latency shows at every border: 64 sequences of four tokens 11.5 us.)
 template <int L, int Q>
 __global__ __launch_bounds__(256) void seq_bwd_kernel(SeqArgs a, const int32_t* __restrict__ counts, const float* __restrict__ coef, float dloss,
                                                       int accumulate, float* dlogits) {
+  extern __shared__ int32_t lds[];  // [4][chunk]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = blockIdx.x * 4 + wave;
   if (c >= a.chunks) return;
@@ -432,77 +584,97 @@ __global__ __launch_bounds__(256) void seq_bwd_kernel(SeqArgs a, const int32_t* 
   const int group = lane / L, l = lane % L;
   const int t0 = c * a.chunk, t1 = min(t0 + a.chunk, a.T);
   const bool softmax = a.gate == MOE_GATE_SOFTMAX;
-  Row<Q> next;
-  int at = t0;  // first of the G tokens at hand
-  auto load = [&](int t) { load_logits<L, Q>(a.logits + (size_t)(t + group) * a.E, l, a.E, t + group < t1, next); };
+  Row<Q> next_x;
+  auto load = [&](int t) { load_logits<L, Q>(a.logits + (size_t)(t + group) * a.E, l, a.E, t + group < t1, next_x); };
   load(t0);
   const float cz = dloss * coef[a.S];
   SeqWalk walk;
   walk.begin(a, t0, t1);
-  int done = t0;  // tokens before it are written
-  auto outside = [&](int to) {  // tokens of no sequence have no gradient
-    if (!accumulate)
-      for (size_t i = (size_t)done * a.E + lane; i < (size_t)to * a.E; i += 64) dlogits[i] = 0.f;
-  };
+  int32_t* owner = lds + wave * a.chunk;
+  for (int i = lane; i < t1 - t0; i += 64) owner[i] = -1;
   int s, from, to;
-  while (walk.next(a, t0, t1, s, from, to)) {
-    Row<Q> up;
-    const float cs = dloss * coef[s];
+  while (walk.next(a, t0, t1, s, from, to))
+    for (int t = from + lane; t < to; t += 64) owner[t - t0] = s;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  Row<Q> up;
+  int32_t next_up[Q][4];
+  float next_c = 0.f;
+  int now = -1, next = -1;  // the token's sequence; -1: none
+  bool other;               // the next step has another one in some group
+  auto load_counts = [&](int t) {
+    next = t + group < t1 ? owner[t + group - t0] : -1;
+    other = __any(next != now && next >= 0);
+    if (!other) return;
+    const int at = max(next, 0);
+    next_c = coef[at];
 #pragma unroll
     for (int q = 0; q < Q; q++)
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         const int e = 4 * (l + L * q) + j;
-        up.v[q][j] = e < a.E ? cs * (float)counts[(size_t)s * a.E + e] : 0.f;
+        next_up[q][j] = e < a.E ? counts[(size_t)at * a.E + e] : 0;
       }
-    outside(from);
-    for (;;) {
-      const int t = at + group;
-      const Row<Q> x = next;
-      const bool more = to > at + G;  // (otherwise these tokens may be another sequence's, too)
-      if (more) load(at + G);
-      if (t >= from && t < to) {
-        Row<Q> soft, score, share;
-        float lse, dot = 0.f;
-        gate_row<L, Q>(x, l, a.E, softmax, cz != 0.f, soft, score, share, lse);
+  };
+  load_counts(t0);
+  for (int t = t0; t < t1; t += G) {
+    const Row<Q> x = next_x;
+    if (other) {
+      const float cs = dloss * next_c;
 #pragma unroll
-        for (int q = 0; q < Q; q++)
+      for (int q = 0; q < Q; q++)
 #pragma unroll
-          for (int j = 0; j < 4; j++) dot = fmaf(share.v[q][j], up.v[q][j], dot);
-        dot = group_sum<L>(dot);
-        const float zl = cz * lse;
-#pragma unroll
-        for (int q = 0; q < Q; q++) {
-          const int e = 4 * (l + L * q);
-          float* o = dlogits + (size_t)t * a.E + e;
-          float dz[4];
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            dz[j] = share.v[q][j] * (up.v[q][j] - dot);
-            if (!softmax) dz[j] *= 1.f - score.v[q][j];
-            if (cz != 0.f) dz[j] = fmaf(zl, soft.v[q][j], dz[j]);
-          }
-          if (e + 4 <= a.E) {
-            if (accumulate) {
-              float old[4];
-              __builtin_memcpy(old, o, 16);
-#pragma unroll
-              for (int j = 0; j < 4; j++) dz[j] += old[j];
-            }
-            __builtin_memcpy(o, dz, 16);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-              if (e + j < a.E) o[j] = accumulate ? o[j] + dz[j] : dz[j];
-          }
-        }
-      }
-      if (!more) break;
-      at += G;
+        for (int j = 0; j < 4; j++) up.v[q][j] = cs * (float)next_up[q][j];
     }
-    done = to;
+    now = next;
+    const int mine = t + group;
+    if (t + G < t1) {
+      load(t + G);
+      load_counts(t + G);
+    }
+    if (mine >= t1 || (now < 0 && accumulate)) continue;
+    Row<Q> dz;  // tokens of no sequence have no gradient
+#pragma unroll
+    for (int q = 0; q < Q; q++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) dz.v[q][j] = 0.f;
+    if (now >= 0) {
+      Row<Q> soft, score, share;
+      float lse, dot = 0.f;
+      gate_row<L, Q>(x, l, a.E, softmax, cz != 0.f, soft, score, share, lse);
+#pragma unroll
+      for (int q = 0; q < Q; q++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) dot = fmaf(share.v[q][j], up.v[q][j], dot);
+      dot = group_sum<L>(dot);
+      const float zl = cz * lse;
+#pragma unroll
+      for (int q = 0; q < Q; q++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          dz.v[q][j] = share.v[q][j] * (up.v[q][j] - dot);
+          if (!softmax) dz.v[q][j] *= 1.f - score.v[q][j];
+          if (cz != 0.f) dz.v[q][j] = fmaf(zl, soft.v[q][j], dz.v[q][j]);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+      const int e = 4 * (l + L * q);
+      float* o = dlogits + (size_t)mine * a.E + e;
+      if (e + 4 <= a.E) {
+        if (accumulate) {
+          float old[4];
+          __builtin_memcpy(old, o, 16);
+#pragma unroll
+          for (int j = 0; j < 4; j++) dz.v[q][j] += old[j];
+        }
+        __builtin_memcpy(o, dz.v[q], 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+          if (e + j < a.E) o[j] = accumulate ? o[j] + dz.v[q][j] : dz.v[q][j];
+      }
+    }
   }
-  outside(t1);
 }
 
 // instances by the lanes that a row of logits takes: CALL(L, Q)
@@ -519,20 +691,25 @@ __global__ __launch_bounds__(256) void seq_bwd_kernel(SeqArgs a, const int32_t* 
     else CALL(64, 4);                 \
   } while (0)
 
-// tokens of a wavefront: enough wavefronts for the chip, four tokens or its groups' at least
-static int seq_chunk(int T, int E) {
-  const int groups = E <= 4 ? 64 : E <= 8 ? 32 : E <= 16 ? 16 : E <= 32 ? 8 : E <= 64 ? 4 : E <= 128 ? 2 : 1;
-  const int want = (T + MOE_KNOB("SEQ_WAVES", 4096) - 1) / MOE_KNOB("SEQ_WAVES", 4096), least = groups < 4 ? MOE_KNOB("SEQ_LEAST", 4) : groups;
-  const int chunk = (want + groups - 1) / groups * groups;
-  return chunk < least ? least : chunk > 256 ? 256 : chunk;
+// Tokens of a team, whole steps of it (64 lanes of a wavefront over a row's lanes): enough teams for the chip.  Teams that leave pieces for the second launch are half as many where
+// they would have less than four steps each (8192 tokens of 256 experts: 512 teams 5.8 + 6.3 us, 1024 5.5 + 7.6).
+static int seq_step(int E) { return E <= 4 ? 64 : E <= 8 ? 32 : E <= 16 ? 16 : E <= 32 ? 8 : E <= 64 ? 4 : E <= 128 ? 2 : 1; }
+static int seq_chunk(int T, int step, int teams) {
+  const int want = (T + teams - 1) / teams, chunk = (want + step - 1) / step * step;
+  return chunk < step ? step : chunk > 512 ? 512 : chunk;
 }
 struct SeqPlan {
+  bool small;  // one block, one launch
+  bool team;   // chunks are a block's, not a wavefront's
   int chunk, chunks;
   size_t pieces, sums, counts, z, bytes;  // places of the workspace
 };
-static SeqPlan seq_plan(const moe_shape_t* s, int n_seqs) {
+static SeqPlan seq_plan(const moe_shape_t* s, int n_seqs, bool backward) {
   SeqPlan p;
-  p.chunk = seq_chunk(s->T, s->E);
+  p.small = !backward && (int64_t)s->T * s->E <= 16384 && (int64_t)n_seqs * ((s->E + 15) / 16) <= 64;
+  const int step = seq_step(s->E);
+  p.team = !p.small && !backward && s->T >= (int64_t)n_seqs * 8 * step;  // (a team meets at every border of two sequences)
+  p.chunk = p.small ? seq_chunk(s->T, step, 16) : p.team ? seq_chunk(s->T, 4 * step, s->T < 1024 * 16 * step ? 512 : 1024) : seq_chunk(s->T, step, 4096);
   p.chunks = (s->T + p.chunk - 1) / p.chunk;
   p.pieces = (size_t)p.chunks + n_seqs;
   const size_t Ep = align_up(s->E, 4);
@@ -562,7 +739,7 @@ static bool aligned4(std::initializer_list<const void*> tensors) {
 
 extern "C" size_t moe_seq_loss_workspace_bytes(const moe_shape_t* shape, int32_t n_seqs) {
   if (!shape || shape->T < 0 || shape->E < 1 || shape->E > MOE_MAX_EXPERTS || n_seqs < 1) return 0;
-  return moe::seq_plan(shape, n_seqs).bytes;
+  return moe::seq_plan(shape, n_seqs, false).bytes;
 }
 
 extern "C" int moe_seq_loss(const moe_shape_t* shape, const float* logits, const int32_t* topk_idx, int32_t n_seqs, const int32_t* seq_start,
@@ -579,32 +756,45 @@ extern "C" int moe_seq_loss(const moe_shape_t* shape, const float* logits, const
     set_error("moe_seq_loss: ws must be 16-byte aligned, every other tensor aligned to its values");
     return MOE_EINVAL;
   }
-  const SeqPlan p = seq_plan(shape, n_seqs);
+  const SeqPlan p = seq_plan(shape, n_seqs, false);
   if (ws_bytes < p.bytes) {
     set_error("moe_seq_loss: workspace of %zu bytes, need %zu", ws_bytes, p.bytes);
     return MOE_EWS;
   }
   hipStream_t st = (hipStream_t)stream;
   char* w = (char*)ws;
-  const SeqArgs a = {logits, topk_idx, seq_start, seq_len, shape->T, shape->E, shape->k, shape->gate, n_seqs, p.chunk, p.chunks,
+  const int parts = n_seqs < 2048 * kSeqTotals ? (n_seqs + 2047) / 2048 : kSeqTotals;
+  const SeqArgs a = {logits, topk_idx, seq_start, seq_len, shape->T, shape->E, shape->k, shape->gate, n_seqs, p.chunk, p.chunks, parts,
                      (float*)(w + p.sums), (uint16_t*)(w + p.counts), (float*)(w + p.z), (SeqInfo*)w};
+  const SeqFinish f = {a, alpha, beta, counts, P, loss, coef};
+  const int64_t jobs = (int64_t)n_seqs * ((shape->E + 15) / 16);
+  const size_t hist = sizeof(int32_t) * align_up(shape->E, 4);
+  if (p.small) {
+    ProfScope prof("seq_small_kernel", st);
+#define MOE_SEQ_SMALL(L, Q) hipLaunchKernelGGL((seq_small_kernel<L, Q>), dim3(1), dim3(1024), 16 * hist, st, f)
+    MOE_BY_ROW(shape->E, MOE_SEQ_SMALL);
+#undef MOE_SEQ_SMALL
+    return launch_status("moe_seq_loss");
+  }
   {
     ProfScope prof("seq_sums_kernel", st);
-    const dim3 grid((p.chunks + 3) / 4 + 1), block(256);
-    const size_t lds = 4 * sizeof(int32_t) * align_up(shape->E, 4);
-#define MOE_SEQ_SUMS(L, Q) hipLaunchKernelGGL((seq_sums_kernel<L, Q>), grid, block, lds, st, a, (int)(beta != 0.f), alpha * (float)shape->E, coef)
+    const dim3 grid((p.team ? p.chunks : (p.chunks + 3) / 4) + parts), block(256);
+#define MOE_SEQ_SUMS(L, Q)                                                                                                                        \
+  do {                                                                                                                                            \
+    if (p.team) hipLaunchKernelGGL((seq_sums_kernel<L, Q, 4>), grid, block, 5 * hist, st, a, (int)(beta != 0.f));                  \
+    else hipLaunchKernelGGL((seq_sums_kernel<L, Q, 1>), grid, block, 4 * hist, st, a, (int)(beta != 0.f));                         \
+  } while (0)
     MOE_BY_ROW(shape->E, MOE_SEQ_SUMS);
 #undef MOE_SEQ_SUMS
   }
   {
     ProfScope prof("seq_finish_kernel", st);
     const int pieces = p.chunks / n_seqs;  // of an ordinary sequence
-    const int waves = pieces > MOE_KNOB("SEQ_WIDE4", 32) ? 4 : 1;
-    const int64_t jobs = (int64_t)n_seqs * ((shape->E + 15) / 16), blocks = waves > 1 ? jobs : (jobs + 3) / 4;
-    const SeqFinish f = {a, alpha, beta, counts, P, loss, coef};
+    const int64_t blocks = pieces > 32 ? jobs : pieces > 4 || jobs <= 256 ? (jobs + 3) / 4 : (jobs + 63) / 64;
     const dim3 grid((unsigned)(blocks < kSeqBlocks ? blocks : kSeqBlocks)), block(256);
-    if (waves == 4) hipLaunchKernelGGL(seq_finish_kernel<4>, grid, block, 0, st, f);
-    else hipLaunchKernelGGL(seq_finish_kernel<1>, grid, block, 0, st, f);
+    if (pieces > 32) hipLaunchKernelGGL(seq_finish_kernel<kLong>, grid, block, 0, st, f);
+    else if (pieces > 4 || jobs <= 256) hipLaunchKernelGGL(seq_finish_kernel<kOrdinary>, grid, block, 0, st, f);
+    else hipLaunchKernelGGL(seq_finish_kernel<kShort>, grid, block, 0, st, f);
   }
   return launch_status("moe_seq_loss");
 }
@@ -623,12 +813,12 @@ extern "C" int moe_seq_loss_bwd(const moe_shape_t* shape, const float* logits, i
     set_error("moe_seq_loss_bwd: every tensor must be aligned to its values");
     return MOE_EINVAL;
   }
-  const SeqPlan p = seq_plan(shape, n_seqs);
-  const SeqArgs a = {logits, nullptr, seq_start, seq_len, shape->T, shape->E, shape->k, shape->gate, n_seqs, p.chunk, p.chunks, nullptr, nullptr, nullptr, nullptr};
+  const SeqPlan p = seq_plan(shape, n_seqs, true);
+  const SeqArgs a = {logits, nullptr, seq_start, seq_len, shape->T, shape->E, shape->k, shape->gate, n_seqs, p.chunk, p.chunks, 0, nullptr, nullptr, nullptr, nullptr};
   hipStream_t st = (hipStream_t)stream;
   ProfScope prof("seq_bwd_kernel", st);
   const dim3 grid((p.chunks + 3) / 4), block(256);
-#define MOE_SEQ_BWD(L, Q) hipLaunchKernelGGL((seq_bwd_kernel<L, Q>), grid, block, 0, st, a, counts, coef, dloss, (int)accumulate, dlogits)
+#define MOE_SEQ_BWD(L, Q) hipLaunchKernelGGL((seq_bwd_kernel<L, Q>), grid, block, 4 * sizeof(int32_t) * p.chunk, st, a, counts, coef, dloss, (int)accumulate, dlogits)
   MOE_BY_ROW(shape->E, MOE_SEQ_BWD);
 #undef MOE_SEQ_BWD
   return launch_status("moe_seq_loss_bwd");

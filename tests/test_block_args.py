@@ -145,8 +145,7 @@ class Library:
 def noted(monkeypatch):
     lib = Library()
     monkeypatch.setattr(binding, "load_library", lambda: lib)
-    monkeypatch.setattr(binding, "_stream", lambda s: 0)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_current", lambda stream: (0, 0))
     return lib
 
 
