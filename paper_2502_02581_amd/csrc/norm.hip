@@ -23,9 +23,10 @@ struct NormBwd {
   const void *dY, *Z, *w, *dZ;
   const float *mean, *rstd;
   void *dR, *dX;
-  float* partial;  // [blocks][2][d]: sums of dw, db; NULL: not wanted
+  float* partial;  // [blocks][2][d]: sums of dw, db; NULL: not wanted, or
+  void *dw, *db;   // written by the blocks behind the first row_blocks
   int64_t lddy, ldz, lddz, lddr, lddx;
-  int n_rows, d, layer, wf32;
+  int n_rows, d, layer, wf32, row_blocks;
   Dropout drop;
 };
 
@@ -167,12 +168,95 @@ __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V =
   }
 }
 
+// dw and db of 128 bytes' worth of columns, over all rows: for calls of few rows, where reading these again costs less than another launch.  P lanes side by side hold a row's pieces,
+// as many rows at once as the block has P lanes.  The mean's rounding error, 2^-24 of it, is less than 8 of the deviation's where the mean is below 8 deviations; other rows'
+// lanes look at the whole row for it.
+template <typename T>
+__device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
+  constexpr int P = sizeof(T) == 2 ? 8 : 4, U = 4;
+  __shared__ float part[16][2][8 * P];
+  const T *dY = (const T*)a.dY, *Z = (const T*)a.Z;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
+  const int p = threadIdx.x & (P - 1), col = 8 * (block * P + p), valid = a.d - col, runs = blockDim.x / P;
+  float dw[8], db[8];
+#pragma unroll
+  for (int j = 0; j < 8; j++) dw[j] = db[j] = 0.f;
+  for (int row0 = threadIdx.x / P; row0 < a.n_rows; row0 += U * runs) {
+    Piece<T> y[U], z[U];
+    float m[U], rstd[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int row = row0 + u * runs;
+      const bool there = row < a.n_rows;
+      load_piece(y[u], dY + row * a.lddy + col, there ? valid : 0);
+      load_piece(z[u], Z + row * a.ldz + col, there ? valid : 0);
+      m[u] = there && a.layer ? a.mean[row] : 0.f;
+      rstd[u] = there ? a.rstd[row] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int row = row0 + u * runs;
+      if (row >= a.n_rows) break;
+      float delta = 0.f;
+      if (fabsf(m[u]) * rstd[u] > 8.f) {
+        float s = 0.f;
+        for (int c = p; 8 * c < a.d; c += P) {
+          Piece<T> x;
+          float v[8];
+          load_piece(x, Z + row * a.ldz + 8 * c, a.d - 8 * c);
+          x.values(v);
+#pragma unroll
+          for (int j = 0; j < 8; j++) s += 8 * c + j < a.d ? v[j] - m[u] : 0.f;
+        }
+        s = add_lanes2(add_lanes1(s));
+        if (P == 8) s = add_lanes4(s);
+        delta = s / (float)a.d;
+      }
+      float dy[8], x[8];
+      y[u].values(dy);
+      z[u].values(x);
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        dw[j] = fmaf(dy[j], ((x[j] - m[u]) - delta) * rstd[u], dw[j]);
+        db[j] += dy[j];
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; j++) {
+    if (P == 4) {
+      dw[j] = add_quads(dw[j]);
+      db[j] = add_quads(db[j]);
+    } else {
+      dw[j] += dpp<0x128>(dw[j]);  // a rotation of sixteen by eight
+      db[j] += dpp<0x128>(db[j]);
+    }
+    dw[j] = add_rows32(add_rows16(dw[j]));
+    db[j] = add_rows32(add_rows16(db[j]));
+    if (lane < P) {
+      part[wave][0][8 * p + j] = dw[j];
+      part[wave][1][8 * p + j] = db[j];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * 8 * P; i += blockDim.x) {
+    const int which = i / (8 * P), c = i % (8 * P), at = 8 * block * P + c;
+    void* out = which ? a.db : a.dw;
+    if (!out || at >= a.d) continue;
+    float t = 0.f;
+    for (int w = 0; w < n_waves; w++) t += part[w][which][c];
+    if (a.wf32) ((float*)out)[at] = t;
+    else Elem<bf16_t>::store((bf16_t*)out + at, t);
+  }
+}
+
 template <typename T, int V, int TEAM, bool DROP>
 __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : 1024) void norm_bwd_kernel(NormBwd a) {
   constexpr bool WIDE = TEAM != kWaveTeam;
+  if (TEAM != kLongTeam && (int)blockIdx.x >= a.row_blocks) return norm_columns<T>(a, blockIdx.x - a.row_blocks);
   __shared__ RowSums<3> sums;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-  const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? gridDim.x : gridDim.x * n_waves;
+  const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? a.row_blocks : a.row_blocks * n_waves;
   const int first = WIDE ? threadIdx.x : lane, step = WIDE ? blockDim.x : kWave;
   const T *dY = (const T*)a.dY, *Z = (const T*)a.Z, *dZ = (const T*)a.dZ;
   T *dR = (T*)a.dR, *dX = (T*)a.dX;
@@ -354,26 +438,38 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial
 //  - longer ones a block whose lanes hold one piece, in the forward pass of long rows two, where there are many (8192 x 7168: 44.0 us for 49.6, 8192 x 2048: 20.4 for 18.5,
 //    500 x 4096: 5.9 for 5.1): half as many wavefronts take part in a row's two barriers;
 //  - 16 wavefronts a unit, each with the next row's loads under way, reach the copy's rate.  The backward pass takes fewer blocks where they would get less than four
-//    rows (six, for teams of a wavefront): their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks 9.7 + 3.4 us, 1024 11.0 + 5.0, 256 12.2 + 4.1).
+//    rows (six, for teams of a wavefront): their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks 9.7 + 3.4 us, 1024 11.0 + 5.0, 256 12.2 + 4.1);
+//  - where blocks of columns have sixteen rows a lane at most, in 8 MB, they are in the same launch as the rows (256 x 4096: 5.2 us for 6.8 + 3.3, 1000 x 4096 13.0 for 11.6 + 4.4,
+//    512 x 1000 8.1 for 5.8 + 3.2; with 31 rows a lane, 1000 x 512, 12.6 for 5.1 + 4.4).
 struct NormPlan {
   int V, team, waves, blocks;
+  int columns;  // blocks for the weights' gradients, in the same launch; 0: a launch of their own, from the blocks' sums
 };
 static NormPlan norm_plan(const moe_norm_t* n, bool backward) {
   const int pieces = (n->d + 7) / 8, rows = n->n_rows;
   const auto at_most = [](int x, int most) { return x < most ? x : most; };
-  NormPlan p;
+  NormPlan p = {};
+  const auto own_columns = [&](int waves) {
+    const int side = n->dtype == MOE_F32 ? 4 : 8;  // pieces of 128 bytes
+    if (backward && rows <= 16 * (64 * waves / side) && (int64_t)rows * n->d * (int64_t)elem_size(n->dtype) <= 1 << 23) p.columns = (pieces + side - 1) / side;
+  };
   if (pieces <= 128) {
-    p = {pieces <= 64 ? 1 : 2, kWaveTeam, 4, at_most((rows + 3) / 4, 2048)};
-    if (backward) p.blocks = at_most((rows + 3) / 4, at_most(rows / 6 + 64, 768));
+    p.V = pieces <= 64 ? 1 : 2;
+    p.team = kWaveTeam;
+    p.waves = 4;
+    own_columns(p.waves);
+    p.blocks = at_most((rows + 3) / 4, 2048);
+    if (backward && !p.columns) p.blocks = at_most(p.blocks, at_most(rows / 6 + 64, 768));
     return p;
   }
   const bool two = pieces > 1024 || (!backward && pieces > 256 && rows > 1024);
   p.V = two ? 2 : 1;
   p.team = pieces > 1024 ? kLongTeam : kBlockTeam;
   p.waves = (pieces + 64 * p.V - 1) / (64 * p.V);
+  if (p.team == kBlockTeam) own_columns(p.waves);
   p.blocks = 4096 / p.waves / 256 * 256;  // 256 units, the same number of blocks each
   if (p.blocks > 2048) p.blocks = 2048;
-  if (backward) p.blocks = at_most(p.blocks, rows / 4 + 64);
+  if (backward && !p.columns) p.blocks = at_most(p.blocks, rows / 4 + 64);
   p.blocks = at_most(p.blocks, rows);
   return p;
 }
@@ -404,7 +500,8 @@ using namespace moe;
 
 extern "C" size_t moe_norm_bwd_workspace_bytes(const moe_norm_t* norm) {
   if (check_norm(norm, "moe_norm_bwd_workspace_bytes")) return 0;
-  return (size_t)norm_plan(norm, true).blocks * 2 * (size_t)norm->d * sizeof(float) + 256;
+  const NormPlan p = norm_plan(norm, true);
+  return (p.columns ? 0 : (size_t)p.blocks * 2 * (size_t)norm->d * sizeof(float)) + 256;
 }
 
 extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, const void* R, int64_t ldr, const moe_drop_t* drop, const void* w,
@@ -492,9 +589,9 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
   }
   hipStream_t st = (hipStream_t)stream;
   if (n > 0) {
-    const NormBwd a = {dY, Z, w, dZ, mean, rstd, dR, dX, weights ? (float*)ws : nullptr, lddy, ldz, lddz, lddr, lddx, n, d,
-                       norm->kind == MOE_NORM_LAYER, norm->wdtype == MOE_F32, dr};
-    const dim3 grid(p.blocks), block(64 * p.waves);
+    const NormBwd a = {dY, Z, w, dZ, mean, rstd, dR, dX, weights && !p.columns ? (float*)ws : nullptr, dw, db, lddy, ldz, lddz, lddr, lddx, n, d,
+                       norm->kind == MOE_NORM_LAYER, norm->wdtype == MOE_F32, p.blocks, dr};
+    const dim3 grid(p.blocks + (weights ? p.columns : 0)), block(64 * p.waves);
     ProfScope prof("norm_bwd_kernel", st);
 #define MOE_NORM_BWD(T, V, TEAM)                                                                          \
   do {                                                                                                    \
@@ -513,7 +610,7 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
 #undef MOE_NORM_BWD_BY_PLAN
 #undef MOE_NORM_BWD
   }
-  if (weights) {
+  if (weights && (n == 0 || !p.columns)) {
     ProfScope prof("norm_weights_kernel", st);
     hipLaunchKernelGGL(norm_weights_kernel, dim3((d + 31) / 32, 2), dim3(1024), 0, st, (const float*)ws, n > 0 ? p.blocks : 0, d, (int)(norm->wdtype == MOE_F32),
                        dw, db);

@@ -129,7 +129,7 @@ def test_strided_rows(n, d, pitch, dtype):
     run(n, d, dtype, dtype, "layer", "drop", pitch=pitch)
 
 
-@pytest.mark.parametrize("n,d,dtype", [(3000, 1000, "bf16"), (5000, 64, "f32"), (2500, 2048, "bf16"), (1030, 7168, "f32"), (16384, 16, "bf16")])
+@pytest.mark.parametrize("n,d,dtype", [(512, 520, "bf16"), (513, 520, "bf16"), (1024, 72, "f32"), (1025, 72, "f32"), (1023, 4096, "bf16"), (1025, 4096, "bf16"), (3000, 1000, "bf16"), (5000, 64, "f32"), (2500, 2048, "bf16"), (1030, 7168, "f32"), (16384, 16, "bf16")])
 def test_many_rows(n, d, dtype):
     """More rows than teams: every block adds several."""
     run(n, d, dtype, dtype, "layer", "plain")
@@ -145,6 +145,13 @@ def test_absent_tensors(weights, bias, dz_in, grads):
 def test_rows_far_from_zero(d):
     """Mean 1e4, deviation 1: the mean's rounding error would be 5e-4 of the deviation."""
     run(7, d, "f32", "f32", "layer", "plain", offset=1e4)
+
+
+@pytest.mark.parametrize("offset", [2.0, 6.0, 12.0, 300.0])
+@pytest.mark.parametrize("n,d", [(30, 500), (2500, 96)])
+def test_means_around_the_lines(n, d, offset):
+    """Means of a few deviations, on both sides of the lines from which on their rounding error is taken out, for both ways to the weights' gradients."""
+    run(n, d, "f32", "f32", "layer", "plain", offset=offset)
 
 
 @pytest.mark.parametrize("d", [48, 5000])
