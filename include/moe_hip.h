@@ -440,17 +440,18 @@ int moe_grad_clip(const moe_grad_t* grads, int32_t n, const float* norm, float m
  *   multiple of 2^-16, and what is kept is scaled by 65536 / (65536 - round(65536 p)).  Dropped values add nothing, infinities and NaN neither.
  *   rng [2] (device, 8-byte aligned): seed and step, read when the kernel runs; a captured graph draws other masks at every replay if a node of it, or the program
  *   between replays, advances the step.  The forward and the backward pass must find the same values there.  Calls of one step that must not share a mask have sites of their own.
- *   X, R, out in dtype (f32 or bf16), cols up to 2^18; out may be X or R (same address and stride).  p = 0 (less than 2^-17) adds only; rng may then be NULL.
+ *   X, R, out in dtype (f32 or bf16), cols up to 2^18, values up to 2^36; out may be X or R (same address and stride).  p = 0 (less than 2^-17) adds only; rng may then be NULL.
  *
  * moe_norm_fwd -- Z = R + drop(X), rounded to dtype (without R and drop, Z = X: Z is then NULL);
  *   MOE_NORM_LAYER: mean = sum Z / d, v = sum (Z - mean)^2 / d;   MOE_NORM_RMS: mean = 0, v = sum Z^2 / d;
  *   rstd = 1 / sqrt(v + eps);   Y = (Z - mean) rstd w + b
  *   w, b [d] in wdtype; NULL: ones, zeros.  mean, rstd [n_rows] f32 out, kept for the backward pass; either may be NULL (RMS has no mean).  1 <= d <= 16384.
- *   Sums are fp32, the mean's own rounding error is taken out of Z - mean (in both passes), and Y is rounded once.  Z may be X or R, Y may be X.
+ *   Sums are fp32, the mean's own rounding error is taken out of Z - mean (in both passes), and Y is rounded once.  Z may be X or R, Y the one
+ *   of them that Z is not (same address and stride).
  * moe_norm_bwd -- g = dY w;  h = (Z - mean) rstd;  dZtotal = dZ + rstd (g - mean(g) [layer] - h mean(g h));
  *   dR = dZtotal;  dX = drop'(dZtotal) (with drop: the mask of the forward pass; dX is then required and dR may be NULL);
  *   dw = sum over rows of dY h,  db = sum over rows of dY  (wdtype; either may be NULL; with n_rows == 0 they are written as zeros)
- *   dZ: the gradient that reaches Z by another way, the residual stream's; NULL: none.  dR may be dY or dZ, and so may dX, but not both the same.
+ *   dZ: the gradient that reaches Z by another way, the residual stream's; NULL: none.  dR may be dY, dZ or Z (same address and stride), and so may dX, but not both the same.
  *   ws >= moe_norm_bwd_workspace_bytes(norm) where dw or db is wanted (sums of the blocks, added in a fixed order: no atomics)
  */
 enum { MOE_NORM_LAYER = 0, MOE_NORM_RMS = 1 };
@@ -484,7 +485,7 @@ int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy, const voi
  *   loss[0] = alpha / S' sum_s E sum_e f_se P_se;    loss[1] = beta / T' sum_t lse_t^2, lse_t = log sum_e exp(logits_te)   (0 without tokens)
  *   Backward, the loads held constant: dlogits of dloss (loss[0] + loss[1]); rows of no sequence get zeros, or nothing when accumulate != 0.
  *   Rows whose logits are all -inf (sigmoid: whose scores are all 0 in fp32) have shares and lse 0; other rows may hold -inf.  topk_idx outside 0..E-1 is not counted.
- *   logits, dlogits [T, E] f32; topk_idx [T, k]; seq_start, seq_len i32 (device); counts [n_seqs, E] i32 out; P [n_seqs, E] f32 out; loss [2] f32 out;
+ *   logits, dlogits [T, E] f32 (dlogits may be logits when accumulate == 0); topk_idx [T, k]; seq_start, seq_len i32 (device); counts [n_seqs, E] i32 out; P [n_seqs, E] f32 out; loss [2] f32 out;
  *   coef [n_seqs + 1] f32 out: alpha E / (S' k T_s^2) for every sequence, 2 beta / T': what the backward pass takes from the forward pass, besides counts.
  *   shape gives T, E, k and gate.  ws >= moe_seq_loss_workspace_bytes(shape, n_seqs).  All sums in a fixed order: two calls give the same bits.
  */

@@ -72,6 +72,11 @@ int check_rows(const char* who, const char* what, const void* p, int64_t ld, int
   return MOE_OK;
 }
 
+int check_places(const char* who, const char* out, const void* p, int64_t ldp, const char* in, const void* q, int64_t ldq, int64_t n_rows) {
+  if (!p || p != q || n_rows <= 1 || ldp == ldq) return MOE_OK;
+  set_error("%s: %s is %s, but with a row stride of %lld for %lld", who, out, in, (long long)ldp, (long long)ldq);
+  return MOE_EINVAL;
+}
 int make_dropout(const moe_drop_t* drop, Dropout& out, const char* who) {
   out = {nullptr, 0, 0, 1.f};
   if (!drop) return MOE_OK;
@@ -119,19 +124,20 @@ extern "C" int moe_dropout(const void* X, int64_t ldx, const void* R, int64_t ld
   if (n_rows == 0) return MOE_OK;
   const size_t e = elem_size(dtype);
   if ((rc = check_rows(who, "X", X, ldx, n_rows, cols, e, true)) || (rc = check_rows(who, "R", R, ldr, n_rows, cols, e, false)) ||
-      (rc = check_rows(who, "out", out, ldo, n_rows, cols, e, true)))
+      (rc = check_rows(who, "out", out, ldo, n_rows, cols, e, true)) || (rc = check_places(who, "out", out, ldo, "X", X, ldx, n_rows)) ||
+      (rc = check_places(who, "out", out, ldo, "R", R, ldr, n_rows)))
     return rc;
   const uint32_t per_row = (uint32_t)(cols + 7) / 8;
   const int64_t pieces = (int64_t)n_rows * per_row;
   const DropoutArgs a = {X, R, out, ldx, ldr, ldo, pieces, cols, per_row, per_row == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + per_row - 1) / per_row), d};
   hipStream_t st = (hipStream_t)stream;
-  ProfScope prof("dropout_kernel", st);
   constexpr int U = 2;
   const int64_t blocks = (pieces + kDropThreads * U - 1) / (kDropThreads * U);
-  if (blocks >= (int64_t)1 << 31) {
-    set_error("%s: too many values", who);
+  if (blocks >= (int64_t)1 << 24) {  // (a launch has less than 2^32 threads)
+    set_error("%s: %d rows of %d are too many values for a call (2^36)", who, n_rows, cols);
     return MOE_EINVAL;
   }
+  ProfScope prof("dropout_kernel", st);
   if (dtype == MOE_F32) hipLaunchKernelGGL((dropout_kernel<float, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
   else hipLaunchKernelGGL((dropout_kernel<bf16_t, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
   return launch_status(who);

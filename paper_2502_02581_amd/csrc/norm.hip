@@ -445,13 +445,14 @@ struct NormPlan {
   int V, team, waves, blocks;
   int columns;  // blocks for the weights' gradients, in the same launch; 0: a launch of their own, from the blocks' sums
 };
-static NormPlan norm_plan(const moe_norm_t* n, bool backward) {
+// in_place: an output is an input whose columns would be read beside it.
+static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
   const int pieces = (n->d + 7) / 8, rows = n->n_rows;
   const auto at_most = [](int x, int most) { return x < most ? x : most; };
   NormPlan p = {};
   const auto own_columns = [&](int waves) {
     const int side = n->dtype == MOE_F32 ? 4 : 8;  // pieces of 128 bytes
-    if (backward && rows <= 16 * (64 * waves / side) && (int64_t)rows * n->d * (int64_t)elem_size(n->dtype) <= 1 << 23) p.columns = (pieces + side - 1) / side;
+    if (backward && !in_place && rows <= 16 * (64 * waves / side) && (int64_t)rows * n->d * (int64_t)elem_size(n->dtype) <= 1 << 23) p.columns = (pieces + side - 1) / side;
   };
   if (pieces <= 128) {
     p.V = pieces <= 64 ? 1 : 2;
@@ -500,8 +501,7 @@ using namespace moe;
 
 extern "C" size_t moe_norm_bwd_workspace_bytes(const moe_norm_t* norm) {
   if (check_norm(norm, "moe_norm_bwd_workspace_bytes")) return 0;
-  const NormPlan p = norm_plan(norm, true);
-  return (p.columns ? 0 : (size_t)p.blocks * 2 * (size_t)norm->d * sizeof(float)) + 256;
+  return (size_t)norm_plan(norm, true, true).blocks * 2 * (size_t)norm->d * sizeof(float) + 256;  // (the call's other plan needs none)
 }
 
 extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, const void* R, int64_t ldr, const moe_drop_t* drop, const void* w,
@@ -519,6 +519,13 @@ extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, 
       (rc = check_rows(who, "w", w, d, 1, d, we, false)) || (rc = check_rows(who, "b", b, d, 1, d, we, false)) ||
       (rc = check_rows(who, "mean", mean, 1, 1, 1, 4, false)) || (rc = check_rows(who, "rstd", rstd, 1, 1, 1, 4, false)))
     return rc;
+  if ((rc = check_places(who, "Z", Z, ldz, "X", X, ldx, n)) || (rc = check_places(who, "Z", Z, ldz, "R", R, ldr, n)) ||
+      (rc = check_places(who, "Y", Y, ldy, "X", X, ldx, n)) || (rc = check_places(who, "Y", Y, ldy, "R", R, ldr, n)))
+    return rc;
+  if (n > 0 && Y == Z) {
+    set_error("%s: Y and Z overlap", who);
+    return MOE_EINVAL;
+  }
   if (Z && !sum) {
     set_error("%s: Z goes with R or drop; without them it would be X", who);
     return MOE_EINVAL;
@@ -528,7 +535,7 @@ extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, 
     return MOE_EINVAL;
   }
   if (n == 0) return MOE_OK;
-  const NormPlan p = norm_plan(norm, false);
+  const NormPlan p = norm_plan(norm, false, false);
   const NormFwd a = {X, R, w, b, Z, Y, mean, rstd, ldx, ldr, ldz, ldy, n, d, norm->kind == MOE_NORM_LAYER, norm->wdtype == MOE_F32, norm->eps, dr};
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid(p.blocks), block(64 * p.waves);
@@ -574,8 +581,16 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
     set_error("%s: dX goes with drop; without it the gradient of the branch is dR", who);
     return MOE_EINVAL;
   }
+  if ((rc = check_places(who, "dR", dR, lddr, "dY", dY, lddy, n)) || (rc = check_places(who, "dR", dR, lddr, "dZ", dZ, lddz, n)) ||
+      (rc = check_places(who, "dR", dR, lddr, "Z", Z, ldz, n)) || (rc = check_places(who, "dX", dX, lddx, "dY", dY, lddy, n)) ||
+      (rc = check_places(who, "dX", dX, lddx, "dZ", dZ, lddz, n)) || (rc = check_places(who, "dX", dX, lddx, "Z", Z, ldz, n)))
+    return rc;
+  if (n > 0 && dR && dR == dX) {
+    set_error("%s: dR and dX overlap", who);
+    return MOE_EINVAL;
+  }
   const bool weights = dw || db;
-  const NormPlan p = norm_plan(norm, true);
+  const NormPlan p = norm_plan(norm, true, (dR && (dR == dY || dR == Z)) || (dX && (dX == dY || dX == Z)));
   if (weights) {
     const size_t need = moe_norm_bwd_workspace_bytes(norm);
     if (!ws || !aligned16(ws)) {

@@ -169,5 +169,7 @@ int make_dropout(const moe_drop_t* drop, Dropout& out, const char* who);
 
 // host: checks one tensor of rows of a call: its pointer (needed: not NULL), alignment and row stride
 int check_rows(const char* who, const char* what, const void* p, int64_t ld, int64_t n_rows, int64_t cols, size_t elem, bool needed);
+// host: an output that is an input has to have its rows where that has them
+int check_places(const char* who, const char* out, const void* p, int64_t ldp, const char* in, const void* q, int64_t ldq, int64_t n_rows);
 
 }  // namespace moe

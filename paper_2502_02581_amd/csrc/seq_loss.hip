@@ -559,7 +559,7 @@ __global__ __launch_bounds__(256) void seq_finish_kernel(SeqFinish f) {
 // Both steps in one block, for calls that are over before a second launch would begin.
 template <int L, int Q>
 __global__ __launch_bounds__(1024) void seq_small_kernel(SeqFinish f) {
-  extern __shared__ int32_t lds[];  // [16][E, in fours]
+  extern __shared__ int32_t lds[];  // [chunks, up to 16][E, in fours]
   __shared__ float2 part[16];
   const SeqArgs& a = f.a;
   const int wave = threadIdx.x >> 6;
@@ -709,7 +709,7 @@ static SeqPlan seq_plan(const moe_shape_t* s, int n_seqs, bool backward) {
   p.small = !backward && (int64_t)s->T * s->E <= 16384 && (int64_t)n_seqs * ((s->E + 15) / 16) <= 64;
   const int step = seq_step(s->E);
   p.team = !p.small && !backward && s->T >= (int64_t)n_seqs * 8 * step;  // (a team meets at every border of two sequences)
-  p.chunk = p.small ? seq_chunk(s->T, step, 16) : p.team ? seq_chunk(s->T, 4 * step, s->T < 1024 * 16 * step ? 512 : 1024) : seq_chunk(s->T, step, 4096);
+  p.chunk = p.small ? seq_chunk(s->T, step, s->E > 512 ? 8 : 16) : p.team ? seq_chunk(s->T, 4 * step, s->T < 1024 * 16 * step ? 512 : 1024) : seq_chunk(s->T, step, 4096);
   p.chunks = (s->T + p.chunk - 1) / p.chunk;
   p.pieces = (size_t)p.chunks + n_seqs;
   const size_t Ep = align_up(s->E, 4);
@@ -771,7 +771,7 @@ extern "C" int moe_seq_loss(const moe_shape_t* shape, const float* logits, const
   const size_t hist = sizeof(int32_t) * align_up(shape->E, 4);
   if (p.small) {
     ProfScope prof("seq_small_kernel", st);
-#define MOE_SEQ_SMALL(L, Q) hipLaunchKernelGGL((seq_small_kernel<L, Q>), dim3(1), dim3(1024), 16 * hist, st, f)
+#define MOE_SEQ_SMALL(L, Q) hipLaunchKernelGGL((seq_small_kernel<L, Q>), dim3(1), dim3(1024), (size_t)(p.chunks < 16 ? p.chunks : 16) * hist, st, f)  /* 32 KB at most */
     MOE_BY_ROW(shape->E, MOE_SEQ_SMALL);
 #undef MOE_SEQ_SMALL
     return launch_status("moe_seq_loss");

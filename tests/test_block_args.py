@@ -46,6 +46,8 @@ def test_dropout(lib):
     for kw in (dict(X=ODD), dict(R=ODD), dict(out=ODD)):
         assert f(**kw) == -1 and "aligned" in text(lib)
     assert f(n=0, X=None, R=None, out=None) == 0
+    assert f(X=OK16, out=OK16, ldo=101) == -1 and "stride" in text(lib)
+    assert f(n=1 << 30, cols=1 << 10, ldx=1 << 10, ldr=1 << 10, ldo=1 << 10) == -1 and "too many" in text(lib)
 
 
 def norm(**kw):
@@ -55,7 +57,7 @@ def norm(**kw):
 
 
 def test_norm_fwd(lib):
-    def f(nm=None, X=OK16, ldx=100, R=OK16, ldr=100, d=None, w=OK16, b=OK16, Z=OK16, ldz=100, Y=OK16, ldy=100, mean=OK16, rstd=OK16):
+    def f(nm=None, X=OK16, ldx=100, R=OK16, ldr=100, d=None, w=OK16, b=OK16, Z=OK16, ldz=100, Y=ctypes.c_void_p(12288), ldy=100, mean=OK16, rstd=OK16):
         return lib.moe_norm_fwd(ctypes.byref(nm or norm()), X, ldx, R, ldr, d, w, b, Z, ldz, Y, ldy, mean, rstd, None)
 
     for kw in (dict(dtype=2), dict(wdtype=-1), dict(kind=2)):
@@ -74,6 +76,9 @@ def test_norm_fwd(lib):
     assert f(d=drop(2.0)) == -1 and "probability" in text(lib)
     assert lib.moe_norm_fwd(None, OK16, 8, None, 0, None, None, None, None, 0, OK16, 8, None, None, None) == -1
     assert f(norm(n_rows=0), X=None, R=None, Z=None, Y=None) == 0
+    there = ctypes.c_void_p(8192)
+    assert f(Y=OK16) == -1 and "overlap" in text(lib)
+    assert f(X=there, Z=there, ldz=101) == -1 and f(R=there, Z=there, ldz=101) == -1 and f(X=there, Y=there, ldy=101) == -1 and "stride" in text(lib)
 
 
 def test_norm_bwd(lib):
@@ -93,6 +98,11 @@ def test_norm_bwd(lib):
     assert f(dX=OK16, lddx=100) == -1 and "dX goes with" in text(lib)
     assert f(nb=need - 1) == -2 and "workspace" in text(lib)
     assert f(norm(dtype=9)) == -3
+    assert f(d=drop(), dX=OK16, lddx=100) == -1 and "overlap" in text(lib)
+    there = ctypes.c_void_p(8192)
+    for kw in (dict(dY=there), dict(dZ=there), dict(Z=there)):
+        assert f(dR=there, lddr=101, **kw) == -1 and "stride" in text(lib)
+        assert f(d=drop(), dX=there, lddx=101, **kw) == -1 and "stride" in text(lib)
     assert f(norm(n_rows=0), dY=None, Z=None, mean=None, rstd=None, dZ=None, dR=None, dw=None, db=None, ws=None, nb=0) == 0
 
 

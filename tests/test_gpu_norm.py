@@ -173,12 +173,12 @@ def test_rows_that_are_not_finite_stay_alone(kind, d):
         assert torch.isnan(Y[3]).all() and not Y[4].any() and abs(float(rstd[4]) * EPS ** 0.5 - 1) < 1e-6
 
 
-@pytest.mark.parametrize("d", [96, 7000])
-def test_outputs_that_are_inputs(d):
-    """The residual stream updated in place, the gradient written over the one that came in: the same bits as into tensors of their own."""
+@pytest.mark.parametrize("n,d", [(50, 96), (50, 7000), (700, 520), (9, 9000)])
+def test_outputs_that_are_inputs(n, d):
+    """The residual stream updated in place, the gradient written over the one that came in, or over the saved rows: what it is into tensors of their own, the same bits (the
+    weights' gradients, which then take another order: within fp32's rounding of their sums, and bf16's)."""
     import paper_2502_02581_amd as moe
 
-    n = 50
     g = torch.Generator().manual_seed(d)
     X, R, dY, dZ = (rows(g, n, d, "bf16") for _ in range(4))
     w, b = torch.randn(d, generator=g).bfloat16().cuda(), torch.randn(d, generator=g).bfloat16().cuda()
@@ -196,7 +196,42 @@ def test_outputs_that_are_inputs(d):
     dy, dz = dY.clone(), dZ.clone()
     dw2, db2 = torch.empty_like(w), torch.empty_like(b)
     moe.moe_norm_bwd(norm, dy, Z, w, mean, rstd, dz, dw2, db2, ws, dZ=dz, drop=drop, dX=dy)
-    assert torch.equal(dz, dR) and torch.equal(dy, dX) and torch.equal(dw, dw2) and torch.equal(db, db2)
+    assert torch.equal(dz, dR) and torch.equal(dy, dX)
+    h = (Z.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    for a, b2, terms in ((dw, dw2, dY.double() * h), (db, db2, dY.double())):
+        assert ((a.double() - b2.double()).abs() <= 2 * (2.0 ** -8 * terms.sum(0).abs() + 256 * U * terms.abs().sum(0) * 3)).all()
+    zz = Z.clone()
+    moe.moe_norm_bwd(norm, dY, zz, w, mean, rstd, zz, dw2, db2, ws, dZ=dZ, drop=drop, dX=dX)
+    assert torch.equal(zz, dR)
+
+
+def test_beyond_two_to_the_31_values():
+    """Rows whose values lie behind 2^31 others, forward and backward: the last rows against the definition."""
+    import paper_2502_02581_amd as moe
+
+    d = 16384
+    n = (1 << 31) // d + 40
+    g = torch.Generator().manual_seed(9)
+    few = [rows(g, 8, d, "bf16") for _ in range(2)]
+    X, dY, Y = (torch.zeros(n, d, dtype=torch.bfloat16, device="cuda:0") for _ in range(3))
+    X[-8:], dY[-8:] = few
+    w = torch.randn(d, generator=g).cuda()
+    norm = moe.MoENorm(n, d, "layer", EPS, "bf16", "f32")
+    mean, rstd, dw, db = torch.empty(n, device="cuda:0"), torch.empty(n, device="cuda:0"), torch.empty_like(w), torch.empty_like(w)
+    ws = torch.empty(moe.moe_norm_bwd_workspace_bytes(norm), dtype=torch.uint8, device="cuda:0")
+    moe.moe_norm_fwd(norm, X, w, None, Y, mean, rstd)
+    x, dy = np64(few[0]), np64(few[1])
+    y, m64, r64, h = ob.norm_fwd(x, np64(w), None, "layer", EPS)
+    close(Y[-8:], y, U * (64 * (1 + np.abs(h)) * np.abs(np64(w)) + 2 * np.abs(y)), "bf16")
+    assert not Y[:-8].any()
+    moe.moe_norm_bwd(norm, dY, X, w, mean, rstd, Y, dw, db, ws)
+    dz, dw64, db64 = ob.norm_bwd(dy, h, r64, np64(w), "layer")
+    gg = np.abs(dy * np64(w))
+    tol = 256 * U * r64[:, None] * (gg + gg.mean(1)[:, None] + (1 + np.abs(h)) * (gg * (1 + np.abs(h))).mean(1)[:, None]) + 2 * U * np.abs(dz)
+    close(Y[-8:], dz, tol, "bf16")
+    assert not Y[:-8].any()
+    close(dw, dw64, 256 * U * (np.abs(dy) * (1 + np.abs(h))).sum(0), "f32")
+    close(db, db64, 256 * U * np.abs(dy).sum(0), "f32")
 
 
 def test_no_rows():

@@ -91,6 +91,51 @@ def test_experts(E, k, gate):
 
 
 @pytest.mark.parametrize("gate", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("T,E,k,S", [(16, 1024, 8, 1), (31, 513, 4, 1), (10, 1000, 64, 1), (32, 512, 2, 2), (16384, 1, 1, 5), (4096, 4, 2, 64), (4097, 4, 2, 64), (4096, 4, 2, 65), (130, 126, 3, 8)])
+def test_around_the_line_of_small_calls(T, E, k, S, gate):
+    """One launch or two: 16384 logits, 64 jobs of 16 experts; as many experts as its counters have room for."""
+    start = [T * i // S for i in range(S)]
+    run(T, E, k, gate, start=start, length=[max(0, T // S - i % 3) for i in range(S)])
+
+
+def test_mixed_lengths():
+    """One long sequence among hundreds of short ones: those of many pieces are joined by a wavefront, the others by four lanes."""
+    start = list(range(0, 600, 2)) + [600, 30000, 30001]
+    length = [1 + i % 2 for i in range(300)] + [29400, 1, 5]
+    run(30010, 64, 2, "softmax", start=start, length=length)
+    run(30010, 64, 2, "sigmoid", start=[0, 100] + [30000 + i for i in range(10)], length=[90, 29800] + [1] * 10)
+
+
+def test_beyond_two_to_the_31_values():
+    """Logits behind 2^31 others: the last of three sequences against the definition (the others: nothing, and all alike)."""
+    import paper_2502_02581_amd as moe
+
+    E, k, tail = 1024, 4, 70
+    T = (1 << 31) // E + 100
+    g = torch.Generator().manual_seed(2)
+    x = torch.zeros(T, E, device="cuda:0")
+    last = torch.randn(tail, E, generator=g)
+    x[-tail:] = last.cuda()
+    topk = torch.zeros(T, k, dtype=torch.int32, device="cuda:0")
+    ids = torch.topk(last, k, dim=1).indices.to(torch.int32)
+    topk[-tail:] = ids.cuda()
+    st = torch.tensor([0, 5, T - tail, T], dtype=torch.int32, device="cuda:0")
+    st[1] = 0
+    shape = moe.MoEShape(T, 8, E, k, 8, "f32")
+    f = dict(device="cuda:0")
+    counts, P, loss, coef = torch.empty(3, E, dtype=torch.int32, **f), torch.empty(3, E, **f), torch.empty(2, **f), torch.empty(4, **f)
+    ws = torch.empty(moe.moe_seq_loss_workspace_bytes(shape, 3), dtype=torch.uint8, **f)
+    moe.moe_seq_loss(shape, x, topk, st, None, 0.01, 0.0, counts, P, loss, coef, ws)
+    moe.moe_seq_loss_bwd(shape, x, st, None, counts, coef, 1.0, False, x)   # (over the logits: each is read before its gradient is written)
+    c64, P64, _, dz = ob.seq_loss(np64(last), ids.numpy(), [(0, tail)], k, "softmax", 0.01 / 2, 0.0)
+    assert np.array_equal(counts[2].cpu().numpy(), c64[0]) and int(counts[1, 0]) == k * (T - tail) and not counts[0].any()
+    assert (np.abs(np64(P[2]) - P64[0]) <= 1024 * U * P64[0]).all()
+    share = ob.shares(np64(last), "softmax")[0]
+    up = 0.005 * E * c64[0] / (k * tail) / tail
+    assert (np.abs(np64(x[-tail:]) - dz) <= 128 * U * share * (up + (share * up).sum(1, keepdims=True))).all()
+
+
+@pytest.mark.parametrize("gate", ["softmax", "sigmoid"])
 def test_sequences(gate):
     """Offsets without lengths, empty sequences at every place, tokens before the first and behind the last, lengths that reach beyond."""
     run(100, 16, 2, gate, start=[0, 40, 40, 100])
