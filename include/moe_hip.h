@@ -445,8 +445,8 @@ int moe_grad_clip(const moe_grad_t* grads, int32_t n, const float* norm, float m
  * moe_norm_fwd -- Z = R + drop(X), rounded to dtype (without R and drop, Z = X: Z is then NULL);
  *   MOE_NORM_LAYER: mean = sum Z / d, v = sum (Z - mean)^2 / d;   MOE_NORM_RMS: mean = 0, v = sum Z^2 / d;
  *   rstd = 1 / sqrt(v + eps);   Y = (Z - mean) rstd w + b
- *   w, b [d] in wdtype; NULL: ones, zeros.  mean, rstd [n_rows] f32 out, kept for the backward pass; either may be NULL (RMS has no mean).  1 <= d <= 16384.
- *   Sums are fp32, the mean's own rounding error is taken out of Z - mean (in both passes), and Y is rounded once.  Z may be X or R, Y the one
+ *   w, b [d] in wdtype; NULL: ones, zeros.  mean, rstd [n_rows] f32 out, kept for the backward pass; either may be NULL (RMS has no mean).  1 <= d <= 16384, n_rows < 2^31 - 2^14.
+ *   Sums are fp32 (a row whose squares' sum is beyond their range has rstd 0), the mean's own rounding error is taken out of Z - mean (in both passes), Y is rounded once.  Z may be X or R, Y the one
  *   of them that Z is not (same address and stride).
  * moe_norm_bwd -- g = dY w;  h = (Z - mean) rstd;  dZtotal = dZ + rstd (g - mean(g) [layer] - h mean(g h));
  *   dR = dZtotal;  dX = drop'(dZtotal) (with drop: the mask of the forward pass; dX is then required and dR may be NULL);
@@ -487,7 +487,7 @@ int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy, const voi
  *   Rows whose logits are all -inf (sigmoid: whose scores are all 0 in fp32) have shares and lse 0; other rows may hold -inf.  topk_idx outside 0..E-1 is not counted.
  *   logits, dlogits [T, E] f32 (dlogits may be logits when accumulate == 0); topk_idx [T, k]; seq_start, seq_len i32 (device); counts [n_seqs, E] i32 out; P [n_seqs, E] f32 out; loss [2] f32 out;
  *   coef [n_seqs + 1] f32 out: alpha E / (S' k T_s^2) for every sequence, 2 beta / T': what the backward pass takes from the forward pass, besides counts.
- *   shape gives T, E, k and gate.  ws >= moe_seq_loss_workspace_bytes(shape, n_seqs).  All sums in a fixed order: two calls give the same bits.
+ *   shape gives T (below 2^31 - 2^16), E, k and gate.  ws >= moe_seq_loss_workspace_bytes(shape, n_seqs).  All sums in a fixed order: two calls give the same bits.
  */
 size_t moe_seq_loss_workspace_bytes(const moe_shape_t* shape, int32_t n_seqs);
 int moe_seq_loss(const moe_shape_t* shape, const float* logits, const int32_t* topk_idx, int32_t n_seqs, const int32_t* seq_start, const int32_t* seq_len,

@@ -8,7 +8,7 @@
 
 namespace moe {
 
-constexpr int kNormMaxD = 16384;
+constexpr int kNormMaxD = 16384, kNormMaxRows = INT32_MAX - (1 << 14);  // (a team's next row is an index, too)
 
 struct NormFwd {
   const void *X, *R, *w, *b;
@@ -46,15 +46,15 @@ __device__ __forceinline__ void load_weights(const void* w, int wf32, int col, i
   }
 }
 
-// Rows far from zero: the rounding error of the mean would be that of every value of the row.  delta, the mean of z - m, puts it right, so that they lose nothing but
-// what their own values have lost (mean 1e4, deviation 1, fp32).  Where the mean is below the deviation its error is below the deviation's, and delta would bring in the
-// roundings of z - m, which have one sign for all z of a binade; there it is left out.
-enum { kPlain = 0, kAdd = 1, kDrop = 2 };
+enum { kPlain = 0, kAdd = 1, kDrop = 2 };  // z = x, r + x, r + drop(x)
 
 // TEAM: who works on a row.  A wavefront of the block's four; the block; or (rows of more than 8192 values) a block of up to sixteen wavefronts, whose lanes have too few
 // registers to hold the next row as well, or, in the backward pass, this one.
 enum { kWaveTeam = 0, kBlockTeam = 1, kLongTeam = 2 };
 
+// Rows far from zero: the rounding error of the mean would be that of every value of the row.  delta, the mean of z - m, puts it right, so that they lose nothing but
+// what their own values have lost (mean 1e4, deviation 1, fp32).  Where the mean is below the deviation its error is below the deviation's, and delta would bring in the
+// roundings of z - m, which have one sign for all z of a binade; there it is left out.
 template <typename T, int V, int TEAM, int MODE>
 __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_fwd_kernel(NormFwd a) {
   constexpr bool WIDE = TEAM != kWaveTeam;
@@ -488,7 +488,7 @@ static int check_norm(const moe_norm_t* n, const char* who) {
     set_error("%s: unknown kind %d", who, n->kind);
     return MOE_EDTYPE;
   }
-  if (n->n_rows < 0 || n->d < 1 || n->d > kNormMaxD || !(n->eps >= 0.f) || n->eps > 3.4e38f) {
+  if (n->n_rows < 0 || n->n_rows > kNormMaxRows || n->d < 1 || n->d > kNormMaxD || !(n->eps >= 0.f) || n->eps > 3.4e38f) {
     set_error("%s: bad sizes: %d rows of %d (1 to %d), eps %g", who, n->n_rows, n->d, kNormMaxD, (double)n->eps);
     return MOE_EINVAL;
   }

@@ -5,7 +5,7 @@
 //   balance = alpha / S' sum_s E sum_e f_se P_se;   z = beta / T' sum_t lse_t^2, lse_t = log sum_e exp(logit_te)
 //   dz_te = coef_s n_s. through the shares (the loads held constant) + coef_z lse_t softmax_te,  coef_s = alpha E / (S' k T_s^2),  coef_z = 2 beta / T'
 //
-// Tokens are cut into chunks of equal length, one a wavefront, and chunks into the pieces that belong to one sequence.  Sequences ascend, so chunk c's
+// Tokens are cut into chunks of equal length, each a wavefront's or a block's, and chunks into the pieces that belong to one sequence.  Sequences ascend, so chunk c's
 // piece of sequence s has the number c + s: along the tokens one of the two grows by one at every border, no two pieces share a number, and those of a
 // sequence are neighbours.  The sums of a piece, of a sequence's pieces and of the loss are each added in a fixed order.
 #include <initializer_list>
@@ -15,9 +15,9 @@
 namespace moe {
 
 constexpr int kSeqBlocks = 1024, kSeqGroups = kSeqBlocks / 32;  // blocks of the second launch at most
-constexpr int kSeqTotals = 16;  // blocks that count sequences and tokens, at most
-struct SeqInfo {  // start of the workspace
-  int2 totals[kSeqTotals];  // S' and T', in parts
+constexpr int kSeqTotals = 16;                                  // blocks that count sequences and tokens, at most
+struct SeqInfo {                      // start of the workspace
+  int2 totals[kSeqTotals];            // S' and T', in parts
   uint32_t done[1 + kSeqGroups][16];  // blocks of the second launch that have ended, by groups of 32, and groups that have (a line of the cache each)
   float2 part[kSeqBlocks];            // their sums of the two losses
 };
@@ -726,6 +726,10 @@ static int check_seqs(const moe_shape_t* shape, int n_seqs, const int32_t* start
     set_error("%s: bad sequences: %d of them (1 to 2^24; without seq_start one, and then no seq_len)", who, n_seqs);
     return MOE_EINVAL;
   }
+  if (shape->T > INT32_MAX - (1 << 16)) {  // (the end of the last chunk is an index, too)
+    set_error("%s: T=%d overflows the index range", who, shape->T);
+    return MOE_EINVAL;
+  }
   return MOE_OK;
 }
 
@@ -738,7 +742,7 @@ static bool aligned4(std::initializer_list<const void*> tensors) {
 }  // namespace moe
 
 extern "C" size_t moe_seq_loss_workspace_bytes(const moe_shape_t* shape, int32_t n_seqs) {
-  if (!shape || shape->T < 0 || shape->E < 1 || shape->E > MOE_MAX_EXPERTS || n_seqs < 1) return 0;
+  if (!shape || shape->T < 0 || shape->T > INT32_MAX - (1 << 16) || shape->E < 1 || shape->E > MOE_MAX_EXPERTS || n_seqs < 1) return 0;
   return moe::seq_plan(shape, n_seqs, false).bytes;
 }
 
@@ -769,9 +773,9 @@ extern "C" int moe_seq_loss(const moe_shape_t* shape, const float* logits, const
   const SeqFinish f = {a, alpha, beta, counts, P, loss, coef};
   const int64_t jobs = (int64_t)n_seqs * ((shape->E + 15) / 16);
   const size_t hist = sizeof(int32_t) * align_up(shape->E, 4);
-  if (p.small) {
+  if (p.small) {  // (32 KB of LDS at most)
     ProfScope prof("seq_small_kernel", st);
-#define MOE_SEQ_SMALL(L, Q) hipLaunchKernelGGL((seq_small_kernel<L, Q>), dim3(1), dim3(1024), (size_t)(p.chunks < 16 ? p.chunks : 16) * hist, st, f)  /* 32 KB at most */
+#define MOE_SEQ_SMALL(L, Q) hipLaunchKernelGGL((seq_small_kernel<L, Q>), dim3(1), dim3(1024), (size_t)(p.chunks < 16 ? p.chunks : 16) * hist, st, f)
     MOE_BY_ROW(shape->E, MOE_SEQ_SMALL);
 #undef MOE_SEQ_SMALL
     return launch_status("moe_seq_loss");

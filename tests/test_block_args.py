@@ -62,7 +62,7 @@ def test_norm_fwd(lib):
 
     for kw in (dict(dtype=2), dict(wdtype=-1), dict(kind=2)):
         assert f(norm(**kw)) == -3 and "unknown" in text(lib)
-    for kw in (dict(n_rows=-1), dict(d=0), dict(d=16385), dict(eps=-1e-9), dict(eps=float("nan")), dict(eps=float("inf"))):
+    for kw in (dict(n_rows=-1), dict(n_rows=2 ** 31 - 2 ** 14, d=1), dict(d=0), dict(d=16385), dict(eps=-1e-9), dict(eps=float("nan")), dict(eps=float("inf"))):
         assert f(norm(**kw)) == -1 and "bad" in text(lib)
         assert moe.load_library().moe_norm_bwd_workspace_bytes(ctypes.byref(norm(**kw))) == 0
     for kw in (dict(X=None), dict(Y=None), dict(Z=None)):
@@ -126,6 +126,7 @@ def test_seq_loss(lib):
         assert call(shape(gate=3)) == -3 and call(shape(k=9)) == -1 and call(shape(T=-1)) == -1
         for kw in (dict(n=0), dict(n=-1), dict(n=(1 << 24) + 1), dict(st=None), dict(st=None, ln=None), dict(n=1, st=None)):
             assert call(**kw) == -1 and "sequences" in text(lib), kw
+        assert call(shape(T=2 ** 31 - 5, k=1, E=1)) == -1 and "index range" in text(lib)
     for kw in (dict(lg=None), dict(tk=None), dict(counts=None), dict(P=None), dict(loss=None), dict(coef=None), dict(ws=None)):
         assert f(**kw) == -1 and "null" in text(lib)
     for kw in (dict(lg=None), dict(counts=None), dict(coef=None), dict(dl=None)):
