@@ -35,9 +35,9 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
     row[u] = row0 + over;
     c[u] = q - over * a.per_row;
     valid[u] = base + i < a.pieces ? a.cols - 8 * (int)c[u] : 0;
-    load_piece(x[u], (const T*)a.X + (int64_t)row[u] * a.ldx + 8 * c[u], valid[u]);
+    load_piece<true>(x[u], (const T*)a.X + (int64_t)row[u] * a.ldx + 8 * c[u], valid[u]);
     r[u].clear();
-    if (a.R) load_piece(r[u], (const T*)a.R + (int64_t)row[u] * a.ldr + 8 * c[u], valid[u]);
+    if (a.R) load_piece<true>(r[u], (const T*)a.R + (int64_t)row[u] * a.ldr + 8 * c[u], valid[u]);
   }
 #pragma unroll
   for (int u = 0; u < U; u++) {

@@ -46,7 +46,9 @@ __device__ __forceinline__ void load_weights(const void* w, int wf32, int col, i
   }
 }
 
-enum { kPlain = 0, kAdd = 1, kDrop = 2 };  // z = x, r + x, r + drop(x)
+// z = x, r + x, r + drop(x); kPass: z = x, and no statistics are kept, so no backward pass will read x again (with kPlain it will: no streaming hint on its loads, or
+// the backward pass of 1000 x 4096 right behind takes 15.7 us for 13.0)
+enum { kPlain = 0, kAdd = 1, kDrop = 2, kPass = 3 };
 
 // TEAM: who works on a row.  A wavefront of the block's four; the block; or (rows of more than 8192 values) a block of up to sixteen wavefronts, whose lanes have too few
 // registers to hold the next row as well, or, in the backward pass, this one.
@@ -57,7 +59,7 @@ enum { kWaveTeam = 0, kBlockTeam = 1, kLongTeam = 2 };
 // roundings of z - m, which have one sign for all z of a binade; there it is left out.
 template <typename T, int V, int TEAM, int MODE>
 __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_fwd_kernel(NormFwd a) {
-  constexpr bool WIDE = TEAM != kWaveTeam;
+  constexpr bool WIDE = TEAM != kWaveTeam, ADD = MODE == kAdd || MODE == kDrop;
   __shared__ RowSums<2> sums;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
   const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? gridDim.x : gridDim.x * n_waves;
@@ -80,10 +82,10 @@ __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V =
 #pragma unroll
     for (int v = 0; v < V; v++) {
       const int col = 8 * (first + v * step);
-      load_piece(x[v], X + row * a.ldx + col, valid[v]);
-      if (MODE != kPlain) {
+      load_piece<MODE != kPlain>(x[v], X + row * a.ldx + col, valid[v]);
+      if (ADD) {
         r[v].clear();
-        if (R) load_piece(r[v], R + row * a.ldr + col, valid[v]);
+        if (R) load_piece<true>(r[v], R + row * a.ldr + col, valid[v]);
       }
     }
   };
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V =
     for (int v = 0; v < V; v++) {
       const int c = first + v * step;
       x[v].values(z[v]);
-      if (MODE != kPlain) {
+      if (ADD) {
         float add[8];
         r[v].values(add);
         if (MODE == kDrop) {
@@ -250,10 +252,11 @@ __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
   }
 }
 
-template <typename T, int V, int TEAM, bool DROP>
-__global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : 1024) void norm_bwd_kernel(NormBwd a) {
+// ONCE: nobody else reads the rows; with blocks of columns beside those of rows they would miss them (1000 x 4096: 16.3 us for 13.0).
+template <typename T, int V, int TEAM, bool DROP, bool ONCE>
+__global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_bwd_kernel(NormBwd a) {
   constexpr bool WIDE = TEAM != kWaveTeam;
-  if (TEAM != kLongTeam && (int)blockIdx.x >= a.row_blocks) return norm_columns<T>(a, blockIdx.x - a.row_blocks);
+  if ((TEAM == kWaveTeam || V == 1) && (int)blockIdx.x >= a.row_blocks) return norm_columns<T>(a, blockIdx.x - a.row_blocks);
   __shared__ RowSums<3> sums;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
   const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? a.row_blocks : a.row_blocks * n_waves;
@@ -277,9 +280,9 @@ __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : 1024) void norm_bwd_kerne
   };
   auto load = [&](Loads& p, int row, int v, bool all) {
     const int col = 8 * (first + v * step);
-    load_piece(p.y, dY + row * a.lddy + col, valid[v]);
-    load_piece(p.z, Z + row * a.ldz + col, valid[v]);
-    if (all && dZ) load_piece(p.in, dZ + row * a.lddz + col, valid[v]);
+    load_piece<ONCE>(p.y, dY + row * a.lddy + col, valid[v]);
+    load_piece<ONCE>(p.z, Z + row * a.ldz + col, valid[v]);
+    if (all && dZ) load_piece<ONCE>(p.in, dZ + row * a.lddz + col, valid[v]);
     else p.in.clear();
   };
   float s[3];  // sums of g, of g (z - m) and, for the mean's rounding error as in the forward pass, of z - m
@@ -435,10 +438,11 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial
 
 // Pieces of a lane, wavefronts of a row, blocks.  Measured (T rows of d, bf16 unless it says otherwise):
 //  - rows of up to 1024 values take a wavefront (16384 x 768 backward: 18.5 us, with a block of two wavefronts 20.2), four a block;
-//  - longer ones a block whose lanes hold one piece, in the forward pass of long rows two, where there are many (8192 x 7168: 44.0 us for 49.6, 8192 x 2048: 20.4 for 18.5,
-//    500 x 4096: 5.9 for 5.1): half as many wavefronts take part in a row's two barriers;
-//  - 16 wavefronts a unit, each with the next row's loads under way, reach the copy's rate.  The backward pass takes fewer blocks where they would get less than four
-//    rows (six, for teams of a wavefront): their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks 9.7 + 3.4 us, 1024 11.0 + 5.0, 256 12.2 + 4.1);
+//  - longer ones a block whose lanes hold one piece, or two where rows are long and many: half as many wavefronts take part in a row's barriers (forward 8192 x 7168: 44.0 us for
+//    49.6, 8192 x 2048: 20.4 for 18.5, 500 x 4096: 5.9 for 5.1; both passes of 8192 x 7168 121 for 136, of 8192 x 4096 70.1 for 72.9);
+//  - 16 wavefronts a unit, each with the next row's loads under way, reach the copy's rate, in the backward pass with two pieces a lane eight.  The backward pass takes fewer
+//    blocks where they would get less than four rows (six, for teams of a wavefront): their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks
+//    9.7 + 3.4 us, 1024 11.0 + 5.0, 256 12.2 + 4.1);
 //  - where blocks of columns have sixteen rows a lane at most, in 8 MB, they are in the same launch as the rows (256 x 4096: 5.2 us for 6.8 + 3.3, 1000 x 4096 13.0 for 11.6 + 4.4,
 //    512 x 1000 8.1 for 5.8 + 3.2; with 31 rows a lane, 1000 x 512, 12.6 for 5.1 + 4.4).
 struct NormPlan {
@@ -463,12 +467,12 @@ static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
     if (backward && !p.columns) p.blocks = at_most(p.blocks, at_most(rows / 6 + 64, 768));
     return p;
   }
-  const bool two = pieces > 1024 || (!backward && pieces > 256 && rows > 1024);
+  const bool two = pieces > 1024 || (pieces > 256 && rows > 1024);
   p.V = two ? 2 : 1;
   p.team = pieces > 1024 ? kLongTeam : kBlockTeam;
   p.waves = (pieces + 64 * p.V - 1) / (64 * p.V);
-  if (p.team == kBlockTeam) own_columns(p.waves);
-  p.blocks = 4096 / p.waves / 256 * 256;  // 256 units, the same number of blocks each
+  if (!two) own_columns(p.waves);
+  p.blocks = (backward && two && p.team == kBlockTeam ? 2048 : 4096) / p.waves / 256 * 256;  // 256 units, the same number of blocks each: one at least, of 16 wavefronts, or of 8
   if (p.blocks > 2048) p.blocks = 2048;
   if (backward && !p.columns) p.blocks = at_most(p.blocks, rows / 4 + 64);
   p.blocks = at_most(p.blocks, rows);
@@ -550,7 +554,8 @@ extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, 
   } while (0)
 #define MOE_NORM_FWD(T, V, TEAM)                                                                                \
   do {                                                                                                          \
-    if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kPlain>), grid, block, 0, st, a);                  \
+    if (!sum && rstd) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kPlain>), grid, block, 0, st, a);          \
+    else if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kPass>), grid, block, 0, st, a);              \
     else if (dr.threshold == 0) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kAdd>), grid, block, 0, st, a); \
     else hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kDrop>), grid, block, 0, st, a);                        \
   } while (0)
@@ -607,18 +612,24 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
     const NormBwd a = {dY, Z, w, dZ, mean, rstd, dR, dX, weights && !p.columns ? (float*)ws : nullptr, dw, db, lddy, ldz, lddz, lddr, lddx, n, d,
                        norm->kind == MOE_NORM_LAYER, norm->wdtype == MOE_F32, p.blocks, dr};
     const dim3 grid(p.blocks + (weights ? p.columns : 0)), block(64 * p.waves);
+    const bool once = dZ && !p.columns;
     ProfScope prof("norm_bwd_kernel", st);
-#define MOE_NORM_BWD(T, V, TEAM)                                                                          \
+#define MOE_NORM_BWD(T, V, TEAM, ONCE)                                                                        \
   do {                                                                                                    \
-    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, true>), grid, block, 0, st, a);              \
-    else hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, false>), grid, block, 0, st, a);                  \
+    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, true, ONCE>), grid, block, 0, st, a);        \
+    else hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, false, ONCE>), grid, block, 0, st, a);            \
   } while (0)
 #define MOE_NORM_BWD_BY_PLAN(T)                                   \
   do {                                                            \
-    if (p.team == kLongTeam) MOE_NORM_BWD(T, 2, kLongTeam);       \
-    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, 1, kBlockTeam); \
-    else if (p.V == 2) MOE_NORM_BWD(T, 2, kWaveTeam);             \
-    else MOE_NORM_BWD(T, 1, kWaveTeam);                           \
+    if (p.team == kLongTeam) MOE_NORM_BWD(T, 2, kLongTeam, false);       \
+    else if (p.team == kBlockTeam && p.V == 2 && once) MOE_NORM_BWD(T, 2, kBlockTeam, true); \
+    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_BWD(T, 2, kBlockTeam, false); \
+    else if (p.team == kBlockTeam && !once) MOE_NORM_BWD(T, 1, kBlockTeam, false); \
+    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, 1, kBlockTeam, true); \
+    else if (p.V == 2 && !once) MOE_NORM_BWD(T, 2, kWaveTeam, false); \
+    else if (p.V == 2) MOE_NORM_BWD(T, 2, kWaveTeam, true);             \
+    else if (!once) MOE_NORM_BWD(T, 1, kWaveTeam, false);           \
+    else MOE_NORM_BWD(T, 1, kWaveTeam, true);                           \
   } while (0)
     if (norm->dtype == MOE_F32) MOE_NORM_BWD_BY_PLAN(float);
     else MOE_NORM_BWD_BY_PLAN(bf16_t);
