@@ -421,8 +421,13 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial
   float s = 0.f;
   if (col < d) {
     const float* p = partial + (size_t)blockIdx.y * d + col;
-#pragma unroll 16
-    for (int q = threadIdx.x >> 5; q < blocks; q += 32) s += p[(size_t)q * 2 * d];
+    for (int q = threadIdx.x >> 5; q < blocks; q += 32 * 8) {  // eight loads in flight, the last ones, too
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; u++) v[u] = p[(size_t)min(q + 32 * u, blocks - 1) * 2 * d];
+#pragma unroll
+      for (int u = 0; u < 8; u++) s += q + 32 * u < blocks ? v[u] : 0.f;
+    }
   }
   s = add_rows32(s);
   if ((threadIdx.x & 63) < 32) part[threadIdx.x >> 6][lane] = s;
@@ -453,6 +458,11 @@ struct NormPlan {
 static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
   const int pieces = (n->d + 7) / 8, rows = n->n_rows;
   const auto at_most = [](int x, int most) { return x < most ? x : most; };
+  const auto evenly = [&](int teams, int blocks) {  // no more blocks of so many teams than give the same number of rounds
+    if (rows == 0) return 0;
+    const int per = (rows + teams * blocks - 1) / (teams * blocks);
+    return (rows + teams * per - 1) / (teams * per);
+  };
   NormPlan p = {};
   const auto own_columns = [&](int waves) {
     const int side = n->dtype == MOE_F32 ? 4 : 8;  // pieces of 128 bytes
@@ -464,7 +474,7 @@ static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
     p.waves = 4;
     own_columns(p.waves);
     p.blocks = at_most((rows + 3) / 4, 2048);
-    if (backward && !p.columns) p.blocks = at_most(p.blocks, at_most(rows / 6 + 64, 768));
+    if (backward && !p.columns) p.blocks = evenly(4, at_most(p.blocks, at_most(rows / 6 + 64, 768)));
     return p;
   }
   const bool two = pieces > 1024 || (pieces > 256 && rows > 1024);
@@ -474,7 +484,7 @@ static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
   if (!two) own_columns(p.waves);
   p.blocks = (backward && two && p.team == kBlockTeam ? 2048 : 4096) / p.waves / 256 * 256;  // 256 units, the same number of blocks each: one at least, of 16 wavefronts, or of 8
   if (p.blocks > 2048) p.blocks = 2048;
-  if (backward && !p.columns) p.blocks = at_most(p.blocks, rows / 4 + 64);
+  if (backward && !p.columns) p.blocks = evenly(1, at_most(p.blocks, rows / 4 + 64));
   p.blocks = at_most(p.blocks, rows);
   return p;
 }
