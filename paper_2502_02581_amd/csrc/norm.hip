@@ -252,9 +252,11 @@ __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
   }
 }
 
-// ONCE: nobody else reads the rows; with blocks of columns beside those of rows they would miss them (1000 x 4096: 16.3 us for 13.0).
+// ONCE: streaming hints on the loads of rows.  With a dZ the rows are a residual stream's, four arrays of them, and the hints make the pass quicker (8192 x 4096: 60 us for
+// 61.5); without one they make the forward pass behind it slower by more (8192 x 4096: 37.7 us for 28.5, both passes 82 for 73; 8192 x 7168 both 138 for 136).  Blocks of
+// columns read the rows beside those of rows: no hints there.
 template <typename T, int V, int TEAM, bool DROP, bool ONCE>
-__global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_bwd_kernel(NormBwd a) {
+__global__ __launch_bounds__(TEAM == kWaveTeam || (TEAM == kBlockTeam && V == 2) ? 512 : 1024) void norm_bwd_kernel(NormBwd a) {
   constexpr bool WIDE = TEAM != kWaveTeam;
   if ((TEAM == kWaveTeam || V == 1) && (int)blockIdx.x >= a.row_blocks) return norm_columns<T>(a, blockIdx.x - a.row_blocks);
   __shared__ RowSums<3> sums;
@@ -449,7 +451,8 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial
 //    blocks where they would get less than four rows (six, for teams of a wavefront): their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks
 //    9.7 + 3.4 us, 1024 11.0 + 5.0, 256 12.2 + 4.1);
 //  - where blocks of columns have sixteen rows a lane at most, in 8 MB, they are in the same launch as the rows (256 x 4096: 5.2 us for 6.8 + 3.3, 1000 x 4096 13.0 for 11.6 + 4.4,
-//    512 x 1000 8.1 for 5.8 + 3.2; with 31 rows a lane, 1000 x 512, 12.6 for 5.1 + 4.4).
+//    512 x 1000 6.3 for 5.8 + 3.2; with more, eight wavefronts, 1000 x 512, 8.5 for 5.1 + 2.9, 2000 x 333 fp32 18.2 for 6.4 + 3.0).  For teams of a wavefront that is
+//    counted for four a block, but beside blocks of columns they are eight: as many again share the columns' rows (777 x 333 fp32: 8.1 us for 11.0, 512 x 1000 6.3 for 8.3).
 struct NormPlan {
   int V, team, waves, blocks;
   int columns;  // blocks for the weights' gradients, in the same launch; 0: a launch of their own, from the blocks' sums
@@ -471,9 +474,9 @@ static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
   if (pieces <= 128) {
     p.V = pieces <= 64 ? 1 : 2;
     p.team = kWaveTeam;
-    p.waves = 4;
-    own_columns(p.waves);
-    p.blocks = at_most((rows + 3) / 4, 2048);
+    own_columns(4);
+    p.waves = p.columns ? 8 : 4;
+    p.blocks = at_most((rows + p.waves - 1) / p.waves, 2048);
     if (backward && !p.columns) p.blocks = evenly(4, at_most(p.blocks, at_most(rows / 6 + 64, 768)));
     return p;
   }
