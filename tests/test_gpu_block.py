@@ -286,6 +286,69 @@ def test_two_graphs_on_one_workspace():
         one()
 
 
+def test_two_streams_at_once():
+    """The same calls on two streams side by side, each with tensors and a workspace of its own: the bits of one after the other.  A row of 16384 values, weights' gradients from
+    the blocks' sums and from the columns, sequences of many chunks, the small call's single launch and the loss that the last block writes."""
+    import paper_2502_02581_amd as moe
+
+    class Calls:
+        def __init__(self, seed):
+            g = torch.Generator().manual_seed(seed)
+            self.jobs, self.outs = [], []
+            for n, d in ((6000, 1000), (200, 1000), (40, 16384)):
+                X, dY = torch.randn(n, d, generator=g).bfloat16().to(DEV), torch.randn(n, d, generator=g).bfloat16().to(DEV)
+                norm, Z, Y, dR, dX = moe.MoENorm(n, d), *(torch.empty_like(X) for _ in range(4))
+                drop = moe.MoEDropout(0.3, torch.tensor([seed, 5], dtype=torch.int64, device=DEV), 2)
+                mean, rstd, dw, db = (torch.empty(m, device=DEV) for m in (n, n, d, d))
+                w, dw, db = torch.ones(d, device=DEV).bfloat16(), dw.bfloat16(), db.bfloat16()
+                self.jobs.append(("norm", norm, X, dY, w, drop, Z, Y, dR, dX, mean, rstd, dw, db, self.space(moe.moe_norm_bwd_workspace_bytes(norm))))
+                self.outs += [Z, Y, dR, dX, mean, rstd, dw, db]
+            for T, E, S in ((9000, 60, 3), (100, 16, 4), (5000, 8, 2500)):
+                logits = torch.randn(T, E, generator=g).to(DEV)
+                topk, start = torch.topk(logits, 2, 1).indices.to(torch.int32), torch.tensor([T * i // S for i in range(S + 1)], dtype=torch.int32, device=DEV)
+                shape, dl, counts = moe.MoEShape(T, 8, E, 2, 8, "f32"), torch.empty_like(logits), torch.empty(S, E, dtype=torch.int32, device=DEV)
+                P, loss, coef = torch.empty(S, E, device=DEV), torch.empty(2, device=DEV), torch.empty(S + 1, device=DEV)
+                self.jobs.append(("seq", shape, logits, topk, start, counts, P, loss, coef, dl, self.space(moe.moe_seq_loss_workspace_bytes(shape, S))))
+                self.outs += [P, loss, coef, dl]
+
+        @staticmethod
+        def space(n):
+            return torch.full((n,), 255, dtype=torch.uint8, device=DEV)
+
+        def issue(self, job):
+            if job[0] == "norm":
+                _, norm, X, dY, w, drop, Z, Y, dR, dX, mean, rstd, dw, db, ws = job
+                moe.moe_norm_fwd(norm, X, w, None, Y, mean, rstd, R=dY, drop=drop, Z=Z)
+                moe.moe_norm_bwd(norm, dY, Z, w, mean, rstd, dR, dw, db, ws, drop=drop, dX=dX)
+            else:
+                _, shape, logits, topk, start, counts, P, loss, coef, dl, ws = job
+                moe.moe_seq_loss(shape, logits, topk, start, None, 0.1, 0.1, counts, P, loss, coef, ws)
+                moe.moe_seq_loss_bwd(shape, logits, start, None, counts, coef, 1.0, False, dl)
+
+    sides = [Calls(1), Calls(2)]
+    want = []
+    for c in sides:
+        for job in c.jobs:
+            c.issue(job)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in c.outs])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(6):
+        for c in sides:
+            for t in c.outs:
+                t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        n = len(sides[0].jobs)
+        for i in range(n):   # the two streams' jobs shifted against each other
+            for j, (c, s) in enumerate(zip(sides, streams)):
+                with torch.cuda.stream(s):
+                    c.issue(c.jobs[(i + j * turn) % n])
+        torch.cuda.synchronize()
+        for c, w in zip(sides, want):
+            for k, (t, r) in enumerate(zip(c.outs, w)):
+                assert torch.equal(t, r), (turn, k)
+
+
 def test_clipping_a_blocks_gradients():
     """gradients() lists the router's and the norm's, too."""
     import paper_2502_02581_amd as moe
