@@ -50,7 +50,7 @@ __device__ __forceinline__ void load_weights(const void* w, int wf32, int col, i
 // the backward pass of 1000 x 4096 right behind takes 15.7 us for 13.0)
 enum { kPlain = 0, kAdd = 1, kDrop = 2, kPass = 3 };
 
-// TEAM: who works on a row.  A wavefront of the block's four; the block; or (rows of more than 8192 values) a block of up to sixteen wavefronts, whose lanes have too few
+// TEAM: who works on a row.  A wavefront; the block; or (rows of more than 8192 values) a block of up to sixteen wavefronts, whose lanes have too few
 // registers to hold the next row as well, or, in the backward pass, this one.
 enum { kWaveTeam = 0, kBlockTeam = 1, kLongTeam = 2 };
 
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(TEAM == kWaveTeam || (TEAM == kBlockTeam && V == 2)
     }
   }
   if (!a.partial) return;
-  if (WIDE) {
+  auto store_sums = [&] {
     float* p = a.partial + (size_t)blockIdx.x * 2 * a.d;
 #pragma unroll
     for (int v = 0; v < V; v++) {
@@ -390,27 +390,35 @@ __global__ __launch_bounds__(TEAM == kWaveTeam || (TEAM == kBlockTeam && V == 2)
       o.set(db[v]);
       store_piece(o, p + a.d + col, valid[v]);
     }
-  } else {  // the wavefronts of the block, one after the other
-    __shared__ float all[2][64 * 8 * V];
-    for (int q = 0; q < n_waves; q++) {
-      if (wave == q) {
+  };
+  if (WIDE) {
+    store_sums();
+  } else {  // the upper half of the wavefronts to the lower half, until one is left
+    __shared__ float4 all[4][V * 4][64];
+    for (int half = n_waves / 2; half > 0; half /= 2) {
+      if (wave >= half && wave < 2 * half) {
 #pragma unroll
         for (int v = 0; v < V; v++)
 #pragma unroll
-          for (int j = 0; j < 8; j++) {
-            const int at = (v * 8 + j) * 64 + lane;
-            all[0][at] = q ? all[0][at] + dw[v][j] : dw[v][j];
-            all[1][at] = q ? all[1][at] + db[v][j] : db[v][j];
+          for (int j = 0; j < 8; j += 4) {
+            all[wave - half][4 * v + j / 4][lane] = make_float4(dw[v][j], dw[v][j + 1], dw[v][j + 2], dw[v][j + 3]);
+            all[wave - half][4 * v + 2 + j / 4][lane] = make_float4(db[v][j], db[v][j + 1], db[v][j + 2], db[v][j + 3]);
+          }
+      }
+      __syncthreads();
+      if (wave < half) {
+#pragma unroll
+        for (int v = 0; v < V; v++)
+#pragma unroll
+          for (int j = 0; j < 8; j += 4) {
+            const float4 x = all[wave][4 * v + j / 4][lane], y = all[wave][4 * v + 2 + j / 4][lane];
+            dw[v][j] += x.x, dw[v][j + 1] += x.y, dw[v][j + 2] += x.z, dw[v][j + 3] += x.w;
+            db[v][j] += y.x, db[v][j + 1] += y.y, db[v][j + 2] += y.z, db[v][j + 3] += y.w;
           }
       }
       __syncthreads();
     }
-    float* p = a.partial + (size_t)blockIdx.x * 2 * a.d;
-    for (int col = threadIdx.x; col < a.d; col += blockDim.x) {
-      const int c = col >> 3, at = ((c >> 6) * 8 + (col & 7)) * 64 + (c & 63);
-      p[col] = all[0][at];
-      p[a.d + col] = all[1][at];
-    }
+    if (wave == 0) store_sums();
   }
 }
 
@@ -444,15 +452,17 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial
 }
 
 // Pieces of a lane, wavefronts of a row, blocks.  Measured (T rows of d, bf16 unless it says otherwise):
-//  - rows of up to 1024 values take a wavefront (16384 x 768 backward: 18.5 us, with a block of two wavefronts 20.2), four a block;
+//  - rows of up to 1024 values take a wavefront (16384 x 768 backward: 18.5 us, with a block of two wavefronts 20.2), four a block; in the backward pass eight, whose sums of
+//    the weights' gradients are one, in as many blocks as the registers of 256 units hold at once (65536 x 256: 512 blocks 27.5 us, 384 34.7, 768 30.3, blocks of four 31.5;
+//    6000 x 1000 fp32: 256 blocks 16.8, 384 20.4, 512 20.1, of four 19.9);
 //  - longer ones a block whose lanes hold one piece, or two where rows are long and many: half as many wavefronts take part in a row's barriers (forward 8192 x 7168: 44.0 us for
 //    49.6, 8192 x 2048: 20.4 for 18.5, 500 x 4096: 5.9 for 5.1; both passes of 8192 x 7168 121 for 136, of 8192 x 4096 70.1 for 72.9);
 //  - 16 wavefronts a unit, each with the next row's loads under way, reach the copy's rate, in the backward pass with two pieces a lane eight.  The backward pass takes fewer
-//    blocks where they would get less than four rows (six, for teams of a wavefront): their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks
-//    9.7 + 3.4 us, 1024 11.0 + 5.0, 256 12.2 + 4.1);
+//    blocks where they would get less than four rows: their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks 9.7 + 3.4 us, 1024 11.0 + 5.0,
+//    256 12.2 + 4.1);
 //  - where blocks of columns have sixteen rows a lane at most, in 8 MB, they are in the same launch as the rows (256 x 4096: 5.2 us for 6.8 + 3.3, 1000 x 4096 13.0 for 11.6 + 4.4,
-//    512 x 1000 6.3 for 5.8 + 3.2; with more, eight wavefronts, 1000 x 512, 8.5 for 5.1 + 2.9, 2000 x 333 fp32 18.2 for 6.4 + 3.0).  For teams of a wavefront that is
-//    counted for four a block, but beside blocks of columns they are eight: as many again share the columns' rows (777 x 333 fp32: 8.1 us for 11.0, 512 x 1000 6.3 for 8.3).
+//    512 x 1000 6.3 for 5.8 + 3.2; 1000 x 512 8.5 for 4.6 + 2.9, 2000 x 333 fp32 18.2 for 5.6 + 3.0).  The blocks of eight wavefronts, beside rows of up to 1024
+//    values, count as half their size (with eight rows a lane 777 x 333 fp32 takes 8.1 us, with sixteen, in blocks of four, 11.0).
 struct NormPlan {
   int V, team, waves, blocks;
   int columns;  // blocks for the weights' gradients, in the same launch; 0: a launch of their own, from the blocks' sums
@@ -475,9 +485,9 @@ static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
     p.V = pieces <= 64 ? 1 : 2;
     p.team = kWaveTeam;
     own_columns(4);
-    p.waves = p.columns ? 8 : 4;
+    p.waves = backward ? 8 : 4;
     p.blocks = at_most((rows + p.waves - 1) / p.waves, 2048);
-    if (backward && !p.columns) p.blocks = evenly(4, at_most(p.blocks, at_most(rows / 6 + 64, 768)));
+    if (backward && !p.columns) p.blocks = evenly(8, at_most(p.blocks, 512 / p.V));
     return p;
   }
   const bool two = pieces > 1024 || (pieces > 256 && rows > 1024);
