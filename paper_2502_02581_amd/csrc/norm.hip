@@ -50,20 +50,28 @@ __device__ __forceinline__ void load_weights(const void* w, int wf32, int col, i
 // the backward pass of 1000 x 4096 right behind takes 15.7 us for 13.0)
 enum { kPlain = 0, kAdd = 1, kDrop = 2, kPass = 3 };
 
-// TEAM: who works on a row.  A wavefront; the block; or (rows of more than 8192 values) a block of up to sixteen wavefronts, whose lanes have too few
-// registers to hold the next row as well, or, in the backward pass, this one.
-enum { kWaveTeam = 0, kBlockTeam = 1, kLongTeam = 2 };
+// TEAM: who works on a row.  Sixteen or thirty-two lanes; a wavefront; the block; or (rows of more than 8192 values) a block of up to sixteen wavefronts, whose lanes have
+// too few registers to hold the next row as well, or, in the backward pass, this one.
+enum { kWaveTeam = 0, kBlockTeam = 1, kLongTeam = 2, kLanes16Team = 3, kLanes32Team = 4 };
+constexpr bool wide_team(int team) { return team == kBlockTeam || team == kLongTeam; }
+constexpr int lanes_of(int team) { return team == kLanes16Team ? 16 : team == kLanes32Team ? 32 : 64; }
+// over the lanes of a team that is no block (whose lanes are active alike)
+template <int TEAM>
+__device__ __forceinline__ float team_sum(float x) {
+  return TEAM == kLanes16Team ? row16_sum(x) : TEAM == kLanes32Team ? add_rows16(row16_sum(x)) : lanes_sum(x);
+}
 
 // Rows far from zero: the rounding error of the mean would be that of every value of the row.  delta, the mean of z - m, puts it right, so that they lose nothing but
 // what their own values have lost (mean 1e4, deviation 1, fp32).  Where the mean is below the deviation its error is below the deviation's, and delta would bring in the
 // roundings of z - m, which have one sign for all z of a binade; there it is left out.
 template <typename T, int V, int TEAM, int MODE>
-__global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_fwd_kernel(NormFwd a) {
-  constexpr bool WIDE = TEAM != kWaveTeam, ADD = MODE == kAdd || MODE == kDrop;
+__global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_fwd_kernel(NormFwd a) {
+  constexpr bool WIDE = wide_team(TEAM), ADD = MODE == kAdd || MODE == kDrop;
+  constexpr int LANES = lanes_of(TEAM);
   __shared__ RowSums<2> sums;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-  const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? gridDim.x : gridDim.x * n_waves;
-  const int first = WIDE ? threadIdx.x : lane, step = WIDE ? blockDim.x : kWave;
+  const int wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6, block_teams = WIDE ? 1 : blockDim.x / LANES;
+  const int team = WIDE ? blockIdx.x : blockIdx.x * block_teams + threadIdx.x / LANES, n_teams = gridDim.x * block_teams;
+  const int first = WIDE ? threadIdx.x : threadIdx.x % LANES, step = WIDE ? blockDim.x : LANES;
   const T *X = (const T*)a.X, *R = (const T*)a.R;
   T *Z = (T*)a.Z, *Y = (T*)a.Y;
   const DropKey key = MODE == kDrop ? drop_key(a.drop) : DropKey{};
@@ -120,7 +128,7 @@ __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V =
 #pragma unroll
         for (int j = 0; j < 8; j++) s[0] += z[v][j];
       if (WIDE) sums.sum(s, wave, n_waves, turn);
-      else s[0] = lanes_sum(s[0]);
+      else s[0] = team_sum<TEAM>(s[0]);
       m = s[0] * inv_d;
       float t[2] = {0.f, 0.f};
 #pragma unroll
@@ -136,8 +144,8 @@ __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V =
       if (WIDE) {
         sums.sum(t, wave, n_waves, turn);
       } else {
-        t[0] = lanes_sum(t[0]);
-        t[1] = lanes_sum(t[1]);
+        t[0] = team_sum<TEAM>(t[0]);
+        t[1] = team_sum<TEAM>(t[1]);
       }
       var = t[1] / (float)a.d;
       if (m * m > var) {
@@ -151,7 +159,7 @@ __global__ __launch_bounds__(TEAM == kWaveTeam ? 256 : TEAM == kBlockTeam && V =
 #pragma unroll
         for (int j = 0; j < 8; j++) t[0] = fmaf(z[v][j], z[v][j], t[0]);
       if (WIDE) sums.sum(t, wave, n_waves, turn);
-      else t[0] = lanes_sum(t[0]);
+      else t[0] = team_sum<TEAM>(t[0]);
       var = t[0] / (float)a.d;
     }
     const float rstd = 1.f / sqrtf(var + a.eps);
@@ -256,13 +264,14 @@ __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
 // 61.5); without one they make the forward pass behind it slower by more (8192 x 4096: 37.7 us for 28.5, both passes 82 for 73; 8192 x 7168 both 138 for 136).  Blocks of
 // columns read the rows beside those of rows: no hints there.
 template <typename T, int V, int TEAM, bool DROP, bool ONCE>
-__global__ __launch_bounds__(TEAM == kWaveTeam || (TEAM == kBlockTeam && V == 2) ? 512 : 1024) void norm_bwd_kernel(NormBwd a) {
-  constexpr bool WIDE = TEAM != kWaveTeam;
-  if ((TEAM == kWaveTeam || V == 1) && (int)blockIdx.x >= a.row_blocks) return norm_columns<T>(a, blockIdx.x - a.row_blocks);
+__global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) ? 512 : 1024) void norm_bwd_kernel(NormBwd a) {
+  constexpr bool WIDE = wide_team(TEAM);
+  constexpr int LANES = lanes_of(TEAM);
+  if ((!WIDE || V == 1) && (int)blockIdx.x >= a.row_blocks) return norm_columns<T>(a, blockIdx.x - a.row_blocks);
   __shared__ RowSums<3> sums;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-  const int team = WIDE ? blockIdx.x : blockIdx.x * n_waves + wave, n_teams = WIDE ? a.row_blocks : a.row_blocks * n_waves;
-  const int first = WIDE ? threadIdx.x : lane, step = WIDE ? blockDim.x : kWave;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6, block_teams = WIDE ? 1 : blockDim.x / LANES;
+  const int team = WIDE ? blockIdx.x : blockIdx.x * block_teams + threadIdx.x / LANES, n_teams = a.row_blocks * block_teams;
+  const int first = WIDE ? threadIdx.x : threadIdx.x % LANES, step = WIDE ? blockDim.x : LANES;
   const T *dY = (const T*)a.dY, *Z = (const T*)a.Z, *dZ = (const T*)a.dZ;
   T *dR = (T*)a.dR, *dX = (T*)a.dX;
   const DropKey key = DROP ? drop_key(a.drop) : DropKey{};
@@ -362,7 +371,7 @@ __global__ __launch_bounds__(TEAM == kWaveTeam || (TEAM == kBlockTeam && V == 2)
       sums.sum(s, wave, n_waves, turn);
     } else {
 #pragma unroll
-      for (int i = 0; i < 3; i++) s[i] = lanes_sum(s[i]);
+      for (int i = 0; i < 3; i++) s[i] = team_sum<TEAM>(s[i]);
     }
     delta = fabsf(m) * rstd > 1.f ? s[2] * inv_d : 0.f;  // (no mean, no delta)
     s1 = a.layer ? s[0] * inv_d : 0.f;
@@ -393,7 +402,16 @@ __global__ __launch_bounds__(TEAM == kWaveTeam || (TEAM == kBlockTeam && V == 2)
   };
   if (WIDE) {
     store_sums();
-  } else {  // the upper half of the wavefronts to the lower half, until one is left
+  } else {  // the teams of a wavefront, then the upper half of the wavefronts to the lower half, until one is left
+    if (LANES < 64) {
+#pragma unroll
+      for (int v = 0; v < V; v++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          dw[v][j] = add_rows32(LANES == 16 ? add_rows16(dw[v][j]) : dw[v][j]);
+          db[v][j] = add_rows32(LANES == 16 ? add_rows16(db[v][j]) : db[v][j]);
+        }
+    }
     __shared__ float4 all[4][V * 4][64];
     for (int half = n_waves / 2; half > 0; half /= 2) {
       if (wave >= half && wave < 2 * half) {
@@ -418,7 +436,7 @@ __global__ __launch_bounds__(TEAM == kWaveTeam || (TEAM == kBlockTeam && V == 2)
       }
       __syncthreads();
     }
-    if (wave == 0) store_sums();
+    if (threadIdx.x < LANES) store_sums();
   }
 }
 
@@ -483,11 +501,12 @@ static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
   };
   if (pieces <= 128) {
     p.V = pieces <= 64 ? 1 : 2;
-    p.team = kWaveTeam;
+    p.team = pieces <= 16 ? kLanes16Team : pieces <= 32 ? kLanes32Team : kWaveTeam;
     own_columns(4);
     p.waves = backward ? 8 : 4;
-    p.blocks = at_most((rows + p.waves - 1) / p.waves, 2048);
-    if (backward && !p.columns) p.blocks = evenly(8, at_most(p.blocks, 512 / p.V));
+    const int teams = p.waves * (64 / lanes_of(p.team));
+    p.blocks = at_most((rows + teams - 1) / teams, 2048);
+    if (backward && !p.columns) p.blocks = evenly(teams, at_most(p.blocks, 512 / p.V));
     return p;
   }
   const bool two = pieces > 1024 || (pieces > 256 && rows > 1024);
@@ -573,6 +592,8 @@ extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, 
     else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_FWD(T, 2, kBlockTeam); \
     else if (p.team == kBlockTeam) MOE_NORM_FWD(T, 1, kBlockTeam);           \
     else if (p.V == 2) MOE_NORM_FWD(T, 2, kWaveTeam);                        \
+    else if (p.team == kLanes16Team) MOE_NORM_FWD(T, 1, kLanes16Team);       \
+    else if (p.team == kLanes32Team) MOE_NORM_FWD(T, 1, kLanes32Team);       \
     else MOE_NORM_FWD(T, 1, kWaveTeam);                                      \
   } while (0)
 #define MOE_NORM_FWD(T, V, TEAM)                                                                                \
@@ -637,27 +658,31 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
     const dim3 grid(p.blocks + (weights ? p.columns : 0)), block(64 * p.waves);
     const bool once = dZ && !p.columns;
     ProfScope prof("norm_bwd_kernel", st);
-#define MOE_NORM_BWD(T, V, TEAM, ONCE)                                                                        \
-  do {                                                                                                    \
-    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, true, ONCE>), grid, block, 0, st, a);        \
-    else hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, false, ONCE>), grid, block, 0, st, a);            \
+#define MOE_NORM_BWD_AS(T, V, TEAM, ONCE)                                                          \
+  do {                                                                                             \
+    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, true, ONCE>), grid, block, 0, st, a); \
+    else hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, false, ONCE>), grid, block, 0, st, a);     \
   } while (0)
-#define MOE_NORM_BWD_BY_PLAN(T)                                   \
-  do {                                                            \
-    if (p.team == kLongTeam) MOE_NORM_BWD(T, 2, kLongTeam, false);       \
-    else if (p.team == kBlockTeam && p.V == 2 && once) MOE_NORM_BWD(T, 2, kBlockTeam, true); \
-    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_BWD(T, 2, kBlockTeam, false); \
-    else if (p.team == kBlockTeam && !once) MOE_NORM_BWD(T, 1, kBlockTeam, false); \
-    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, 1, kBlockTeam, true); \
-    else if (p.V == 2 && !once) MOE_NORM_BWD(T, 2, kWaveTeam, false); \
-    else if (p.V == 2) MOE_NORM_BWD(T, 2, kWaveTeam, true);             \
-    else if (!once) MOE_NORM_BWD(T, 1, kWaveTeam, false);           \
-    else MOE_NORM_BWD(T, 1, kWaveTeam, true);                           \
+#define MOE_NORM_BWD(T, V, TEAM)                       \
+  do {                                                 \
+    if (once) MOE_NORM_BWD_AS(T, V, TEAM, true);       \
+    else MOE_NORM_BWD_AS(T, V, TEAM, false);           \
+  } while (0)
+#define MOE_NORM_BWD_BY_PLAN(T)                                                 \
+  do {                                                                          \
+    if (p.team == kLongTeam) MOE_NORM_BWD_AS(T, 2, kLongTeam, false);           \
+    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_BWD(T, 2, kBlockTeam);  \
+    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, 1, kBlockTeam);              \
+    else if (p.V == 2) MOE_NORM_BWD(T, 2, kWaveTeam);                           \
+    else if (p.team == kLanes16Team) MOE_NORM_BWD(T, 1, kLanes16Team);          \
+    else if (p.team == kLanes32Team) MOE_NORM_BWD(T, 1, kLanes32Team);          \
+    else MOE_NORM_BWD(T, 1, kWaveTeam);                                         \
   } while (0)
     if (norm->dtype == MOE_F32) MOE_NORM_BWD_BY_PLAN(float);
     else MOE_NORM_BWD_BY_PLAN(bf16_t);
 #undef MOE_NORM_BWD_BY_PLAN
 #undef MOE_NORM_BWD
+#undef MOE_NORM_BWD_AS
   }
   if (weights && (n == 0 || !p.columns)) {
     ProfScope prof("norm_weights_kernel", st);
