@@ -20,14 +20,14 @@ struct DropoutArgs {
 // A block takes kDropThreads * U neighbouring pieces, numbered through the rows.  Their rows: the block's first one by a 64-bit division, the others by a product with
 // the reciprocal, which is exact for numbers below per_row + kDropThreads * U (per_row up to 2^15: the product's error is below 2^15 * 2^16 / 2^32 of a row's).
 constexpr int kDropThreads = 256;
-template <typename T, int U>
+template <typename T, int TAIL, int U>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
   const DropKey key = drop_key(a.drop);
   const int64_t base = (int64_t)blockIdx.x * (kDropThreads * U);
   const uint32_t row0 = (uint32_t)(base / a.per_row), off = (uint32_t)(base - (int64_t)row0 * a.per_row);
   Piece<T> x[U], r[U];
   uint32_t row[U], c[U];
-  int valid[U];
+  int valid[U], back[U];
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const uint32_t i = u * kDropThreads + threadIdx.x, q = off + i;
@@ -35,13 +35,16 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
     row[u] = row0 + over;
     c[u] = q - over * a.per_row;
     valid[u] = base + i < a.pieces ? a.cols - 8 * (int)c[u] : 0;
-    load_piece<true>(x[u], (const T*)a.X + (int64_t)row[u] * a.ldx + 8 * c[u], valid[u]);
+    back[u] = piece_back<TAIL>(8 * (int)c[u], valid[u]);
+    load_piece<TAIL, true>(x[u], (const T*)a.X + (int64_t)row[u] * a.ldx + 8 * c[u], valid[u], back[u]);
     r[u].clear();
-    if (a.R) load_piece<true>(r[u], (const T*)a.R + (int64_t)row[u] * a.ldr + 8 * c[u], valid[u]);
+    if (a.R) load_piece<TAIL, true>(r[u], (const T*)a.R + (int64_t)row[u] * a.ldr + 8 * c[u], valid[u], back[u]);
   }
 #pragma unroll
   for (int u = 0; u < U; u++) {
     float v[8], add[8];
+    settle<TAIL>(x[u], back[u]);
+    settle<TAIL>(r[u], back[u]);
     x[u].values(v);
     r[u].values(add);
     if (a.drop.threshold) {
@@ -51,7 +54,7 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
       for (int j = 0; j < 8; j++) v[j] += add[j];
     }
     x[u].set(v);
-    store_piece(x[u], (T*)a.out + (int64_t)row[u] * a.ldo + 8 * c[u], valid[u]);
+    store_piece<TAIL>(x[u], (T*)a.out + (int64_t)row[u] * a.ldo + 8 * c[u], valid[u]);
   }
 }
 
@@ -138,7 +141,9 @@ extern "C" int moe_dropout(const void* X, int64_t ldx, const void* R, int64_t ld
     return MOE_EINVAL;
   }
   ProfScope prof("dropout_kernel", st);
-  if (dtype == MOE_F32) hipLaunchKernelGGL((dropout_kernel<float, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
-  else hipLaunchKernelGGL((dropout_kernel<bf16_t, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
+  if (dtype == MOE_F32) hipLaunchKernelGGL((dropout_kernel<float, kByValue, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
+  else if (cols % 8 == 0) hipLaunchKernelGGL((dropout_kernel<bf16_t, kNoTail, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
+  else if (cols > 8) hipLaunchKernelGGL((dropout_kernel<bf16_t, kTail, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
+  else hipLaunchKernelGGL((dropout_kernel<bf16_t, kTinyTail, U>), dim3((unsigned)blocks), dim3(kDropThreads), 0, st, a);
   return launch_status(who);
 }

@@ -37,11 +37,13 @@ __device__ __forceinline__ void load_weights(const void* w, int wf32, int col, i
     for (int j = 0; j < 8; j++) v[j] = fill;
   } else if (wf32) {
     Piece<float> p;
-    load_piece(p, (const float*)w + col, valid);
+    load_piece<kByValue>(p, (const float*)w + col, valid, 0);
     p.values(v);
   } else {
     Piece<bf16_t> p;
-    load_piece(p, (const bf16_t*)w + col, valid);
+    const int back = piece_back<kTinyTail>(col, valid);
+    load_piece<kTinyTail>(p, (const bf16_t*)w + col, valid, back);
+    settle<kTinyTail>(p, back);
     p.values(v);
   }
 }
@@ -64,7 +66,7 @@ __device__ __forceinline__ float team_sum(float x) {
 // Rows far from zero: the rounding error of the mean would be that of every value of the row.  delta, the mean of z - m, puts it right, so that they lose nothing but
 // what their own values have lost (mean 1e4, deviation 1, fp32).  Where the mean is below the deviation its error is below the deviation's, and delta would bring in the
 // roundings of z - m, which have one sign for all z of a binade; there it is left out.
-template <typename T, int V, int TEAM, int MODE>
+template <typename T, int TAIL, int V, int TEAM, int MODE>
 __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V == 2 ? 512 : 1024) void norm_fwd_kernel(NormFwd a) {
   constexpr bool WIDE = wide_team(TEAM), ADD = MODE == kAdd || MODE == kDrop;
   constexpr int LANES = lanes_of(TEAM);
@@ -75,12 +77,13 @@ __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V ==
   const T *X = (const T*)a.X, *R = (const T*)a.R;
   T *Z = (T*)a.Z, *Y = (T*)a.Y;
   const DropKey key = MODE == kDrop ? drop_key(a.drop) : DropKey{};
-  int turn = 0, valid[V];
+  int turn = 0, valid[V], back[V];
   float w[V][8], b[V][8];
 #pragma unroll
   for (int v = 0; v < V; v++) {
     const int col = 8 * (first + v * step);
     valid[v] = a.d - col;
+    back[v] = piece_back<TAIL>(col, valid[v]);
     load_weights(a.w, a.wf32, col, valid[v], 1.f, w[v]);
     load_weights(a.b, a.wf32, col, valid[v], 0.f, b[v]);
   }
@@ -90,10 +93,10 @@ __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V ==
 #pragma unroll
     for (int v = 0; v < V; v++) {
       const int col = 8 * (first + v * step);
-      load_piece<MODE != kPlain>(x[v], X + row * a.ldx + col, valid[v]);
+      load_piece<TAIL, MODE != kPlain>(x[v], X + row * a.ldx + col, valid[v], back[v]);
       if (ADD) {
         r[v].clear();
-        if (R) load_piece<true>(r[v], R + row * a.ldr + col, valid[v]);
+        if (R) load_piece<TAIL, true>(r[v], R + row * a.ldr + col, valid[v], back[v]);
       }
     }
   };
@@ -104,9 +107,11 @@ __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V ==
 #pragma unroll
     for (int v = 0; v < V; v++) {
       const int c = first + v * step;
+      settle<TAIL>(x[v], back[v]);
       x[v].values(z[v]);
       if (ADD) {
         float add[8];
+        settle<TAIL>(r[v], back[v]);
         r[v].values(add);
         if (MODE == kDrop) {
           drop_piece(a.drop, key, c, row, z[v], add);
@@ -115,7 +120,7 @@ __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V ==
           for (int j = 0; j < 8; j++) z[v][j] += add[j];
         }
         x[v].set(z[v]);  // the norm is of the values that are kept
-        store_piece(x[v], Z + row * a.ldz + 8 * c, valid[v]);
+        store_piece<TAIL>(x[v], Z + row * a.ldz + 8 * c, valid[v]);
         x[v].values(z[v]);
       }
     }
@@ -173,7 +178,7 @@ __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V ==
 #pragma unroll
       for (int j = 0; j < 8; j++) z[v][j] = fmaf((z[v][j] - delta) * rstd, w[v][j], b[v][j]);
       y.set(z[v]);
-      store_piece(y, Y + row * a.ldy + 8 * (first + v * step), valid[v]);
+      store_piece<TAIL>(y, Y + row * a.ldy + 8 * (first + v * step), valid[v]);
     }
   }
 }
@@ -181,13 +186,13 @@ __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V ==
 // dw and db of 128 bytes' worth of columns, over all rows: for calls of few rows, where reading these again costs less than another launch.  P lanes side by side hold a row's pieces,
 // as many rows at once as the block has P lanes.  The mean's rounding error, 2^-24 of it, is less than 8 of the deviation's where the mean is below 8 deviations; other rows'
 // lanes look at the whole row for it.
-template <typename T>
+template <typename T, int TAIL>
 __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
   constexpr int P = sizeof(T) == 2 ? 8 : 4, U = 4;
   __shared__ float part[16][2][8 * P];
   const T *dY = (const T*)a.dY, *Z = (const T*)a.Z;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-  const int p = threadIdx.x & (P - 1), col = 8 * (block * P + p), valid = a.d - col, runs = blockDim.x / P;
+  const int p = threadIdx.x & (P - 1), col = 8 * (block * P + p), valid = a.d - col, back = piece_back<TAIL>(col, valid), runs = blockDim.x / P;
   float dw[8], db[8];
 #pragma unroll
   for (int j = 0; j < 8; j++) dw[j] = db[j] = 0.f;
@@ -198,8 +203,8 @@ __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
     for (int u = 0; u < U; u++) {
       const int row = row0 + u * runs;
       const bool there = row < a.n_rows;
-      load_piece(y[u], dY + row * a.lddy + col, there ? valid : 0);
-      load_piece(z[u], Z + row * a.ldz + col, there ? valid : 0);
+      load_piece<TAIL>(y[u], dY + row * a.lddy + col, there ? valid : 0, there ? back : 0);
+      load_piece<TAIL>(z[u], Z + row * a.ldz + col, there ? valid : 0, there ? back : 0);
       m[u] = there && a.layer ? a.mean[row] : 0.f;
       rstd[u] = there ? a.rstd[row] : 0.f;
     }
@@ -213,7 +218,9 @@ __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
         for (int c = p; 8 * c < a.d; c += P) {
           Piece<T> x;
           float v[8];
-          load_piece(x, Z + row * a.ldz + 8 * c, a.d - 8 * c);
+          const int short_of = piece_back<TAIL>(8 * c, a.d - 8 * c);
+          load_piece<TAIL>(x, Z + row * a.ldz + 8 * c, a.d - 8 * c, short_of);
+          settle<TAIL>(x, short_of);
           x.values(v);
 #pragma unroll
           for (int j = 0; j < 8; j++) s += 8 * c + j < a.d ? v[j] - m[u] : 0.f;
@@ -223,6 +230,8 @@ __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
         delta = s / (float)a.d;
       }
       float dy[8], x[8];
+      settle<TAIL>(y[u], back);
+      settle<TAIL>(z[u], back);
       y[u].values(dy);
       z[u].values(x);
 #pragma unroll
@@ -263,11 +272,11 @@ __device__ __forceinline__ void norm_columns(const NormBwd& a, int block) {
 // ONCE: streaming hints on the loads of rows.  With a dZ the rows are a residual stream's, four arrays of them, and the hints make the pass quicker (8192 x 4096: 60 us for
 // 61.5); without one they make the forward pass behind it slower by more (8192 x 4096: 37.7 us for 28.5, both passes 82 for 73; 8192 x 7168 both 138 for 136).  Blocks of
 // columns read the rows beside those of rows: no hints there.
-template <typename T, int V, int TEAM, bool DROP, bool ONCE>
+template <typename T, int TAIL, int V, int TEAM, bool DROP, bool ONCE>
 __global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) ? 512 : 1024) void norm_bwd_kernel(NormBwd a) {
   constexpr bool WIDE = wide_team(TEAM);
   constexpr int LANES = lanes_of(TEAM);
-  if ((!WIDE || V == 1) && (int)blockIdx.x >= a.row_blocks) return norm_columns<T>(a, blockIdx.x - a.row_blocks);
+  if ((!WIDE || V == 1) && (int)blockIdx.x >= a.row_blocks) return norm_columns<T, TAIL>(a, blockIdx.x - a.row_blocks);
   __shared__ RowSums<3> sums;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6, block_teams = WIDE ? 1 : blockDim.x / LANES;
   const int team = WIDE ? blockIdx.x : blockIdx.x * block_teams + threadIdx.x / LANES, n_teams = a.row_blocks * block_teams;
@@ -275,12 +284,13 @@ __global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) 
   const T *dY = (const T*)a.dY, *Z = (const T*)a.Z, *dZ = (const T*)a.dZ;
   T *dR = (T*)a.dR, *dX = (T*)a.dX;
   const DropKey key = DROP ? drop_key(a.drop) : DropKey{};
-  int turn = 0, valid[V];
+  int turn = 0, valid[V], back[V];
   float w[V][8], dw[V][8], db[V][8];
 #pragma unroll
   for (int v = 0; v < V; v++) {
     const int col = 8 * (first + v * step);
     valid[v] = a.d - col;
+    back[v] = piece_back<TAIL>(col, valid[v]);
     load_weights(a.w, a.wf32, col, valid[v], 1.f, w[v]);
 #pragma unroll
     for (int j = 0; j < 8; j++) dw[v][j] = db[v][j] = 0.f;
@@ -291,10 +301,15 @@ __global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) 
   };
   auto load = [&](Loads& p, int row, int v, bool all) {
     const int col = 8 * (first + v * step);
-    load_piece<ONCE>(p.y, dY + row * a.lddy + col, valid[v]);
-    load_piece<ONCE>(p.z, Z + row * a.ldz + col, valid[v]);
-    if (all && dZ) load_piece<ONCE>(p.in, dZ + row * a.lddz + col, valid[v]);
+    load_piece<TAIL, ONCE>(p.y, dY + row * a.lddy + col, valid[v], back[v]);
+    load_piece<TAIL, ONCE>(p.z, Z + row * a.ldz + col, valid[v], back[v]);
+    if (all && dZ) load_piece<TAIL, ONCE>(p.in, dZ + row * a.lddz + col, valid[v], back[v]);
     else p.in.clear();
+  };
+  auto settle_loads = [&](Loads& p, int v) {
+    settle<TAIL>(p.y, back[v]);
+    settle<TAIL>(p.z, back[v]);
+    settle<TAIL>(p.in, back[v]);
   };
   float s[3];  // sums of g, of g (z - m) and, for the mean's rounding error as in the forward pass, of z - m
   float m = 0.f, rstd = 0.f;
@@ -327,13 +342,13 @@ __global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) 
     Piece<T> out;
     if (dR) {
       out.set(o);
-      store_piece(out, dR + row * a.lddr + 8 * c, valid[v]);
+      store_piece<TAIL>(out, dR + row * a.lddr + 8 * c, valid[v]);
     }
     if (DROP) {
       const float zero[8] = {};
       drop_piece(a.drop, key, c, row, o, zero);
       out.set(o);
-      store_piece(out, dX + row * a.lddx + 8 * c, valid[v]);
+      store_piece<TAIL>(out, dX + row * a.lddx + 8 * c, valid[v]);
     }
   };
   Loads next[V];  // the next row: its loads are under way while the one before is worked on
@@ -353,7 +368,10 @@ __global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) 
     rstd = next_rstd;
     if (TEAM != kLongTeam) {
 #pragma unroll
-      for (int v = 0; v < V; v++) now[v] = next[v];
+      for (int v = 0; v < V; v++) {
+        now[v] = next[v];
+        settle_loads(now[v], v);
+      }
     }
     if (row + n_teams < a.n_rows) load_row(row + n_teams);
     s[0] = s[1] = s[2] = 0.f;
@@ -362,6 +380,7 @@ __global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) 
       if (TEAM == kLongTeam) {
         Loads p;
         load(p, row, v, false);
+        settle_loads(p, v);
         add(p, v);
       } else {
         add(now[v], v);
@@ -381,6 +400,7 @@ __global__ __launch_bounds__(!wide_team(TEAM) || (TEAM == kBlockTeam && V == 2) 
       if (TEAM == kLongTeam) {
         Loads p;
         load(p, row, v, true);
+        settle_loads(p, v);
         finish(p, row, v);
       } else {
         finish(now[v], row, v);
@@ -473,20 +493,25 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial
 //  - rows of up to 1024 values take a wavefront (16384 x 768 backward: 18.5 us, with a block of two wavefronts 20.2), four a block; in the backward pass eight, whose sums of
 //    the weights' gradients are one, in as many blocks as the registers of 256 units hold at once (65536 x 256: 512 blocks 27.5 us, 384 34.7, 768 30.3, blocks of four 31.5;
 //    6000 x 1000 fp32: 256 blocks 16.8, 384 20.4, 512 20.1, of four 19.9);
-//  - longer ones a block whose lanes hold one piece, or two where rows are long and many: half as many wavefronts take part in a row's barriers (forward 8192 x 7168: 44.0 us for
-//    49.6, 8192 x 2048: 20.4 for 18.5, 500 x 4096: 5.9 for 5.1; both passes of 8192 x 7168 121 for 136, of 8192 x 4096 70.1 for 72.9);
+//  - longer ones a block whose lanes hold one piece, or two where rows of bf16 are long and many: half as many wavefronts take part in a row's barriers (forward 8192 x 7168:
+//    44.0 us for 49.6, 8000 x 5000 33 for 62, 8192 x 2048 20.4 for 18.5, 500 x 4096 5.9 for 5.1).  In the backward pass only rows of full pieces, long enough for seven or eight
+//    wavefronts a unit, without dropout (8000 x 6000 60 us for 62.5, 8000 x 4096 35.8 for 35.3; with dropout 8000 x 5000 95 for 75, 8000 x 7168 99 for 95, rows of 3500 64 for
+//    55, of 2200 without dropout 32 for 26); nor in fp32, where a piece is 32 bytes (4000 x 5000 37 + 43 us for 31.5 + 41.3);
 //  - 16 wavefronts a unit, each with the next row's loads under way, reach the copy's rate, in the backward pass with two pieces a lane eight.  The backward pass takes fewer
 //    blocks where they would get less than four rows: their sums of the weights' gradients are written and read again (2000 x 2048: 512 blocks 9.7 + 3.4 us, 1024 11.0 + 5.0,
-//    256 12.2 + 4.1);
+//    256 12.2 + 4.1).  Blocks of five wavefronts are two a unit there: of three, 15 wavefronts at four a SIMD, the last does not find its place (8000 x 2200 fp32 37.8 us for
+//    46.3, with dropout 38 for 47; bf16 without, whose registers allow five a SIMD, 28.8 for 25.7);
 //  - where blocks of columns have sixteen rows a lane at most, in 8 MB, they are in the same launch as the rows (256 x 4096: 5.2 us for 6.8 + 3.3, 1000 x 4096 13.0 for 11.6 + 4.4,
 //    512 x 1000 6.3 for 5.8 + 3.2; 1000 x 512 8.5 for 4.6 + 2.9, 2000 x 333 fp32 18.2 for 5.6 + 3.0).  The blocks of eight wavefronts, beside rows of up to 1024
 //    values, count as half their size (with eight rows a lane 777 x 333 fp32 takes 8.1 us, with sixteen, in blocks of four, 11.0).
+// With two pieces a lane bf16 rows take a short piece value by value in the forward pass (8000 x 5001: 43 us for 53, backward settled 91 for 99); so do rows of more than 8192
+// values, for their registers.
 struct NormPlan {
   int V, team, waves, blocks;
   int columns;  // blocks for the weights' gradients, in the same launch; 0: a launch of their own, from the blocks' sums
 };
 // in_place: an output is an input whose columns would be read beside it.
-static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
+static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool drop, bool in_place) {
   const int pieces = (n->d + 7) / 8, rows = n->n_rows;
   const auto at_most = [](int x, int most) { return x < most ? x : most; };
   const auto evenly = [&](int teams, int blocks) {  // no more blocks of so many teams than give the same number of rounds
@@ -509,13 +534,14 @@ static NormPlan norm_plan(const moe_norm_t* n, bool backward, bool in_place) {
     if (backward && !p.columns) p.blocks = evenly(teams, at_most(p.blocks, 512 / p.V));
     return p;
   }
-  const bool two = pieces > 1024 || (pieces > 256 && rows > 1024);
+  const bool two = pieces > 1024 || (pieces > 256 && rows > 1024 && n->dtype == MOE_BF16 && !(backward && (drop || n->d % 8 || pieces <= 448)));
   p.V = two ? 2 : 1;
   p.team = pieces > 1024 ? kLongTeam : kBlockTeam;
   p.waves = (pieces + 64 * p.V - 1) / (64 * p.V);
   if (!two) own_columns(p.waves);
   p.blocks = (backward && two && p.team == kBlockTeam ? 2048 : 4096) / p.waves / 256 * 256;  // 256 units, the same number of blocks each: one at least, of 16 wavefronts, or of 8
   if (p.blocks > 2048) p.blocks = 2048;
+  if (backward && p.waves == 5) p.blocks = at_most(p.blocks, 512);
   if (backward && !p.columns) p.blocks = evenly(1, at_most(p.blocks, rows / 4 + 64));
   p.blocks = at_most(p.blocks, rows);
   return p;
@@ -547,7 +573,7 @@ using namespace moe;
 
 extern "C" size_t moe_norm_bwd_workspace_bytes(const moe_norm_t* norm) {
   if (check_norm(norm, "moe_norm_bwd_workspace_bytes")) return 0;
-  return (size_t)norm_plan(norm, true, true).blocks * 2 * (size_t)norm->d * sizeof(float) + 256;  // (the call's other plan needs none)
+  return (size_t)norm_plan(norm, true, true, true).blocks * 2 * (size_t)norm->d * sizeof(float) + 256;  // (no plan of the call has more)
 }
 
 extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, const void* R, int64_t ldr, const moe_drop_t* drop, const void* w,
@@ -581,30 +607,31 @@ extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, 
     return MOE_EINVAL;
   }
   if (n == 0) return MOE_OK;
-  const NormPlan p = norm_plan(norm, false, false);
+  const NormPlan p = norm_plan(norm, false, false, false);
   const NormFwd a = {X, R, w, b, Z, Y, mean, rstd, ldx, ldr, ldz, ldy, n, d, norm->kind == MOE_NORM_LAYER, norm->wdtype == MOE_F32, norm->eps, dr};
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid(p.blocks), block(64 * p.waves);
   ProfScope prof("norm_fwd_kernel", st);
-#define MOE_NORM_FWD_BY_PLAN(T)                                              \
-  do {                                                                       \
-    if (p.team == kLongTeam) MOE_NORM_FWD(T, 2, kLongTeam);                  \
-    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_FWD(T, 2, kBlockTeam); \
-    else if (p.team == kBlockTeam) MOE_NORM_FWD(T, 1, kBlockTeam);           \
-    else if (p.V == 2) MOE_NORM_FWD(T, 2, kWaveTeam);                        \
-    else if (p.team == kLanes16Team) MOE_NORM_FWD(T, 1, kLanes16Team);       \
-    else if (p.team == kLanes32Team) MOE_NORM_FWD(T, 1, kLanes32Team);       \
-    else MOE_NORM_FWD(T, 1, kWaveTeam);                                      \
+#define MOE_NORM_FWD_BY_PLAN(T, TAIL, TINY, BY_VALUE)                                             \
+  do {                                                                                  \
+    if (p.team == kLongTeam) MOE_NORM_FWD(T, BY_VALUE, 2, kLongTeam);                   \
+    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_FWD(T, BY_VALUE, 2, kBlockTeam); \
+    else if (p.team == kBlockTeam) MOE_NORM_FWD(T, TAIL, 1, kBlockTeam);                \
+    else if (p.V == 2) MOE_NORM_FWD(T, BY_VALUE, 2, kWaveTeam);                         \
+    else if (p.team == kLanes16Team) MOE_NORM_FWD(T, TINY, 1, kLanes16Team);            \
+    else if (p.team == kLanes32Team) MOE_NORM_FWD(T, TAIL, 1, kLanes32Team);            \
+    else MOE_NORM_FWD(T, TAIL, 1, kWaveTeam);                                           \
   } while (0)
-#define MOE_NORM_FWD(T, V, TEAM)                                                                                \
+#define MOE_NORM_FWD(T, TAIL, V, TEAM)                                                                                \
   do {                                                                                                          \
-    if (!sum && rstd) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kPlain>), grid, block, 0, st, a);          \
-    else if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kPass>), grid, block, 0, st, a);              \
-    else if (dr.threshold == 0) hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kAdd>), grid, block, 0, st, a); \
-    else hipLaunchKernelGGL((norm_fwd_kernel<T, V, TEAM, kDrop>), grid, block, 0, st, a);                        \
+    if (!sum && rstd) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kPlain>), grid, block, 0, st, a);          \
+    else if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kPass>), grid, block, 0, st, a);              \
+    else if (dr.threshold == 0) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kAdd>), grid, block, 0, st, a); \
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kDrop>), grid, block, 0, st, a);                        \
   } while (0)
-  if (norm->dtype == MOE_F32) MOE_NORM_FWD_BY_PLAN(float);
-  else MOE_NORM_FWD_BY_PLAN(bf16_t);
+  if (norm->dtype == MOE_F32) MOE_NORM_FWD_BY_PLAN(float, kByValue, kByValue, kByValue);
+  else if (d % 8) MOE_NORM_FWD_BY_PLAN(bf16_t, kTail, kTinyTail, kByValue);
+  else MOE_NORM_FWD_BY_PLAN(bf16_t, kNoTail, kNoTail, kNoTail);
 #undef MOE_NORM_FWD
 #undef MOE_NORM_FWD_BY_PLAN
   return launch_status(who);
@@ -639,7 +666,7 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
     return MOE_EINVAL;
   }
   const bool weights = dw || db;
-  const NormPlan p = norm_plan(norm, true, (dR && (dR == dY || dR == Z)) || (dX && (dX == dY || dX == Z)));
+  const NormPlan p = norm_plan(norm, true, dr.threshold != 0, (dR && (dR == dY || dR == Z)) || (dX && (dX == dY || dX == Z)));
   if (weights) {
     const size_t need = moe_norm_bwd_workspace_bytes(norm);
     if (!ws || !aligned16(ws)) {
@@ -658,28 +685,29 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
     const dim3 grid(p.blocks + (weights ? p.columns : 0)), block(64 * p.waves);
     const bool once = dZ && !p.columns;
     ProfScope prof("norm_bwd_kernel", st);
-#define MOE_NORM_BWD_AS(T, V, TEAM, ONCE)                                                          \
+#define MOE_NORM_BWD_AS(T, TAIL, V, TEAM, ONCE)                                                          \
   do {                                                                                             \
-    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, true, ONCE>), grid, block, 0, st, a); \
-    else hipLaunchKernelGGL((norm_bwd_kernel<T, V, TEAM, false, ONCE>), grid, block, 0, st, a);     \
+    if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, TAIL, V, TEAM, true, ONCE>), grid, block, 0, st, a); \
+    else hipLaunchKernelGGL((norm_bwd_kernel<T, TAIL, V, TEAM, false, ONCE>), grid, block, 0, st, a);     \
   } while (0)
-#define MOE_NORM_BWD(T, V, TEAM)                       \
+#define MOE_NORM_BWD(T, TAIL, V, TEAM)                       \
   do {                                                 \
-    if (once) MOE_NORM_BWD_AS(T, V, TEAM, true);       \
-    else MOE_NORM_BWD_AS(T, V, TEAM, false);           \
+    if (once) MOE_NORM_BWD_AS(T, TAIL, V, TEAM, true);       \
+    else MOE_NORM_BWD_AS(T, TAIL, V, TEAM, false);           \
   } while (0)
-#define MOE_NORM_BWD_BY_PLAN(T)                                                 \
-  do {                                                                          \
-    if (p.team == kLongTeam) MOE_NORM_BWD_AS(T, 2, kLongTeam, false);           \
-    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_BWD(T, 2, kBlockTeam);  \
-    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, 1, kBlockTeam);              \
-    else if (p.V == 2) MOE_NORM_BWD(T, 2, kWaveTeam);                           \
-    else if (p.team == kLanes16Team) MOE_NORM_BWD(T, 1, kLanes16Team);          \
-    else if (p.team == kLanes32Team) MOE_NORM_BWD(T, 1, kLanes32Team);          \
-    else MOE_NORM_BWD(T, 1, kWaveTeam);                                         \
+#define MOE_NORM_BWD_BY_PLAN(T, TAIL, TINY, BY_VALUE)                                          \
+  do {                                                                               \
+    if (p.team == kLongTeam) MOE_NORM_BWD_AS(T, BY_VALUE, 2, kLongTeam, false);      \
+    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_BWD(T, TAIL, 2, kBlockTeam); \
+    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, TAIL, 1, kBlockTeam);             \
+    else if (p.V == 2) MOE_NORM_BWD(T, TAIL, 2, kWaveTeam);                          \
+    else if (p.team == kLanes16Team) MOE_NORM_BWD(T, TINY, 1, kLanes16Team);         \
+    else if (p.team == kLanes32Team) MOE_NORM_BWD(T, TAIL, 1, kLanes32Team);         \
+    else MOE_NORM_BWD(T, TAIL, 1, kWaveTeam);                                        \
   } while (0)
-    if (norm->dtype == MOE_F32) MOE_NORM_BWD_BY_PLAN(float);
-    else MOE_NORM_BWD_BY_PLAN(bf16_t);
+    if (norm->dtype == MOE_F32) MOE_NORM_BWD_BY_PLAN(float, kByValue, kByValue, kByValue);
+    else if (d % 8) MOE_NORM_BWD_BY_PLAN(bf16_t, kTail, kTinyTail, kByValue);
+    else MOE_NORM_BWD_BY_PLAN(bf16_t, kNoTail, kNoTail, kNoTail);
 #undef MOE_NORM_BWD_BY_PLAN
 #undef MOE_NORM_BWD
 #undef MOE_NORM_BWD_AS

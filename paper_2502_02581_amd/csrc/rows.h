@@ -8,7 +8,10 @@ namespace moe {
 
 // ---- pieces: eight neighbouring values of a row, 16 bytes in bf16, 32 in fp32.
 // Global loads and stores of 16 bytes need no alignment beyond that of a value here, so a row of any length at any address is full pieces and at
-// most one short one, which goes value by value.
+// most one short one.  Value by value, two bf16 values make a register, so the wavefront waits where it loads them instead of where it uses them; so a short bf16 piece is
+// loaded as the row's last eight values and settled (shifted down) in front of its use (norm's backward pass of 400 x 30: 6.2 us for 11.9; residual of 4000 x 2001 both ways
+// 49.8 for 56.1).  Of an output in place it may read values of the piece before that are overwritten already: they are shifted out.  In fp32 a value is a register, and they
+// are loaded one by one (777 x 333 backward 8.1 us, settled 9.2).  Stores are value by value.
 // Rows that nothing on the chip reads again soon are loaded with the streaming hint (ONCE): what the call writes, and what was written before it, then stays longer in the
 // memory-side cache (dropout of 16384 x 2048 and its adjoint 65.0 -> 60.1 us, a norm's step with residual stream, 8192 x 4096, 121 -> 117.5).  The same hint on stores makes the
 // call itself faster still (56.7 us) and the one that reads its results slower (the norm's backward pass 61.5 -> 68).
@@ -40,6 +43,14 @@ template <> struct Piece<bf16_t> {
     for (int i = 0; i < 4; i++) w[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
   }
   __device__ __forceinline__ void store(bf16_t* p) const { __builtin_memcpy(p, &w, 16); }
+  // without its first n values, 0 to 7
+  __device__ __forceinline__ void shift(int n) {
+    uint32_t a = w[0], b = w[1], c = w[2], d = w[3];
+    a = n & 4 ? c : a, b = n & 4 ? d : b, c = n & 4 ? 0u : c, d = n & 4 ? 0u : d;
+    a = n & 2 ? b : a, b = n & 2 ? c : b, c = n & 2 ? d : c, d = n & 2 ? 0u : d;
+    a = n & 1 ? a >> 16 | b << 16 : a, b = n & 1 ? b >> 16 | c << 16 : b, c = n & 1 ? c >> 16 | d << 16 : c, d = n & 1 ? d >> 16 : d;
+    w = (piece_u32x4){a, b, c, d};
+  }
 };
 template <> struct Piece<float> {
   piece_u32x4 w[2];
@@ -61,14 +72,22 @@ template <> struct Piece<float> {
     __builtin_memcpy(p + 4, &w[1], 16);
   }
 };
-// piece at p of which `valid` values (0 to 8, any other number counts as the nearer one) are part of the row; the others are zero
-template <bool ONCE = false, typename T>
-__device__ __forceinline__ void load_piece(Piece<T>& x, const T* p, int valid) {
-  if (valid >= 8) {
-    x.template load<ONCE>(p);
+// How the short piece is loaded.  kNoTail: there is none.  kTail: settled; kTinyTail: so too, unless the row has less than eight values.
+enum { kNoTail = 0, kTail = 1, kTinyTail = 2, kByValue = 3 };
+// by how much a piece whose first value is `col` is settled
+template <int TAIL>
+__device__ __forceinline__ int piece_back(int col, int valid) {
+  return (TAIL == kTail || TAIL == kTinyTail) && valid > 0 && valid < 8 && col > 0 ? 8 - valid : 0;
+}
+// piece at p of which `valid` values (0 to 8, any other number counts as the nearer one) are part of the row; the others are zero, once it is settled
+template <int TAIL, bool ONCE = false, typename T>
+__device__ __forceinline__ void load_piece(Piece<T>& x, const T* p, int valid, int back) {
+  constexpr bool SETTLED = TAIL == kTail || TAIL == kTinyTail;
+  if (valid + (SETTLED ? back : 0) >= 8) {
+    x.template load<ONCE>(SETTLED ? p - back : p);
   } else {
     x.clear();
-    if (valid > 0) {
+    if (TAIL >= kTinyTail && valid > 0) {
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; j++) v[j] = j < valid ? Elem<T>::load(p + j) : 0.f;
@@ -76,11 +95,15 @@ __device__ __forceinline__ void load_piece(Piece<T>& x, const T* p, int valid) {
     }
   }
 }
-template <typename T>
+template <int TAIL, typename T>
+__device__ __forceinline__ void settle(Piece<T>& x, int back) {
+  if constexpr (TAIL == kTail || TAIL == kTinyTail) x.shift(back);
+}
+template <int TAIL = kByValue, typename T>
 __device__ __forceinline__ void store_piece(const Piece<T>& x, T* p, int valid) {
   if (valid >= 8) {
     x.store(p);
-  } else if (valid > 0) {
+  } else if (TAIL && valid > 0) {
     float v[8];
     x.values(v);
 #pragma unroll

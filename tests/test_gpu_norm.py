@@ -154,7 +154,7 @@ def test_means_around_the_lines(n, d, offset):
     run(n, d, "f32", "f32", "layer", "plain", offset=offset)
 
 
-@pytest.mark.parametrize("d", [48, 5000])
+@pytest.mark.parametrize("d", [48, 5000, 20, 200])
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 def test_rows_that_are_not_finite_stay_alone(kind, d):
     """NaN and infinities reach their own row and no other; a constant row has the deviation sqrt(eps)."""
@@ -173,7 +173,16 @@ def test_rows_that_are_not_finite_stay_alone(kind, d):
         assert torch.isnan(Y[3]).all() and not Y[4].any() and abs(float(rstd[4]) * EPS ** 0.5 - 1) < 1e-6
 
 
-@pytest.mark.parametrize("n,d", [(50, 96), (50, 7000), (700, 520), (9, 9000)])
+@pytest.mark.parametrize("mode", ["plain", "drop"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d", [(1, 6), (300, 7), (70, 15), (37, 127), (41, 128), (45, 130), (21, 255), (23, 256), (33, 257), (2100, 27), (2000, 203), (1500, 505), (1100, 1021), (1100, 1029),
+                                 (1100, 2500), (1100, 3001), (1030, 8191), (20, 8199)])
+def test_short_pieces(n, d, dtype, mode):
+    """Rows that end inside a piece, for every size of team, with few rows and many."""
+    run(n, d, dtype, "f32", "layer", mode)
+
+
+@pytest.mark.parametrize("n,d", [(50, 96), (50, 7000), (700, 520), (9, 9000), (50, 97), (700, 15), (60, 1030), (1100, 3005)])
 def test_outputs_that_are_inputs(n, d):
     """The residual stream updated in place, the gradient written over the one that came in, or over the saved rows: what it is into tensors of their own, the same bits (the
     weights' gradients, which then take another order: within fp32's rounding of their sums, and bf16's)."""
