@@ -612,22 +612,23 @@ extern "C" int moe_norm_fwd(const moe_norm_t* norm, const void* X, int64_t ldx, 
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid(p.blocks), block(64 * p.waves);
   ProfScope prof("norm_fwd_kernel", st);
-#define MOE_NORM_FWD_BY_PLAN(T, TAIL, TINY, BY_VALUE)                                             \
-  do {                                                                                  \
-    if (p.team == kLongTeam) MOE_NORM_FWD(T, BY_VALUE, 2, kLongTeam);                   \
-    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_FWD(T, BY_VALUE, 2, kBlockTeam); \
-    else if (p.team == kBlockTeam) MOE_NORM_FWD(T, TAIL, 1, kBlockTeam);                \
-    else if (p.V == 2) MOE_NORM_FWD(T, BY_VALUE, 2, kWaveTeam);                         \
-    else if (p.team == kLanes16Team) MOE_NORM_FWD(T, TINY, 1, kLanes16Team);            \
-    else if (p.team == kLanes32Team) MOE_NORM_FWD(T, TAIL, 1, kLanes32Team);            \
-    else MOE_NORM_FWD(T, TAIL, 1, kWaveTeam);                                           \
+// (blocks of two pieces a lane are the plan of bf16 rows alone, and in the backward pass of full pieces)
+#define MOE_NORM_FWD_BY_PLAN(T, TAIL, TINY, BY_VALUE)                                         \
+  do {                                                                                        \
+    if (p.team == kLongTeam) MOE_NORM_FWD(T, BY_VALUE, 2, kLongTeam);                         \
+    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_FWD(bf16_t, BY_VALUE, 2, kBlockTeam); \
+    else if (p.team == kBlockTeam) MOE_NORM_FWD(T, TAIL, 1, kBlockTeam);                      \
+    else if (p.V == 2) MOE_NORM_FWD(T, BY_VALUE, 2, kWaveTeam);                               \
+    else if (p.team == kLanes16Team) MOE_NORM_FWD(T, TINY, 1, kLanes16Team);                  \
+    else if (p.team == kLanes32Team) MOE_NORM_FWD(T, TAIL, 1, kLanes32Team);                  \
+    else MOE_NORM_FWD(T, TAIL, 1, kWaveTeam);                                                 \
   } while (0)
 #define MOE_NORM_FWD(T, TAIL, V, TEAM)                                                                                \
-  do {                                                                                                          \
-    if (!sum && rstd) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kPlain>), grid, block, 0, st, a);          \
-    else if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kPass>), grid, block, 0, st, a);              \
+  do {                                                                                                                \
+    if (!sum && rstd) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kPlain>), grid, block, 0, st, a);         \
+    else if (!sum) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kPass>), grid, block, 0, st, a);             \
     else if (dr.threshold == 0) hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kAdd>), grid, block, 0, st, a); \
-    else hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kDrop>), grid, block, 0, st, a);                        \
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, TAIL, V, TEAM, kDrop>), grid, block, 0, st, a);                       \
   } while (0)
   if (norm->dtype == MOE_F32) MOE_NORM_FWD_BY_PLAN(float, kByValue, kByValue, kByValue);
   else if (d % 8) MOE_NORM_FWD_BY_PLAN(bf16_t, kTail, kTinyTail, kByValue);
@@ -685,25 +686,25 @@ extern "C" int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy
     const dim3 grid(p.blocks + (weights ? p.columns : 0)), block(64 * p.waves);
     const bool once = dZ && !p.columns;
     ProfScope prof("norm_bwd_kernel", st);
-#define MOE_NORM_BWD_AS(T, TAIL, V, TEAM, ONCE)                                                          \
-  do {                                                                                             \
+#define MOE_NORM_BWD_AS(T, TAIL, V, TEAM, ONCE)                                                           \
+  do {                                                                                                    \
     if (drop) hipLaunchKernelGGL((norm_bwd_kernel<T, TAIL, V, TEAM, true, ONCE>), grid, block, 0, st, a); \
     else hipLaunchKernelGGL((norm_bwd_kernel<T, TAIL, V, TEAM, false, ONCE>), grid, block, 0, st, a);     \
   } while (0)
-#define MOE_NORM_BWD(T, TAIL, V, TEAM)                       \
+#define MOE_NORM_BWD(T, TAIL, V, TEAM)                 \
   do {                                                 \
-    if (once) MOE_NORM_BWD_AS(T, TAIL, V, TEAM, true);       \
-    else MOE_NORM_BWD_AS(T, TAIL, V, TEAM, false);           \
+    if (once) MOE_NORM_BWD_AS(T, TAIL, V, TEAM, true); \
+    else MOE_NORM_BWD_AS(T, TAIL, V, TEAM, false);     \
   } while (0)
-#define MOE_NORM_BWD_BY_PLAN(T, TAIL, TINY, BY_VALUE)                                          \
-  do {                                                                               \
-    if (p.team == kLongTeam) MOE_NORM_BWD_AS(T, BY_VALUE, 2, kLongTeam, false);      \
-    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_BWD(T, TAIL, 2, kBlockTeam); \
-    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, TAIL, 1, kBlockTeam);             \
-    else if (p.V == 2) MOE_NORM_BWD(T, TAIL, 2, kWaveTeam);                          \
-    else if (p.team == kLanes16Team) MOE_NORM_BWD(T, TINY, 1, kLanes16Team);         \
-    else if (p.team == kLanes32Team) MOE_NORM_BWD(T, TAIL, 1, kLanes32Team);         \
-    else MOE_NORM_BWD(T, TAIL, 1, kWaveTeam);                                        \
+#define MOE_NORM_BWD_BY_PLAN(T, TAIL, TINY, BY_VALUE)                                        \
+  do {                                                                                       \
+    if (p.team == kLongTeam) MOE_NORM_BWD_AS(T, BY_VALUE, 2, kLongTeam, false);              \
+    else if (p.team == kBlockTeam && p.V == 2) MOE_NORM_BWD(bf16_t, kNoTail, 2, kBlockTeam); \
+    else if (p.team == kBlockTeam) MOE_NORM_BWD(T, TAIL, 1, kBlockTeam);                     \
+    else if (p.V == 2) MOE_NORM_BWD(T, TAIL, 2, kWaveTeam);                                  \
+    else if (p.team == kLanes16Team) MOE_NORM_BWD(T, TINY, 1, kLanes16Team);                 \
+    else if (p.team == kLanes32Team) MOE_NORM_BWD(T, TAIL, 1, kLanes32Team);                 \
+    else MOE_NORM_BWD(T, TAIL, 1, kWaveTeam);                                                \
   } while (0)
     if (norm->dtype == MOE_F32) MOE_NORM_BWD_BY_PLAN(float, kByValue, kByValue, kByValue);
     else if (d % 8) MOE_NORM_BWD_BY_PLAN(bf16_t, kTail, kTinyTail, kByValue);
