@@ -41,10 +41,10 @@ struct NormPlan {
 inline NormPlan norm_plan(const moe_norm_t* n, bool backward, bool drop, bool in_place) {
   const int pieces = (n->d + 7) / 8, rows = n->n_rows;
   const auto at_most = [](int x, int most) { return x < most ? x : most; };
-  const auto evenly = [&](int teams, int blocks) {  // no more blocks of so many teams than give the same number of rounds
+  const auto evenly = [&](int64_t teams, int blocks) {  // no more blocks of so many teams than give the same number of rounds
     if (rows == 0) return 0;
-    const int per = (rows + teams * blocks - 1) / (teams * blocks);
-    return (rows + teams * per - 1) / (teams * per);
+    const int64_t per = (rows + teams * blocks - 1) / (teams * blocks);  // (a block's rows are many where all are: the sums pass 2^31)
+    return (int)((rows + teams * per - 1) / (teams * per));
   };
   NormPlan p = {};
   const int elem = n->dtype == MOE_F32 ? 4 : 2;

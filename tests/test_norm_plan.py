@@ -26,6 +26,16 @@ extern "C" long last_index(int rows, int dtype, int backward, int drop, int in_p
   }
   return last;
 }
+// widths whose plan has not one block of rows at least and 2048 at most, or more of them than a team each needs
+extern "C" int unfit(int rows, int dtype, int backward, int drop, int in_place) {
+  int bad = 0;
+  for (int d = 1; d <= kNormMaxD; d++) {
+    const moe_norm_t n = {rows, d, dtype, dtype, 0, 0.f};
+    const NormPlan p = norm_plan(&n, backward, drop, in_place);
+    bad += p.blocks < 1 || p.blocks > 2048 || (p.blocks - 1) * teams(p) >= rows;
+  }
+  return bad;
+}
 """
 
 
@@ -60,3 +70,22 @@ def test_the_line_of_row_counts(plan):
     lib = moe.load_library()
     assert lib.moe_norm_bwd_workspace_bytes(ctypes.byref(_CNorm(plan.max_rows(), 8, 1, 1, 0, 1e-5))) > 0
     assert lib.moe_norm_bwd_workspace_bytes(ctypes.byref(_CNorm(plan.max_rows() + 1, 8, 1, 1, 0, 1e-5))) == 0
+
+
+ROWS = (1, 7, 1000, 1 << 20, 1 << 30, 2143297000, 2143400000, 2 ** 31 - 2 ** 15 - 2, 2 ** 31 - 2 ** 15 - 1)   # (the last: the largest accepted)
+
+
+@pytest.mark.parametrize("rows", ROWS)
+def test_blocks(plan, rows):
+    """Every plan has blocks, and none that no row is left for."""
+    for form in forms():
+        assert plan.unfit(rows, *form) == 0, form
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("d", [1, 128, 200, 1000, 1100, 7168, 16384])
+def test_workspace(rows, d):
+    """Two rows of sums for each of 2048 blocks at most."""
+    for dtype, kind in itertools.product((0, 1), (0, 1)):
+        need = moe.load_library().moe_norm_bwd_workspace_bytes(ctypes.byref(_CNorm(rows, d, dtype, 0, kind, 1e-5)))
+        assert 8 * d <= need <= 2048 * 8 * d + 256, (need, dtype)
