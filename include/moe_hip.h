@@ -484,7 +484,8 @@ int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy, const voi
  *   (as in moe_aux_loss);  0 for empty sequences
  *   loss[0] = alpha / S' sum_s E sum_e f_se P_se;    loss[1] = beta / T' sum_t lse_t^2, lse_t = log sum_e exp(logits_te)   (0 without tokens)
  *   Backward, the loads held constant: dlogits of dloss (loss[0] + loss[1]); rows of no sequence get zeros, or nothing when accumulate != 0.
- *   Rows whose logits are all -inf (sigmoid: whose scores are all 0 in fp32) have shares and lse 0; other rows may hold -inf.  topk_idx outside 0..E-1 is not counted.
+ *   Rows whose logits are all -inf have shares and lse 0, and rows whose sigmoid scores are all 0 in fp32 shares of 0; other rows may hold -inf.  A NaN among a token's logits
+ *   reaches its own row of dlogits, its sequence's row of P and both losses.  topk_idx outside 0..E-1 is not counted.
  *   logits, dlogits [T, E] f32 (dlogits may be logits when accumulate == 0); topk_idx [T, k]; seq_start, seq_len i32 (device); counts [n_seqs, E] i32 out; P [n_seqs, E] f32 out; loss [2] f32 out;
  *   coef [n_seqs + 1] f32 out: alpha E / (S' k T_s^2) for every sequence, 2 beta / T': what the backward pass takes from the forward pass, besides counts.
  *   shape gives T (below 2^31 - 2^16), E, k and gate.  ws >= moe_seq_loss_workspace_bytes(shape, n_seqs).  All sums in a fixed order: two calls give the same bits.

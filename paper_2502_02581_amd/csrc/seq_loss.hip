@@ -138,7 +138,7 @@ __device__ __forceinline__ void load_logits(const float* row, int l, int E, bool
 }
 // The exponentials are the instruction's, 2^(x log2 e): off by 1.5 |x| + 2 roundings, so a share e^-10 of the row's largest by 17, the largest by none.  (The kernels are bound by
 // their instructions before they are by bytes: with expf and divisions 131072 tokens of 64 experts take 14.7 + 18.4 us.)
-// soft: softmax; score, share: the gate's; lse.  A row without a finite logit has shares and lse 0, as has one whose sigmoid scores are all 0 in fp32.
+// soft: softmax; score, share: the gate's; lse.  A row of -inf alone has shares and lse 0, one whose sigmoid scores are all 0 in fp32 shares of 0.  NaN in a row is in all of them.
 template <int L, int Q>
 __device__ __forceinline__ void gate_row(const Row<Q>& x, int l, int E, bool softmax, bool need_soft, Row<Q>& soft, Row<Q>& score, Row<Q>& share, float& lse) {
   lse = 0.f;
@@ -149,16 +149,17 @@ __device__ __forceinline__ void gate_row(const Row<Q>& x, int l, int E, bool sof
 #pragma unroll
       for (int j = 0; j < 4; j++) m = fmaxf(m, x.v[q][j]);
     m = group_max<L>(m);
-    const bool empty = m == -INFINITY;
+    if (m == -INFINITY) m = 0.f;  // nothing but -inf, whose sum is 0, and NaN, which the maximum passes over and the sum does not
     float s = 0.f;
 #pragma unroll
     for (int q = 0; q < Q; q++)
 #pragma unroll
       for (int j = 0; j < 4; j++) {
-        soft.v[q][j] = empty ? 0.f : __expf(x.v[q][j] - m);
+        soft.v[q][j] = __expf(x.v[q][j] - m);
         s += soft.v[q][j];
       }
     s = group_sum<L>(s);
+    const bool empty = s == 0.f;  // (any other row's largest value adds 1)
     const float inv = empty ? 0.f : reciprocal(s);
     lse = empty ? 0.f : m + __logf(s);
 #pragma unroll
