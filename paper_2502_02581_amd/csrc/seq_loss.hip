@@ -138,9 +138,9 @@ __device__ __forceinline__ void load_logits(const float* row, int l, int E, bool
 }
 // The exponentials are the instruction's, 2^(x log2 e): off by 1.5 |x| + 2 roundings, so a share e^-10 of the row's largest by 17, the largest by none.  (The kernels are bound by
 // their instructions before they are by bytes: with expf and divisions 131072 tokens of 64 experts take 14.7 + 18.4 us.)
-// soft: softmax; score, share: the gate's; lse.  A row of -inf alone has shares and lse 0, one whose sigmoid scores are all 0 in fp32 shares of 0.  NaN in a row is in all of them.
+// soft: softmax; share: the gate's; rest: what its sigmoid scores lack to 1; lse.  A row of -inf alone has shares and lse 0, one whose sigmoid scores are all 0 in fp32 shares of 0.  NaN in a row is in all of them.
 template <int L, int Q>
-__device__ __forceinline__ void gate_row(const Row<Q>& x, int l, int E, bool softmax, bool need_soft, Row<Q>& soft, Row<Q>& score, Row<Q>& share, float& lse) {
+__device__ __forceinline__ void gate_row(const Row<Q>& x, int l, int E, bool softmax, bool need_soft, Row<Q>& soft, Row<Q>& rest, Row<Q>& share, float& lse) {
   lse = 0.f;
   if (softmax || need_soft) {
     float m = -INFINITY;
@@ -172,12 +172,15 @@ __device__ __forceinline__ void gate_row(const Row<Q>& x, int l, int E, bool sof
     return;
   }
   float s = 0.f;
+  Row<Q> score;
 #pragma unroll
   for (int q = 0; q < Q; q++)
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       const bool in = 4 * (l + L * q) + j < E;
-      score.v[q][j] = in ? __builtin_amdgcn_rcpf(1.f + __expf(-x.v[q][j])) : 0.f;
+      const float e = __expf(-x.v[q][j]);
+      score.v[q][j] = in ? __builtin_amdgcn_rcpf(1.f + e) : 0.f;
+      rest.v[q][j] = e < 1.f ? e * score.v[q][j] : 1.f - score.v[q][j];  // (the difference has few bits left where the score is close to 1)
       s += score.v[q][j];
     }
   s = group_sum<L>(s);
@@ -216,8 +219,8 @@ __device__ __forceinline__ void chunk_sums(const SeqArgs& a, int c, int wave, in
     ids = i < (int64_t)t1 * a.k ? a.topk[i] : -1;
   };
   auto use = [&]() {
-    Row<Q> soft, score;
-    gate_row<L, Q>(x, l, a.E, softmax, want_z, soft, score, share, lse);
+    Row<Q> soft, rest;
+    gate_row<L, Q>(x, l, a.E, softmax, want_z, soft, rest, share, lse);
     id = ids;
     if (at + GW < t1) load(at + GW);
   };
@@ -639,9 +642,9 @@ __global__ __launch_bounds__(256) void seq_bwd_kernel(SeqArgs a, const int32_t* 
 #pragma unroll
       for (int j = 0; j < 4; j++) dz.v[q][j] = 0.f;
     if (now >= 0) {
-      Row<Q> soft, score, share;
+      Row<Q> soft, rest, share;
       float lse, dot = 0.f;
-      gate_row<L, Q>(x, l, a.E, softmax, cz != 0.f, soft, score, share, lse);
+      gate_row<L, Q>(x, l, a.E, softmax, cz != 0.f, soft, rest, share, lse);
 #pragma unroll
       for (int q = 0; q < Q; q++)
 #pragma unroll
@@ -653,7 +656,7 @@ __global__ __launch_bounds__(256) void seq_bwd_kernel(SeqArgs a, const int32_t* 
 #pragma unroll
         for (int j = 0; j < 4; j++) {
           dz.v[q][j] = share.v[q][j] * (up.v[q][j] - dot);
-          if (!softmax) dz.v[q][j] *= 1.f - score.v[q][j];
+          if (!softmax) dz.v[q][j] *= rest.v[q][j];
           if (cz != 0.f) dz.v[q][j] = fmaf(zl, soft.v[q][j], dz.v[q][j]);
         }
     }
