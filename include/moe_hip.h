@@ -446,7 +446,7 @@ int moe_grad_clip(const moe_grad_t* grads, int32_t n, const float* norm, float m
  *   MOE_NORM_LAYER: mean = sum Z / d, v = sum (Z - mean)^2 / d;   MOE_NORM_RMS: mean = 0, v = sum Z^2 / d;
  *   rstd = 1 / sqrt(v + eps);   Y = (Z - mean) rstd w + b
  *   w, b [d] in wdtype; NULL: ones, zeros.  mean, rstd [n_rows] f32 out, kept for the backward pass; either may be NULL (RMS has no mean).  1 <= d <= 16384, n_rows < 2^31 - 2^15.
- *   Sums are fp32 (a row whose squares' sum is beyond their range has rstd 0), the mean's own rounding error is taken out of Z - mean (in both passes), Y is rounded once.  Z may be X or R, Y the one
+ *   Sums are fp32 (a row whose squares' sum is beyond their range has rstd 0), the mean's own rounding error is taken out of Z - mean (in both passes) and of v, so a constant row has v = 0; Y is rounded once.  Z may be X or R, Y the one
  *   of them that Z is not (same address and stride).
  * moe_norm_bwd -- g = dY w;  h = (Z - mean) rstd;  dZtotal = dZ + rstd (g - mean(g) [layer] - h mean(g h));
  *   dR = dZtotal;  dX = drop'(dZtotal) (with drop: the mask of the forward pass; dX is then required and dR may be NULL);

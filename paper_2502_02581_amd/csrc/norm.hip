@@ -129,27 +129,38 @@ __global__ __launch_bounds__(!wide_team(TEAM) ? 256 : TEAM == kBlockTeam && V ==
       if (WIDE) sums.sum(s, wave, n_waves, turn);
       else s[0] = team_sum<TEAM>(s[0]);
       m = s[0] * inv_d;
-      float t[2] = {0.f, 0.f};
+      // Once, but for rows whose squares are the mean's error for the most part (constant ones of 1e9: 3600 for 0), where delta takes nearly all of them away and leaves its
+      // rounding: again around the better mean, whose error is 2^-18 of that at most.  (The lanes of a team go round alike, their sums have the same bits.)
+      float step = m;
+#pragma unroll 1
+      for (int round = 0;; round++) {
+        float t[2] = {0.f, 0.f};
 #pragma unroll
-      for (int v = 0; v < V; v++) {
+        for (int v = 0; v < V; v++) {
 #pragma unroll
-        for (int j = 0; j < 8; j++) z[v][j] = j < valid[v] ? z[v][j] - m : 0.f;
+          for (int j = 0; j < 8; j++) z[v][j] = j < valid[v] ? z[v][j] - step : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          t[0] += z[v][j];
-          t[1] = fmaf(z[v][j], z[v][j], t[1]);
+          for (int j = 0; j < 8; j++) {
+            t[0] += z[v][j];
+            t[1] = fmaf(z[v][j], z[v][j], t[1]);
+          }
         }
-      }
-      if (WIDE) {
-        sums.sum(t, wave, n_waves, turn);
-      } else {
-        t[0] = team_sum<TEAM>(t[0]);
-        t[1] = team_sum<TEAM>(t[1]);
-      }
-      var = t[1] / (float)a.d;
-      if (m * m > var) {
-        delta = t[0] * inv_d;
-        var -= delta * delta;
+        if (WIDE) {
+          sums.sum(t, wave, n_waves, turn);
+        } else {
+          t[0] = team_sum<TEAM>(t[0]);
+          t[1] = team_sum<TEAM>(t[1]);
+        }
+        var = t[1] / (float)a.d;
+        if (!(m * m > var)) break;
+        step = t[0] * inv_d;
+        const float left = var - step * step;
+        if (left >= 0.5f * var || round == 2) {
+          delta = step;
+          var = left < 0.f ? 0.f : left;
+          break;
+        }
+        m += step;
       }
     } else {
       float t[1] = {0.f};
