@@ -65,6 +65,16 @@ class _CDrop(ctypes.Structure):   # moe_drop_t
     _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("rng", ctypes.c_void_p)]
 
 
+_INT32 = 1 << 31
+
+
+def _fits(who, *sizes):
+    """Refuses sizes that the library's 32-bit arguments do not hold: ctypes would cut them off in silence."""
+    for n in sizes:
+        if not -_INT32 <= n < _INT32:
+            raise MoEError(f"{who}: a size of {n} is beyond 32 bits")
+
+
 @dataclasses.dataclass(frozen=True)
 class MoEShape:
     T: int
@@ -75,6 +85,9 @@ class MoEShape:
     dtype: str = "bf16"      # "f32" | "bf16"
     gate: str = "softmax"    # "softmax" | "sigmoid"
     renorm: bool = True
+
+    def __post_init__(self):
+        _fits("MoEShape", self.T, self.d, self.E, self.k, self.d_ff)
 
     def c(self) -> _CShape:
         c = self.__dict__.get("_c")   # the members never change, so their C form is made once
@@ -103,6 +116,7 @@ class MoENorm:
         for value, known in ((self.kind, ("layer", "rms")), (self.dtype, ("f32", "bf16")), (self.wdtype, ("", "f32", "bf16"))):
             if value not in known:
                 raise MoEError(f"MoENorm: {value!r} is none of {known}")
+        _fits("MoENorm", self.n_rows, self.d)
         code = {"f32": MOE_F32, "bf16": MOE_BF16}
         wdtype = self.wdtype or self.dtype
         types = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -296,10 +310,12 @@ def moe_dispatch_workspace_bytes(shape: MoEShape) -> int:
 
 
 def moe_expert_fwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int, shared: bool) -> int:
+    _fits("moe_expert_fwd_workspace_bytes", n_groups, n_rows)
     return load_library().moe_expert_fwd_workspace_bytes(ctypes.byref(shape.c()), n_groups, n_rows, int(shared))
 
 
 def moe_expert_bwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int, shared: bool) -> int:
+    _fits("moe_expert_bwd_workspace_bytes", n_groups, n_rows)
     return load_library().moe_expert_bwd_workspace_bytes(ctypes.byref(shape.c()), n_groups, n_rows, int(shared))
 
 
@@ -384,6 +400,7 @@ def moe_plan_predict_load(history, w: int = 5):
     h = np.ascontiguousarray(history, dtype=np.float64)
     if h.ndim != 2:
         raise MoEError("history must be [n_iters, E]")
+    _fits("moe_plan_predict_load", *h.shape, int(w))
     F = np.empty(h.shape[1], dtype=np.float64)
     _check(load_library().moe_plan_predict_load(h.ctypes.data, h.shape[0], h.shape[1], int(w), F.ctypes.data),
            "moe_plan_predict_load")
@@ -397,6 +414,7 @@ def moe_plan_materialize(P, F, t: int, m: int, dpn: int):
     if P.ndim != 2:
         raise MoEError("P must be [E, D]")
     E, D = P.shape
+    _fits("moe_plan_materialize", E, D, int(t), int(m), int(dpn))
     F = _host(F, np.float64, (E,), "F")
     out = np.empty_like(P)
     _check(load_library().moe_plan_materialize(E, D, int(dpn), P.ctypes.data, F.ctypes.data, int(t), int(m),
@@ -411,6 +429,7 @@ def moe_plan_dispatch(Pm, T, dpn: int):
     if Pm.ndim != 2:
         raise MoEError("Pm must be [E, D]")
     E, D = Pm.shape
+    _fits("moe_plan_dispatch", E, D, int(dpn))
     T = _host(T, np.int32, (E, D), "T")
     R = np.empty((E, D, D), dtype=np.int32)
     _check(load_library().moe_plan_dispatch(E, D, int(dpn), Pm.ctypes.data, T.ctypes.data, R.ctypes.data),
@@ -484,6 +503,7 @@ def moe_dispatch_static(shape: MoEShape, X, topk_idx, counts, offsets, row_of, s
 
 def moe_expert_fwd(shape: MoEShape, n_groups, offsets, n_rows, Xin, Wg, Wu, Wd, G, U, H, Yout, ws, stream=None):
     dt = shape.torch_dtype
+    _fits("moe_expert_fwd", n_groups, n_rows)
     rc = load_library().moe_expert_fwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, torch.int32, "offsets"), n_rows, _ptr(Xin, dt, "Xin"),
         _ptr(Wg, dt, "Wg"), _ptr(Wu, dt, "Wu"), _ptr(Wd, dt, "Wd"), _ptr(G, dt, "G"), _ptr(U, dt, "U"),
@@ -495,6 +515,7 @@ def moe_expert_fwd(shape: MoEShape, n_groups, offsets, n_rows, Xin, Wg, Wu, Wd, 
 def moe_expert_bwd(shape: MoEShape, n_groups, offsets, n_rows, Xin, Wg, Wu, Wd, G, U, H, dYin, dXin, active_ids,
                    n_active, dWg_c, dWu_c, dWd_c, ws, stream=None):
     dt = shape.torch_dtype
+    _fits("moe_expert_bwd", n_groups, n_rows)
     rc = load_library().moe_expert_bwd(
         ctypes.byref(shape.c()), n_groups, _ptr(offsets, torch.int32, "offsets"), n_rows, _ptr(Xin, dt, "Xin"),
         _ptr(Wg, dt, "Wg"), _ptr(Wu, dt, "Wu"), _ptr(Wd, dt, "Wd"), _ptr(G, dt, "G"), _ptr(U, dt, "U"),
@@ -530,6 +551,7 @@ def _expert_set(shape: MoEShape, d_ff, n_groups, n_rows, ws, ws_bytes, Xin=None,
                 H=None, Yout=None, offsets=None, src_of=None, dYin=None, dY=None, row_w=None, dXin=None, active_ids=None,
                 n_active=None, dWg_c=None, dWu_c=None, dWd_c=None, plan=None) -> _CExpertSet:
     dt, i32 = shape.torch_dtype, torch.int32
+    _fits("moe_expert_set_t", d_ff, n_groups, n_rows)
     return _CExpertSet(
         d_ff, n_groups, n_rows, _ptr(offsets, i32, "offsets"), _ptr(src_of, i32, "src_of"), _ptr(Xin, dt, "Xin"),
         _ptr(Wg, dt, "Wg"), _ptr(Wu, dt, "Wu"), _ptr(Wd, dt, "Wd"), _ptr(G, dt, "G"), _ptr(U, dt, "U"), _ptr(H, dt, "H"),
@@ -638,6 +660,8 @@ def moe_quant_rows(X, Q, S, stream=None):
     if n > 1 and X.stride(0) < cols:
         raise MoEError("X: rows must not overlap")
     _here("moe_quant_rows", X, Q, S)
+    if n >= _INT32 or cols >= _INT32:
+        _fits("moe_quant_rows", n, cols)
     rc = load_library().moe_quant_rows(X.data_ptr(), dt, n, cols, ldx, _sized(Q, (n, moe_quant_row_bytes(cols)), "Q"),
                                        _sized(S, (n, moe_quant_scale_bytes(cols)), "S"), _stream(stream))
     _check(rc, "moe_quant_rows")
@@ -654,6 +678,7 @@ def moe_quant_weights(W, Q, S, Qt, St, stream=None):
     args = []
     _ptr(W, None, "W")
     _here("moe_quant_weights", W, Q, S, Qt, St)
+    _fits("moe_quant_weights", g, K, N)
     for t, shape, what in ((Q, (g, K, moe_quant_row_bytes(N)), "Q"), (S, (g, b(K), b(N)), "S"),
                            (Qt, (g, N, moe_quant_row_bytes(K)), "Qt"), (St, (g, b(N), b(K)), "St")):
         args += _pitched(t, shape, what)
@@ -661,6 +686,7 @@ def moe_quant_weights(W, Q, S, Qt, St, stream=None):
 
 
 def moe_quant_gemm_workspace_bytes(n_groups: int, n_rows: int, K: int, N: int) -> int:
+    _fits("moe_quant_gemm_workspace_bytes", n_groups, n_rows, K, N)
     return int(load_library().moe_quant_gemm_workspace_bytes(n_groups, n_rows, K, N))
 
 
@@ -672,6 +698,7 @@ def moe_quant_gemm(offsets, K: int, A, As, B, Bs, C, ws, stream=None):
     (n, N), g = C.shape, B.shape[0]
     kb, rb = moe_quant_scale_bytes(K), moe_quant_row_bytes(K)
     _here("moe_quant_gemm", offsets, A, As, B, Bs, C, ws)
+    _fits("moe_quant_gemm", g, n, K, N)
     if offsets is not None:
         _sized(offsets, (g + 1,), "offsets", torch.int32)
     rc = load_library().moe_quant_gemm(g, _ptr(offsets, torch.int32, "offsets"), n, K, N, _sized(A, (n, rb), "A"), _sized(As, (n, kb), "As"),
@@ -745,15 +772,18 @@ class MoEQuantWeights:
 
 
 def moe_quant_expert_fwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int) -> int:
+    _fits("moe_quant_expert_fwd_workspace_bytes", n_groups, n_rows)
     return int(load_library().moe_quant_expert_fwd_workspace_bytes(ctypes.byref(shape.c()), n_groups, n_rows))
 
 
 def moe_quant_expert_bwd_workspace_bytes(shape: MoEShape, n_groups: int, n_rows: int) -> int:
+    _fits("moe_quant_expert_bwd_workspace_bytes", n_groups, n_rows)
     return int(load_library().moe_quant_expert_bwd_workspace_bytes(ctypes.byref(shape.c()), n_groups, n_rows))
 
 
 def _quant_args(shape, n_groups, n_rows, src_of, Q, S, W, who, *others):
     _here(who, src_of, Q, S, W.WgT[0], *others)
+    _fits(who, n_groups, n_rows)
     if W.n_groups != n_groups or (W.shape.d, W.shape.d_ff) != (shape.d, shape.d_ff):
         raise MoEError(f"{who}: the weights are those of {W.n_groups} experts of d={W.shape.d}, d_ff={W.shape.d_ff}")
     rows = n_rows if src_of is None else shape.T
@@ -909,6 +939,8 @@ def moe_dropout(X, drop: MoEDropout, out, R=None, stream=None):
     if X.dim() != 2:
         raise MoEError("X must be [n_rows, cols]")
     dt, (n, d) = X.dtype, X.shape
+    if n >= _INT32 or d >= _INT32:   # (0.04 us of the call, _fits by itself 0.2)
+        _fits("moe_dropout", n, d)
     device, stream = _current(stream)
     rc = load_library().moe_dropout(*_rows(X, n, d, dt, device, "X"), *_rows(R, n, d, dt, device, "R"), code, n, d, _drop(drop, device, "moe_dropout"),
                                     *_rows(out, n, d, dt, device, "out"), stream)
@@ -946,6 +978,7 @@ def moe_norm_bwd(norm: MoENorm, dY, Z, w, mean, rstd, dR, dw, db, ws, dZ=None, d
 
 
 def moe_seq_loss_workspace_bytes(shape: MoEShape, n_seqs: int) -> int:
+    _fits("moe_seq_loss_workspace_bytes", n_seqs)
     return int(load_library().moe_seq_loss_workspace_bytes(ctypes.byref(shape.c()), n_seqs))
 
 
@@ -960,6 +993,8 @@ def moe_seq_loss(shape: MoEShape, logits, topk_idx, seq_start, seq_len, alpha, b
     T, E = shape.T, shape.E
     device, stream = _current(stream)
     n, i32, f32 = counts.shape[0], torch.int32, torch.float32
+    if n >= _INT32:
+        _fits("moe_seq_loss", n)
     rc = load_library().moe_seq_loss(ctypes.byref(shape.c()), _vector(logits, T * E, f32, device, "logits"), _vector(topk_idx, T * shape.k, i32, device, "topk_idx"),
                                      n, *_seqs(seq_start, seq_len, n, device), alpha, beta, _vector(counts, n * E, i32, device, "counts"),
                                      _vector(P, n * E, f32, device, "P"), _vector(loss, 2, f32, device, "loss"), _vector(coef, n + 1, f32, device, "coef"),
@@ -973,6 +1008,8 @@ def moe_seq_loss_bwd(shape: MoEShape, logits, seq_start, seq_len, counts, coef, 
     T, E = shape.T, shape.E
     device, stream = _current(stream)
     n, i32, f32 = counts.shape[0], torch.int32, torch.float32
+    if n >= _INT32:
+        _fits("moe_seq_loss_bwd", n)
     rc = load_library().moe_seq_loss_bwd(ctypes.byref(shape.c()), _vector(logits, T * E, f32, device, "logits"), n, *_seqs(seq_start, seq_len, n, device),
                                          _vector(counts, n * E, i32, device, "counts"), _vector(coef, n + 1, f32, device, "coef"), dloss,
                                          bool(accumulate), _vector(dlogits, T * E, f32, device, "dlogits"), stream)
@@ -993,6 +1030,7 @@ def moe_mfma_probe(n_blocks: int, iters: int, sink: torch.Tensor) -> float:
     """Launches the register-resident matrix loop once; returns the FLOPs of the launch (time it outside)."""
     if sink.numel() < n_blocks * 256:
         raise MoEError("moe_mfma_probe: sink needs n_blocks * 256 floats")
+    _fits("moe_mfma_probe", n_blocks, iters)
     flops = ctypes.c_double(0.0)
     rc = load_library().moe_mfma_probe(int(n_blocks), int(iters), _ptr(sink, torch.float32, "sink"), ctypes.byref(flops),
                                        _stream(None))
