@@ -1093,7 +1093,8 @@ class MoEHotPath:
     weights in b["dWr"], b["dnorm_w"], b["dnorm_b"].  Given residual, forward() adds X, the output of the sublayer before, to it first: Z = residual + drop(X),
     out = Z + drop(MoE(norm(Z))); b["dZ"] is then the gradient of residual, and of X without dropout (with it, b["dBranch"]).  dropout: the probability; rng: int64 [2] on the
     GPU, seed and step, of which the program advances the step after every backward pass (rng[1] += 1), in a captured graph, too; the block's two masks have the sites
-    site and site + 1.  norm_dtype: the norm weights' type ("f32" or "bf16"; the layer's).
+    site and site + 1.  norm_dtype: the norm weights' type ("f32" or "bf16"; the layer's).  forward(training=False) evaluates: no masks, no statistics of the norm, and no
+    backward pass before the next forward one.
 
     With seq_alpha or z_beta, forward() also evaluates the balance loss of every sequence and the router's z loss (moe_seq_loss) into b["seq_loss"] [2], with b["seq_counts"],
     b["seq_P"] [n_seqs, E], and backward() adds their gradient to dlogits.  seqs = (seq_start, seq_len) says which tokens are whose; without it all are one
@@ -1174,7 +1175,7 @@ class MoEHotPath:
         f, f32 = dict(dtype=s.torch_dtype, device=dev), dict(dtype=torch.float32, device=dev)
         ws = 0
         self.norm, self.seq_alpha, self.z_beta = None, float(seq_alpha), float(z_beta)
-        self._block, self._seqs, self._added = None, (None, None), False
+        self._block, self._seqs, self._added, self._training = None, (None, None), False, True
         if self.seq_alpha or self.z_beta:
             b.update({"seq_counts": torch.empty(n_seqs, s.E, dtype=torch.int32, device=dev), "seq_P": torch.empty(n_seqs, s.E, **f32),
                       "seq_loss": torch.empty(2, **f32), "seq_coef": torch.empty(n_seqs + 1, **f32)})
@@ -1188,20 +1189,21 @@ class MoEHotPath:
         if self.dropout and rng is None:
             raise MoEError("dropout takes rng, its seed and step on the GPU")
         self.drop_in, self.drop_out = (MoEDropout(self.dropout, rng, site + i) for i in (0, 1))
+        self.drop_none = MoEDropout(0.0, None)
         b.update({n: torch.empty(s.T, s.d, **f) for n in ("Xn", "Z", "Out", "dZ") + (("dYd", "dBranch") if self.dropout else ())})
         b.update({"logits": torch.empty(s.T, s.E, **f32), "mean": torch.empty(s.T, **f32), "rstd": torch.empty(s.T, **f32), "dWr": torch.empty(s.d, s.E, **f)})
         b.update({n: torch.empty(s.d, dtype=self.norm.weight_dtype, device=dev) for n in ("dnorm_w", "dnorm_b")})
         return max(ws, moe_router_fwd_workspace_bytes(s), moe_router_bwd_workspace_bytes(s), moe_norm_bwd_workspace_bytes(self.norm))
 
-    def _enter(self, block, X, residual, stream):
+    def _enter(self, block, X, residual, training, stream):
         """The block's norm and router: the logits and rows that the experts take, and the residual stream."""
         b = self.b
         if not isinstance(block, MoEBlockWeights):
             raise MoEError("a layer with norm takes a MoEBlockWeights in the place of the logits")
-        mean = b["mean"] if self.norm.kind == "layer" else None
+        mean, rstd = b["mean"] if training and self.norm.kind == "layer" else None, b["rstd"] if training else None
         self._block, self._added = block, residual is not None
         Z = b["Z"] if self._added else X
-        moe_norm_fwd(self.norm, X, block.norm_w, block.norm_b, b["Xn"], mean, b["rstd"], R=residual, drop=self.drop_in if self._added and self.dropout else None,
+        moe_norm_fwd(self.norm, X, block.norm_w, block.norm_b, b["Xn"], mean, rstd, R=residual, drop=self.drop_in if training and self._added and self.dropout else None,
                      Z=b["Z"] if self._added else None, stream=stream)
         moe_router_fwd(self.shape, b["Xn"], block.Wr, b["logits"], self.ws, stream)
         return b["logits"], b["Xn"], Z
@@ -1240,12 +1242,13 @@ class MoEHotPath:
         if self.quant != isinstance(Wg, MoEQuantWeights) or (self.quant and (Wu is not None or Wd is not None)):
             raise MoEError("a layer with quant takes a MoEQuantWeights in the place of Wg, None for Wu and Wd; any other layer the matrices")
 
-    def forward(self, logits, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None, residual=None, seqs=None):
+    def forward(self, logits, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None, residual=None, seqs=None, training=True):
         s, b = self.shape, self.b
         A = s.T * s.k
         self._check_weights(Wg, Wu, Wd)
+        self._training = bool(training)
         if self.norm:
-            logits, X, Z = self._enter(logits, X, residual, stream)
+            logits, X, Z = self._enter(logits, X, residual, self._training, stream)
         elif residual is not None or isinstance(logits, MoEBlockWeights):
             raise MoEError("residual and MoEBlockWeights go with norm")
         main = self._fork(Wu, Wsu, stream)
@@ -1288,13 +1291,15 @@ class MoEHotPath:
             moe_seq_loss(s, logits, b["topk_idx"], *self._seqs, self.seq_alpha, self.z_beta, b["seq_counts"], b["seq_P"], b["seq_loss"], b["seq_coef"], self.ws, stream)
         if not self.norm:
             return b["Y"]
-        moe_dropout(b["Y"], self.drop_out, b["Out"], R=Z, stream=stream)
+        moe_dropout(b["Y"], self.drop_out if training else self.drop_none, b["Out"], R=Z, stream=stream)
         return b["Out"]
 
     def backward(self, dY, X, Wg, Wu=None, Wd=None, Wsg=None, Wsu=None, Wsd=None, stream=None):
         s, b = self.shape, self.b
         A = s.T * s.k
         self._check_weights(Wg, Wu, Wd)
+        if not self._training:
+            raise MoEError("backward: the last forward pass was one without training")
         if self.norm:
             if self._block is None:
                 raise MoEError("backward: there was no forward pass yet")
