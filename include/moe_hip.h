@@ -446,7 +446,7 @@ int moe_grad_clip(const moe_grad_t* grads, int32_t n, const float* norm, float m
  *   MOE_NORM_LAYER: mean = sum Z / d, v = sum (Z - mean)^2 / d;   MOE_NORM_RMS: mean = 0, v = sum Z^2 / d;
  *   rstd = 1 / sqrt(v + eps);   Y = (Z - mean) rstd w + b
  *   w, b [d] in wdtype; NULL: ones, zeros.  mean, rstd [n_rows] f32 out, kept for the backward pass; either may be NULL (RMS has no mean).  1 <= d <= 16384, n_rows < 2^31 - 2^15.
- *   Sums are fp32 (a row whose squares' sum is beyond their range has rstd 0), the mean's own rounding error is taken out of Z - mean (in both passes) and of v, so a constant row has v = 0; Y is rounded once.  Z may be X or R, Y the one
+ *   Sums are fp32 (a row whose squares' sum is beyond their range has rstd 0, one whose own sum is, NaN), the mean's own rounding error is taken out of Z - mean (in both passes) and of v, so a constant row has v = 0; Y is rounded once.  Z may be X or R, Y the one
  *   of them that Z is not (same address and stride).
  * moe_norm_bwd -- g = dY w;  h = (Z - mean) rstd;  dZtotal = dZ + rstd (g - mean(g) [layer] - h mean(g h));
  *   dR = dZtotal;  dX = drop'(dZtotal) (with drop: the mask of the forward pass; dX is then required and dR may be NULL);
@@ -485,10 +485,12 @@ int moe_norm_bwd(const moe_norm_t* norm, const void* dY, int64_t lddy, const voi
  *   loss[0] = alpha / S' sum_s E sum_e f_se P_se;    loss[1] = beta / T' sum_t lse_t^2, lse_t = log sum_e exp(logits_te)   (0 without tokens)
  *   Backward, the loads held constant: dlogits of dloss (loss[0] + loss[1]); rows of no sequence get zeros, or nothing when accumulate != 0.
  *   Rows whose logits are all -inf have shares and lse 0, and rows whose sigmoid scores are all 0 in fp32 shares of 0; other rows may hold -inf.  A NaN among a token's logits
- *   reaches its own row of dlogits, its sequence's row of P and both losses.  topk_idx outside 0..E-1 is not counted.
+ *   reaches its own row of dlogits, its sequence's row of P and both losses (the z loss where beta is not 0).  topk_idx outside 0..E-1 is not counted.
  *   logits, dlogits [T, E] f32 (dlogits may be logits when accumulate == 0); topk_idx [T, k]; seq_start, seq_len i32 (device); counts [n_seqs, E] i32 out; P [n_seqs, E] f32 out; loss [2] f32 out;
  *   coef [n_seqs + 1] f32 out: alpha E / (S' k T_s^2) for every sequence, 2 beta / T': what the backward pass takes from the forward pass, besides counts.
  *   shape gives T (below 2^31 - 2^16), E, k and gate.  ws >= moe_seq_loss_workspace_bytes(shape, n_seqs).  All sums in a fixed order: two calls give the same bits.
+ *   Exponentials, logarithms and reciprocals are the instructions' (moe_route_bwd and moe_aux_loss take expf and divide): a share is off by 2 |logit - the row's largest| + 16
+ *   (sigmoid: 4 |logit| + 16 with the row's farthest from 0) roundings of 2^-24 at most, sums of shares are fp32.  The gradient's 1 - score behind a sigmoid gate is as exact where the score is close to 1.
  */
 size_t moe_seq_loss_workspace_bytes(const moe_shape_t* shape, int32_t n_seqs);
 int moe_seq_loss(const moe_shape_t* shape, const float* logits, const int32_t* topk_idx, int32_t n_seqs, const int32_t* seq_start, const int32_t* seq_len,

@@ -3,7 +3,8 @@
 //   z = r + drop(x);   layer: m = mean z, v = mean (z - m)^2;   rms: m = 0, v = mean z^2;   s = 1 / sqrt(v + eps);   h = (z - m) s;   y = h w + b
 //   g = dy w;   dz = dz_in + s (g - mean g [layer] - h mean(g h));   dr = dz;   dx = drop'(dz);   dw = sum over rows of dy h;   db = sum over rows of dy
 //
-// Both passes are bound by HBM.  A row stays in the registers of its team (a wavefront, or the wavefronts of a block) from its one load to its one store.
+// Both passes are bound by HBM.  A row stays in the registers of its team (16 or 32 lanes, a wavefront, or the wavefronts of a block) from its one load to its one store; but in
+// the backward pass rows of more than 8192 values are read twice, and so are those beside which blocks of columns add up the weights' gradients.
 #include "norm_plan.h"
 #include "rows.h"
 
